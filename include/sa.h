@@ -68,12 +68,27 @@ typedef enum {
 } sa_status;
 
 /* Key code family: the value is k, the number of mantissa bits (eq. (2), eq. (5)). */
-enum { SA_POT4 = 0, SA_POTM1 = 1, SA_POTM2 = 2, SA_POTM4 = 4, SA_INT8 = 8, SA_KV_FP16 = 16 };
+enum { SA_POT4 = 0, SA_POTM1 = 1, SA_POTM2 = 2, SA_POTM4 = 4, SA_INT8 = 8, SA_KV_FP16 = 16, SA_KV_FP4 = 32 };
 /* SA_INT8 is the comparison code of section III / VI (an INT8 multiply-accumulate kernel built on the
  * same skeleton as the shift kernels): uniform INT8 keys, khat = round(K * 127 / amax) with the row maximum as
  * scale, stored one byte per element in the byte container (132 bytes per key at d = 64, the same
  * as PoT-M4); scores are integer dot products with INT32 sums.  Everything else (query and
  * value quantisers, softmax, A.V, merge, cache layout) is shared with the power-of-two codes. */
+/* SA_KV_FP4: keys AND values in 4 bits, (the paper has no counterpart: its caches hold values in 8).  A vector of head_dim channels is
+ * cut into blocks of 16.  A block's scale is s = max|x| / 6 rounded to the nearest unsigned 8-bit float (5 bits of exponent, 3 of
+ * mantissa, ties to even), at most 10240, held as a byte b: s is the binary16 number of the bits b << 7.  A channel's code is x / s rounded to the nearest
+ * of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (numbers 0 .. 7 of its lowest three bits; ties to the even number, 6 at most), bit 3 the sign (which a zero may or may not
+ * carry); it stands for code * s, exactly a binary16 number.  A block of at most 2.28e-5 (6 * 2^-18) throughout is zeros; beyond 61440 channels saturate there.
+ * d + d / 8 bytes per key: 72 at head_dim 64, 144 at 128.  Queries stay binary16 (rotated first with SA_FLAG_HADAMARD), the
+ * attention is softmax(Q K^T / sqrt(d)) V of eq. (1) over the numbers that the codes stand for.  Layout in each half block (t = token % 32, c = channel):
+ *   key codes at kcode_off    : chunk k = 2 (c / 64) + c / 8 % 2 of 16 bytes a token at (k * 32 + t) * 16; byte c / 16 % 4 * 4 + c % 8 / 2 of it holds
+ *                               channels c (even; low nibble) and c + 1;
+ *   key scales at meta_off    : byte c / 64 * 128 + c / 16 % 4 * 32 + t % 8 * 4 + t / 8;
+ *   value codes at v_off      : byte c / 32 * 512 + c % 8 * 64 + t % 8 / 2 * 16 + c / 16 % 2 * 8 + t / 16 * 4 + t / 8 % 2 * 2 + c / 8 % 2 holds tokens
+ *                               t (even; low nibble) and t + 1;
+ *   value scales at v_off + 16 * head_dim: byte c / 32 * 64 + t % 8 / 2 * 16 + c / 16 % 2 * 8 + t / 16 * 4 + t % 2 * 2 + t / 8 % 2.
+ * klayout SA_KLAYOUT_BYTE, headroom_F 0, of the flags SA_FLAG_HADAMARD only.  Served by sa_append_kv, sa_fill_kv, sa_read_kv, sa_decode_attention (without
+ * dbg_scores: there are no integer scores), its _stages and _static forms, sa_decode_step and sa_decode_step_host. */
 /* How key codes are stored in a page.
  * SA_KLAYOUT_BYTE: one byte per element (any code).
  * SA_KLAYOUT_NIBBLE: SA_POT4 only, two 4-bit codes (sign, exponent) per byte.
@@ -107,7 +122,7 @@ typedef struct {
     int head_dim;    /* 64 or 128 */
     int n_q_heads;   /* multiple of n_kv_heads */
     int n_kv_heads;
-    int code;        /* SA_POT4 / SA_POTM1 / SA_POTM2 / SA_POTM4, SA_INT8 (comparison), or SA_KV_FP16 (FP16 baseline cache) */
+    int code;        /* SA_POT4 / SA_POTM1 / SA_POTM2 / SA_POTM4, SA_INT8 (comparison), SA_KV_FP16 (FP16 baseline cache) or SA_KV_FP4 */
     int klayout;     /* SA_KLAYOUT_BYTE, SA_KLAYOUT_NIBBLE (only with SA_POT4) or SA_KLAYOUT_PLANAR (SA_POTM1 / SA_POTM2) */
     int headroom_F;  /* fixed-point head-room F of eq. (3); 0 selects the default E + k = 6 + k.
                         Must satisfy F >= 6 + k (eq. (4): every shift is a left shift) and
@@ -185,6 +200,50 @@ sa_status sa_append_kv(const sa_config* cfg, const sa_cache* cache, const uint16
  * 0 .. T_b - 1 of every sequence; does not touch seq_lens. */
 sa_status sa_fill_kv(const sa_config* cfg, const sa_cache* cache, const uint16_t* K,
                      const uint16_t* V, const int64_t* cu_lens_host, sa_stream stream);
+
+/* Reads keys and values back out of a cache of any code, as binary16 (the paper has no counterpart; for programs that move a cached
+ * prefix on: into another code, another layout, the attention of a prompt's next chunk).  Sequence b's tokens starts_host[b] ..
+ * starts_host[b] + n_b - 1, n_b = cu_lens_host[b+1] - cu_lens_host[b], go to rows cu_lens_host[b] .. cu_lens_host[b+1] - 1 of K and V
+ * [sum_b n_b, n_kv_heads, head_dim]; either may be NULL, starts_host too (all 0).  HOST arrays of batch and batch + 1 entries.
+ * Written are the numbers that the codes stand for, rounded once to binary16 (FP32 arithmetic; exact for SA_KV_FP4 and
+ * SA_KV_FP16); keys that were rotated on their way in (SA_FLAG_HADAMARD) are rotated back.  The caller keeps the range within
+ * what has been written (seq_lens is not read): slots that never were hold anything.  Tokens whose page is not mapped come back as zeros; no other
+ * row of K or V is touched. */
+sa_status sa_read_kv(const sa_config* cfg, const sa_cache* cache, const int64_t* starts_host, const int64_t* cu_lens_host,
+                     uint16_t* K, uint16_t* V, sa_stream stream);
+
+/* Queries, keys and values of n tokens from a layer's projections (the paper starts behind this step): for every query and key
+ * head y = x / sqrt(mean(x^2) + eps) * w (norm = 1), then the rotation of the first rotary_dim channels by the token's
+ * position(s); values are converted.  FP32 arithmetic on inputs of any of three types, one rounding to binary16, in the contiguous
+ * rows that sa_decode_step, sa_append_kv and sa_fill_kv take.
+ *   pair j (of rotary_dim / 2) turns by the angle positions[axis][token] * inv_freq[j], axis = pair_axis[j]: (a, b) -> scale * (a cos - b sin, a sin + b cos).
+ * The angle's fraction of a turn is taken in 64 bits, so far positions lose nothing.  Several axes (time, height, width of
+ * images and video) are up to 4 rows of positions; pair_axis says which pair follows which, in sections, interleaved or otherwise
+ * (a number beyond n_axes - 1 counts as the last axis). */
+enum { SA_F16 = 0, SA_BF16 = 1, SA_F32 = 2 };
+enum { SA_PAIR_HALVES = 0,     /* channels j and j + rotary_dim / 2 */
+       SA_PAIR_NEIGHBOURS = 1  /* channels 2 j and 2 j + 1 */ };
+typedef struct {
+    int dtype;                /* of Q, K, V and the weights: SA_F16, SA_BF16 or SA_F32 */
+    int rotary_dim;           /* channels that are rotated, the first ones: a multiple of 8, 0 (none) to head_dim */
+    int pairs;                /* SA_PAIR_HALVES or SA_PAIR_NEIGHBOURS */
+    int n_axes;               /* 1 .. 4 positions per token */
+    int norm;                 /* 1: queries and keys are normed, 0: not */
+    float eps;                /* >= 0 */
+    float scale;              /* factor on the rotated channels (1: none) */
+    const void* q_weight;     /* [head_dim] of the inputs' type, 16-byte aligned, or NULL: ones (read with norm = 1 only) */
+    const void* k_weight;
+    const float* inv_freq;    /* [rotary_dim / 2] radians per position */
+    const uint8_t* pair_axis; /* [rotary_dim / 2], or NULL with one axis */
+} sa_rotary;
+/* Q, K, V: token i's heads, one after another, start q_stride (k_stride, v_stride) elements behind token i - 1's, so the three may
+ * lie side by side in one projection's output; addresses and strides are multiples of 16 bytes.  Any of the three may be NULL together with its output.
+ * positions: int32 [n_axes][n].  Q_out [n, n_q_heads, head_dim], K_out, V_out [n, n_kv_heads, head_dim] binary16; an output may be
+ * its own input where the two have the same layout (SA_F16, contiguous rows).  Of cfg only the head counts and head_dim matter.
+ * A result beyond 65504 becomes infinite; a head of zeros with eps = 0 becomes NaN. */
+sa_status sa_rotate_qkv(const sa_config* cfg, const sa_rotary* rot, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                        const void* V, int64_t v_stride, const int32_t* positions, int64_t n, uint16_t* Q_out, uint16_t* K_out,
+                        uint16_t* V_out, sa_stream stream);
 
 /* Decode attention over the quantised cache — the hot path (section II-B eq. (3), II-C eq. (4),
  * II-D eq. (5), II-E, II-F):
@@ -310,7 +369,7 @@ sa_status sa_decode_attention_fp16_stages(const sa_config* cfg, const sa_cache* 
  *     calls that overlap on the GPU (different streams, or graphs replayed concurrently) race on
  *     it and corrupt each other's output.  Serialise them, or give the overlapping ones their own
  *     workspace through sa_decode_attention.
- *   - cfg->code must be one of the quantised key codes (the power-of-two codes or SA_INT8), not SA_KV_FP16. */
+ *   - cfg->code must be one of the quantised key codes (the power-of-two codes or SA_INT8) or SA_KV_FP4, not SA_KV_FP16. */
 #define SA_STATIC_SCRATCH_BYTES (4u << 20)
 sa_status sa_decode_attention_static(const sa_config* cfg, const sa_cache* cache, const uint16_t* Q,
                                      float* O, int32_t* dbg_scores, sa_stream stream);

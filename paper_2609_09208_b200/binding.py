@@ -17,20 +17,22 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsa.so")
 NATIVE_PATH = os.path.join(_HERE, "_native.so")
 
-SA_POT4, SA_POTM1, SA_POTM2, SA_POTM4, SA_INT8, SA_KV_FP16 = 0, 1, 2, 4, 8, 16
+SA_POT4, SA_POTM1, SA_POTM2, SA_POTM4, SA_INT8, SA_KV_FP16, SA_KV_FP4 = 0, 1, 2, 4, 8, 16, 32
 SA_KLAYOUT_BYTE, SA_KLAYOUT_NIBBLE, SA_KLAYOUT_PLANAR = 0, 1, 2
 SA_FLAG_HADAMARD = 1
 SA_FLAG_SHIFT_BY_MULTIPLY = 2
 SA_FLAG_ADD_ON_ALU = 4
 SA_FLAG_SHIFT_ADD = 16
 PAGE_TOKENS = 64
+SA_F16, SA_BF16, SA_F32 = 0, 1, 2
+SA_PAIR_HALVES, SA_PAIR_NEIGHBOURS = 0, 1
 
 EXPORTS = [
     "sa_version", "sa_status_string", "sa_get_layout", "sa_workspace_bytes", "sa_encode_keys",
     "sa_quantise_query", "sa_quantise_values", "sa_append_kv", "sa_fill_kv", "sa_decode_attention",
     "sa_decode_attention_fp16", "sa_decode_attention_stages", "sa_decode_attention_fp16_stages", "sa_debug_unpack", "sa_staging_bytes", "sa_decode_step_host",
     "sa_decode_attention_static", "sa_pipe_microbench", "sa_shiftav_workspace_bytes", "sa_decode_attention_shiftav",
-    "sa_decode_step", "sa_debug_decode_lost_copy",
+    "sa_decode_step", "sa_debug_decode_lost_copy", "sa_read_kv", "sa_rotate_qkv",
 ]
 
 
@@ -48,6 +50,12 @@ class SaLayout(C.Structure):
 class SaCache(C.Structure):
     _fields_ = [("pages", C.c_void_p), ("page_table", C.c_void_p), ("seq_lens", C.c_void_p),
                 ("batch", C.c_int), ("max_pages_per_seq", C.c_int), ("n_pages", C.c_int)]
+
+
+class SaRotary(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("rotary_dim", C.c_int), ("pairs", C.c_int), ("n_axes", C.c_int), ("norm", C.c_int),
+                ("eps", C.c_float), ("scale", C.c_float), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p),
+                ("inv_freq", C.c_void_p), ("pair_axis", C.c_void_p)]
 
 
 class SaError(RuntimeError):
@@ -176,6 +184,60 @@ def fill_kv(cfg, cache: SaCache, K, V, cu_lens_host):
     st = (_nat or native()).fill_kv(cfg, cache, K, V, np.ascontiguousarray(cu_lens_host, dtype=np.int64))
     if st:
         raise SaError(st, "sa_fill_kv")
+
+
+def read_kv(cfg, cache: SaCache, starts, cu_lens_host, K=None, V=None):
+    """Tokens starts[b] .. of every sequence, cu_lens_host[b + 1] - cu_lens_host[b] of them, as binary16 rows of K and V
+    ([rows, n_kv_heads, head_dim], contiguous; either may be None).  starts (None: all 0), cu_lens_host: numpy int64 of batch and batch + 1
+    entries (host memory)."""
+    import numpy as np
+    starts = None if starts is None else np.ascontiguousarray(starts, dtype=np.int64)
+    st = (_nat or native()).read_kv(cfg, cache, starts, np.ascontiguousarray(cu_lens_host, dtype=np.int64), K, V)
+    if st:
+        raise SaError(st, "sa_read_kv")
+
+
+class Rotary:
+    """What rotate_qkv does with a layer's projections, made once: the tables stay with it (sa_rotary in the C header).
+
+    inv_freq: float32 CUDA tensor, radians per position of each pair of channels (None: no rotation).  pairs: "halves" (channels
+    j, j + rotary_dim / 2) or "neighbours" (2 j, 2 j + 1).  pair_axis: uint8, which of the n_axes rows of positions each pair follows.
+    norm: queries and keys are normed, with q_weight, k_weight ([head_dim], of `dtype`; None: ones).  scale: factor on rotated channels."""
+
+    def __init__(self, cfg: SaConfig, inv_freq=None, *, dtype, pairs: str = "halves", n_axes: int = 1, pair_axis=None, norm: bool = False,
+                 eps: float = 1e-6, scale: float = 1.0, q_weight=None, k_weight=None):
+        import torch
+        kinds = {torch.float16: SA_F16, torch.bfloat16: SA_BF16, torch.float32: SA_F32}
+        if dtype not in kinds:
+            raise ValueError("dtype is float16, bfloat16 or float32, not %s" % dtype)
+        if pairs not in ("halves", "neighbours"):
+            raise ValueError('pairs is "halves" or "neighbours", not %r' % (pairs,))
+        n = 0 if inv_freq is None else inv_freq.numel()
+        tables = [("inv_freq", inv_freq, torch.float32, n), ("pair_axis", pair_axis, torch.uint8, n),
+                  ("q_weight", q_weight, dtype, cfg.head_dim), ("k_weight", k_weight, dtype, cfg.head_dim)]
+        devices = set()
+        for name, t, kind, count in tables:
+            if t is None:
+                continue
+            if t.dtype != kind or t.numel() != count or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError("%s is a contiguous CUDA tensor of %d numbers of %s" % (name, count, kind))
+            devices.add(t.get_device())
+        if len(devices) > 1:
+            raise ValueError("the tables lie on different devices")
+        self.cfg, self.dtype, self.tables = cfg, dtype, [t for _, t, _, _ in tables]
+        self.device = devices.pop() if devices else -1                # -1: no table, any device
+        ptr = [0 if t is None else t.data_ptr() for t in self.tables]
+        self.handle = SaRotary(kinds[dtype], 2 * n, SA_PAIR_NEIGHBOURS if pairs == "neighbours" else SA_PAIR_HALVES, n_axes, 1 if norm else 0,
+                               eps, scale, ptr[2], ptr[3], ptr[0], ptr[1])
+
+
+def rotate_qkv(rot: Rotary, Q, K, V, positions, Q_out, K_out, V_out):
+    """Q [n, n_q_heads, head_dim], K, V [n, n_kv_heads, head_dim] of rot.dtype (a token's heads contiguous; views of one projection's
+    output will do) to contiguous binary16 outputs of the same shapes; any of the three may be None with its output.
+    positions: int32 [n_axes, n] (or [n]), None where nothing is rotated."""
+    st = (_nat or native()).rotate_qkv(rot.cfg, rot.handle, rot.dtype, rot.device, Q, K, V, positions, Q_out, K_out, V_out)
+    if st:
+        raise SaError(st, "sa_rotate_qkv")
 
 
 def decode_attention(cfg, cache: SaCache, Q, O, workspace, dbg_scores=None, stages: int = 3):

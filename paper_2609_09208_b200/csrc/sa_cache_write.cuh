@@ -2,6 +2,7 @@
 // append / fill kernels and by the decode kernel when it appends the step's new token itself.
 #pragma once
 #include "sa_common.cuh"
+#include "sa_fp4.cuh"
 #include "sa_quant.cuh"
 
 namespace sa {
@@ -99,6 +100,29 @@ SA_D void write_token_fp16(uint8_t* block, const CacheArgs& a, int t, int lane, 
     }
 }
 
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+inline sa_status check_cache(const Plan& p, const sa_cache* c, CacheArgs* a) {
+    if (!c || !c->pages || !c->page_table || !c->seq_lens) return SA_ERR_INVALID_ARG;
+    if (c->batch <= 0 || c->max_pages_per_seq <= 0 || c->n_pages <= 0) return SA_ERR_INVALID_ARG;
+    if (!aligned(c->pages, p.lay.align) || !aligned(c->page_table, 4) || !aligned(c->seq_lens, 4))
+        return SA_ERR_ALIGNMENT;
+    a->pages = static_cast<uint8_t*>(c->pages);
+    a->page_table = c->page_table;
+    a->seq_lens = c->seq_lens;
+    a->batch = c->batch;
+    a->max_pages = c->max_pages_per_seq;
+    a->n_pages = c->n_pages;
+    a->Hkv = p.Hkv;
+    a->page_bytes = p.lay.page_bytes;
+    a->kcode_off = p.lay.kcode_off;
+    a->meta_off = p.lay.meta_off;
+    a->v_off = p.lay.v_off;
+    a->plane_off = p.plane_off;
+    a->hadamard = p.hadamard ? 1 : 0;
+    return SA_OK;
+}
+
 // block pointer of logical page `lp` of sequence b, KV head h; nullptr if unmapped / out of range
 SA_D uint8_t* page_block(const CacheArgs& a, int b, int lp, int h) {
     if (lp < 0 || lp >= a.max_pages) return nullptr;
@@ -108,11 +132,12 @@ SA_D uint8_t* page_block(const CacheArgs& a, int b, int lp, int h) {
 }
 
 // MODE: 0..4 = power-of-two code with K mantissa bits (byte container), 7 = the same with a.k of them, 8 = PoT-4 nibble, 9 / 10 = PoT-M1 /
-// PoT-M2 in the dense planar container, 16 = FP16, 32 = uniform INT8 comparison code
+// PoT-M2 in the dense planar container, 16 = FP16, 32 = uniform INT8 comparison code, 33 = 4 bits for keys and values
 template <int D, int MODE>
 SA_D void write_token(uint8_t* block, const CacheArgs& a, int t, int lane, const uint16_t* krow,
                       const uint16_t* vrow) {
     if constexpr (MODE == 7) write_token_quant<D, -1, false>(block, a, t, lane, krow, vrow);
+    else if constexpr (MODE == 33) write_token_fp4<D>(block + (size_t)(t >> 5) * (a.page_bytes >> 1), a.v_off, a.hadamard != 0, t & 31, lane, krow, vrow);
     else if constexpr (MODE == 16) write_token_fp16<D>(block, a, t, lane, krow, vrow);
     else if constexpr (MODE == 8) write_token_quant<D, 0, true>(block, a, t, lane, krow, vrow);
     else if constexpr (MODE == 9) write_token_quant<D, 1, true>(block, a, t, lane, krow, vrow);

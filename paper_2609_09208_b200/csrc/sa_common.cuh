@@ -24,6 +24,7 @@ constexpr int half_block_bytes(int d, int kb, bool nib) {
     return kTileTokens * (nib ? d / 2 : d) + ((nib && kb > 0) ? kb * kTileTokens * (d / 8) : 0) + kTileTokens * 4 + kTileTokens * d;
 }
 constexpr int half_block_bytes_fp16(int d) { return 2 * kTileTokens * d * 2; }
+constexpr int half_block_bytes_fp4(int d) { return 2 * kTileTokens * (d / 2 + d / 16); }       // codes and scale bytes of keys and values
 constexpr int kNumSMsB200 = 148;          // the split plan's SM count where no device can be asked (see sm_count())
 constexpr int kEmax = 6;                  // largest exponent of the 3-bit field
 constexpr int kMNone = -(1 << 29);        // running-maximum value meaning "no key seen yet"
@@ -39,6 +40,8 @@ constexpr KernelShape mma_shape(int d, int kb) {
 }
 // ... over the binary16 cache (tiles of 8 and 16 KB).
 constexpr KernelShape fp16_shape(int d) { return d == 128 ? KernelShape{6, 2, 1} : KernelShape{5, 2, 2}; }
+// ... over the 4-bit cache.
+constexpr KernelShape fp4_shape(int d) { return d == 128 ? KernelShape{6, 2, 2} : KernelShape{8, 2, 2}; }
 // The kernel of one block per SM (sa_decode_stream.cuh).
 constexpr KernelShape stream_shape(int d, bool fp16) {
     return fp16 ? KernelShape{12, 1, d == 128 ? 1 : 2} : d == 128 ? KernelShape{12, 1, 2} : KernelShape{16, 1, 2};
@@ -73,6 +76,7 @@ struct Plan {
     bool mulshift;            // SA_FLAG_SHIFT_BY_MULTIPLY: the scores' shifts run on the integer multiplier
     bool addalu;              // SA_FLAG_ADD_ON_ALU: sign flips and adds as logic/add instructions, no multiply-add
     bool shiftadd;            // SA_FLAG_SHIFT_ADD: shifts, and sign flip and add as one multiply-add by +1 / -1
+    bool fp4;                 // SA_KV_FP4: keys and values in 4 bits with a scale for every 16 channels
     bool fp16, nibble, hadamard, int8;   // nibble: 4-bit sign/exponent codes (PoT-4 nibble container, or with k = 1, 2
                                          // the dense planar container); int8: the uniform INT8 comparison code
     int F;                    // head-room actually used

@@ -11,11 +11,13 @@ void launch_mma_lost_copy(const DecodeArgs& a, dim3 grid, cudaStream_t s);
 void launch_mma_dense(int d, int k, const DecodeArgs& a, dim3 grid, cudaStream_t s);
 void launch_mma_int8(int d, const DecodeArgs& a, dim3 grid, cudaStream_t s);
 void launch_mma_fp16(int d, const DecodeArgs& a, dim3 grid, cudaStream_t s);
+void launch_mma_fp4(int d, const DecodeArgs& a, dim3 grid, cudaStream_t s);
 void launch_stream_byte(int d, int k, const DecodeArgs& a, cudaStream_t s);                   // sa_decode_stream_*.cu
 void launch_stream_lost_copy(const DecodeArgs& a, cudaStream_t s);
 void launch_stream_dense(int d, int k, const DecodeArgs& a, cudaStream_t s);
 void launch_stream_int8(int d, const DecodeArgs& a, cudaStream_t s);
 void launch_stream_fp16(int d, const DecodeArgs& a, cudaStream_t s);
+void launch_stream_fp4(int d, const DecodeArgs& a, cudaStream_t s);
 void launch_shift_pot4(bool nib, int d, ShiftMode mode, const DecodeArgs& a, int GT, dim3 grid, cudaStream_t s);   // sa_decode_pot*.cu
 void launch_shift_potm1(bool nib, int d, ShiftMode mode, const DecodeArgs& a, int GT, dim3 grid, cudaStream_t s);
 void launch_shift_potm2(bool nib, int d, ShiftMode mode, const DecodeArgs& a, int GT, dim3 grid, cudaStream_t s);
@@ -27,11 +29,13 @@ void launch_decode_main(const Plan& p, const DecodeArgs& a, int GT, cudaStream_t
     const ShiftMode mode = a.zr ? SHIFT_SCORE_PASS : p.mulshift ? SHIFT_MUL : p.addalu ? SHIFT_ALU : SHIFT_FMA;
     if (a.stream) {
         if (p.fp16) launch_stream_fp16(p.d, a, s);
+        else if (p.fp4) launch_stream_fp4(p.d, a, s);
         else if (p.int8) launch_stream_int8(p.d, a, s);
         else if (p.nibble) launch_stream_dense(p.d, p.k, a, s);
         else launch_stream_byte(p.d, p.k, a, s);
     } else if (p.matrix) {
         if (p.fp16) launch_mma_fp16(p.d, a, grid, s);
+        else if (p.fp4) launch_mma_fp4(p.d, a, grid, s);
         else if (p.int8) launch_mma_int8(p.d, a, grid, s);
         else if (p.nibble) launch_mma_dense(p.d, p.k, a, grid, s);
         else launch_mma_byte(p.d, p.k, a, grid, s);
@@ -46,6 +50,7 @@ void launch_decode_main(const Plan& p, const DecodeArgs& a, int GT, cudaStream_t
 static sa_status decode_stages(const Plan& p, const sa_cache* cache, const uint16_t* Q, float* O, void* workspace,
                                size_t workspace_bytes, int32_t* dbg_scores, int stages, sa_stream stream) {
     if ((stages & ~3) || stages == 0) return SA_ERR_INVALID_ARG;
+    if (dbg_scores && p.fp4) return SA_ERR_UNSUPPORTED;          // its scores are no integers
     DecodeArgs a;
     int GT;
     const sa_status st = make_decode_args(p, cache, Q, O, workspace, workspace_bytes, &a, &GT);
@@ -96,7 +101,7 @@ extern "C" sa_status sa_debug_decode_lost_copy(const sa_config* cfg, const sa_ca
     Plan p;
     sa_status st = make_plan(cfg, &p);
     if (st != SA_OK) return st;
-    if (p.fp16 || p.int8 || p.nibble || p.d != 64 || p.k != 4 || p.G != 8 || !p.matrix) return SA_ERR_UNSUPPORTED;
+    if (p.fp16 || p.fp4 || p.int8 || p.nibble || p.d != 64 || p.k != 4 || p.G != 8 || !p.matrix) return SA_ERR_UNSUPPORTED;
     DecodeArgs a;
     int GT;
     st = make_decode_args(p, cache, Q, O, workspace, workspace_bytes, &a, &GT);

@@ -626,7 +626,7 @@ inline sa_status make_decode_args(const Plan& p, const sa_cache* c, const uint16
 // The sums of sa_score_mma.cuh come in units of 2^-(6 + k) (PoT-M4: 2^-18; INT8, nibbles: 1) whatever F is.
 inline void set_scales(const Plan& p, DecodeArgs* a) {
     const double base = 1.4426950408889634 / sqrt((double)p.d);
-    if (p.fp16) a->zscale = (float)base;
+    if (p.fp16 || p.fp4) a->zscale = (float)base;
     else if (p.int8) a->zscale = (float)(base / 127.0);                       // key unit = scale / 127
     else if (!p.matrix) a->zscale = (float)(base / (double)(1LL << p.F));
     else if (p.nibble && p.k == 0) a->zscale = (float)(base / 64.0);

@@ -32,7 +32,7 @@ struct MmaSmem {
     static_assert(kSumOff + 8 * D * 4 <= NW * NS * Stage::kBytes, "merge rows and sums must fit in the stage buffers");
     static_assert(kHeadOff >= NW * NS * Stage::kBytes, "no copy may land on the marks");
     static_assert(NW * NS * Stage::kBytes >= kPlanScratchInts * 4, "the block plan's scratch must fit in the stage buffers");
-    static_assert(Stage::kBytes == (FMT == FMT_FP16 ? half_block_bytes_fp16(D) : half_block_bytes(D, format_kb<FMT>(), ScoreMma<D, FMT>::kDense)), "a stage buffer is a verbatim copy of half a page block");
+    static_assert(Stage::kBytes == format_half_bytes<D, FMT>(), "a stage buffer is a verbatim copy of half a page block");
 };
 
 // This block's share of the outputs of a cluster (a.cluster blocks, each with the O[D] of its query heads at shared address

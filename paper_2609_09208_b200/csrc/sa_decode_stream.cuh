@@ -143,7 +143,7 @@ struct FinishArgs {
 template <int D, int FMT, int NW>
 SA_D void finish_units(const FinishArgs& a, const UnitSums& j0, const float* rows0, const UnitSums& j1, const float* rows1) {
     constexpr int NT = 32 * NW, kStep = TileMma<D, FMT, true, false>::kRowStep;
-    constexpr float kValueScale = 1.0f / (1 << kWeightShift), kSumScale = FMT == FMT_FP16 ? kValueScale : 1.0f;
+    constexpr float kValueScale = 1.0f / (1 << kWeightShift), kSumScale = TileMma<D, FMT, true, false>::kPlain ? kValueScale : 1.0f;
     const int GT = a.GT;
     if (threadIdx.x < 2 * NW * 8) {                           // every warp's 2^(R - R of the block's largest), and l times that
         float2* h = a.heads + threadIdx.x / (NW * 8) * (NW * 8);

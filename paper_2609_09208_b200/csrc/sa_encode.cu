@@ -269,6 +269,65 @@ SA_D void fill_values(uint8_t* half, const CacheArgs& a, int t, const uint4* src
     *reinterpret_cast<uint16_t*>(half + a.meta_off + (size_t)t * 4 + 2) = (uint16_t)(g & 0xff);
 }
 
+// 4-bit cache.  Keys: lane = token, as above.  Values: the lane's codes of 32 channels, 8 to a word, change places with those of the
+// seven tokens with which it shares bytes and words (fp4_transpose), and the warp's 16-byte stores are 512 contiguous bytes.
+// n: tokens of the tile that are written; the nibbles and scales of the others stay.
+template <int D, bool HAD>
+SA_D void fill_keys_fp4(uint8_t* half, int t, const uint4* src) {
+    VecRow<D, HAD> row(src, t);
+#pragma unroll(HAD ? D / 64 : 1)
+    for (int h = 0; h < D / 64; ++h) {
+        uint32_t w[2][4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            uint32_t x[8];
+            row.get(8 * h + 2 * b, x);
+            row.get(8 * h + 2 * b + 1, x + 4);
+            w[0][b] = fp4_block(x, &w[1][b], half + fp4_key_scale(D, t, 64 * h + 16 * b));
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            *reinterpret_cast<uint4*>(half + ((2 * h + k) * kTileTokens + t) * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+    }
+}
+template <int D>
+SA_D void fill_values_fp4(uint8_t* v, int t, int n, const uint4* src) {
+    VecRow<D, false> row(src, t);
+    const int piece = fp4_piece_of(t), pair = (t & 7) >> 1;
+    // of the bytes [t / 16][t / 8 % 2], two nibbles each, that this pair of tokens has in a word: those of written tokens
+    uint32_t written = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) written |= (16 * (i >> 2) + 8 * (i >> 1 & 1) + 2 * pair + (i & 1) < n ? 0xfu : 0u) << (4 * i);
+#pragma unroll 1
+    for (int p = 0; p < D / 32; ++p) {
+        uint32_t w[2][2];                                      // [channel / 16 % 2][channel / 8 % 2]
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            uint32_t x[8];
+            row.get(4 * p + 2 * m, x);
+            row.get(4 * p + 2 * m + 1, x + 4);
+            w[m][0] = fp4_block(x, &w[m][1], t < n ? v + fp4_value_scale(D, t, 32 * p + 16 * m) : nullptr);
+        }
+        uint32_t out[4], mask[4];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const uint32_t a = fp4_transpose(w[m][0], t), b = fp4_transpose(w[m][1], t);
+            out[2 * m] = __byte_perm(a, b, 0x5140);
+            out[2 * m + 1] = __byte_perm(a, b, 0x7362);
+            mask[2 * m] = __byte_perm(written, 0u, 0x1100);
+            mask[2 * m + 1] = __byte_perm(written, 0u, 0x3322);
+        }
+        uint4* at = reinterpret_cast<uint4*>(v + p * 512 + piece * 64 + pair * 16);
+        if (n < kTileTokens) {
+            const uint4 old = *at;
+            const uint32_t o[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[i] = (out[i] & mask[i]) | (o[i] & ~mask[i]);
+        }
+        *at = make_uint4(out[0], out[1], out[2], out[3]);
+    }
+}
+
 template <int D, int MODE, bool HAD>                          // HAD on its own: the rotation needs twice the registers
 __global__ void __launch_bounds__(128) fill_kernel(CacheArgs a, const uint16_t* __restrict__ Kin, const uint16_t* __restrict__ Vin,
                                                    const __grid_constant__ FillSeqs seqs) {
@@ -305,8 +364,15 @@ __global__ void __launch_bounds__(128) fill_kernel(CacheArgs a, const uint16_t* 
         if (row < n) src[row * C + (ch ^ (row & 7))] = v[k];
     }
     __syncwarp();
+    if constexpr (MODE == 33)
+        if (rest & 1) {                                                       // (all lanes: they exchange codes)
+            fill_values_fp4<D>(half + a.v_off, lane, n, src);
+            return;
+        }
     if (lane >= n) return;
-    if constexpr (MODE == 16) {                                               // unquantised: 16-byte chunks of 8 elements
+    if constexpr (MODE == 33) {
+        fill_keys_fp4<D, HAD>(half, lane, src);
+    } else if constexpr (MODE == 16) {                                               // unquantised: 16-byte chunks of 8 elements
         uint8_t* dst = half + ((rest & 1) ? a.v_off : a.kcode_off);
 #pragma unroll
         for (int k = 0; k < D / 8; ++k) *reinterpret_cast<uint4*>(dst + (size_t)(k * kTileTokens + lane) * 16) = src[lane * C + (k ^ (lane & 7))];
@@ -367,30 +433,7 @@ __global__ void __launch_bounds__(128) unpack_kernel(CacheArgs a, int b, int T, 
     }
 }
 
-static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-static sa_status check_cache(const Plan& p, const sa_cache* c, CacheArgs* a) {
-    if (!c || !c->pages || !c->page_table || !c->seq_lens) return SA_ERR_INVALID_ARG;
-    if (c->batch <= 0 || c->max_pages_per_seq <= 0 || c->n_pages <= 0) return SA_ERR_INVALID_ARG;
-    if (!aligned(c->pages, p.lay.align) || !aligned(c->page_table, 4) || !aligned(c->seq_lens, 4))
-        return SA_ERR_ALIGNMENT;
-    a->pages = static_cast<uint8_t*>(c->pages);
-    a->page_table = c->page_table;
-    a->seq_lens = c->seq_lens;
-    a->batch = c->batch;
-    a->max_pages = c->max_pages_per_seq;
-    a->n_pages = c->n_pages;
-    a->Hkv = p.Hkv;
-    a->page_bytes = p.lay.page_bytes;
-    a->kcode_off = p.lay.kcode_off;
-    a->meta_off = p.lay.meta_off;
-    a->v_off = p.lay.v_off;
-    a->plane_off = p.plane_off;
-    a->hadamard = p.hadamard ? 1 : 0;
-    return SA_OK;
-}
-
-static int mode_of(const Plan& p) { return p.fp16 ? 16 : (p.int8 ? 32 : (p.nibble ? 8 + p.k : p.k)); }
+static int mode_of(const Plan& p) { return p.fp16 ? 16 : p.fp4 ? 33 : (p.int8 ? 32 : (p.nibble ? 8 + p.k : p.k)); }
 
 #define SA_LAUNCH_CHECK() (cudaGetLastError() == cudaSuccess ? SA_OK : SA_ERR_CUDA)
 
@@ -408,6 +451,7 @@ static int mode_of(const Plan& p) { return p.fp16 ? 16 : (p.int8 ? 32 : (p.nibbl
                 case 9: CALL(64, 9); break;                                             \
                 case 10: CALL(64, 10); break;                                           \
                 case 32: CALL(64, 32); break;                                           \
+                case 33: CALL(64, 33); break;                                           \
                 default: CALL(64, 16); break;                                           \
             }                                                                           \
         } else {                                                                        \
@@ -420,6 +464,7 @@ static int mode_of(const Plan& p) { return p.fp16 ? 16 : (p.int8 ? 32 : (p.nibbl
                 case 9: CALL(128, 9); break;                                            \
                 case 10: CALL(128, 10); break;                                          \
                 case 32: CALL(128, 32); break;                                          \
+                case 33: CALL(128, 33); break;                                          \
                 default: CALL(128, 16); break;                                          \
             }                                                                           \
         }                                                                               \
@@ -436,7 +481,7 @@ sa_status sa_encode_keys(const sa_config* cfg, const uint16_t* K, int64_t n, uin
     Plan p;
     sa_status st = make_plan(cfg, &p);
     if (st != SA_OK) return st;
-    if (p.fp16) return SA_ERR_UNSUPPORTED;
+    if (p.fp16 || p.fp4) return SA_ERR_UNSUPPORTED;           // (no canonical code bytes)
     if (!K || !codes || !scales || n < 0) return SA_ERR_INVALID_ARG;
     if (!aligned(K, 16) || !aligned(codes, 16) || !aligned(scales, 2)) return SA_ERR_ALIGNMENT;
     const int64_t n_vec = n * p.Hkv;
@@ -555,7 +600,7 @@ sa_status sa_debug_unpack(const sa_config* cfg, const sa_cache* cache, int b, in
     Plan p;
     sa_status st = make_plan(cfg, &p);
     if (st != SA_OK) return st;
-    if (p.fp16) return SA_ERR_UNSUPPORTED;
+    if (p.fp16 || p.fp4) return SA_ERR_UNSUPPORTED;
     CacheArgs a;
     st = check_cache(p, cache, &a);
     if (st != SA_OK) return st;

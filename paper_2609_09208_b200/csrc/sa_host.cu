@@ -44,6 +44,23 @@ sa_status make_plan(const sa_config* cfg, Plan* out) {
         *out = p;
         return SA_OK;
     }
+    if (cfg->code == SA_KV_FP4) {
+        if (cfg->klayout != SA_KLAYOUT_BYTE || cfg->headroom_F != 0 || p.mulshift || p.addalu || p.shiftadd) return SA_ERR_UNSUPPORTED;
+        p.fp4 = true;
+        p.matrix = true;
+        p.shape = fp4_shape(p.d);
+        p.k = 0;
+        p.F = 0;
+        p.f_extra = 0;
+        p.lay.kcode_off = 0;
+        p.lay.meta_off = (size_t)kTileTokens * p.d / 2;         // the keys' scale bytes
+        p.lay.v_off = p.lay.meta_off + (size_t)kTileTokens * p.d / 16;
+        p.lay.page_bytes = 4 * p.lay.v_off;
+        if (p.lay.page_bytes != 2 * (size_t)half_block_bytes_fp4(p.d)) return SA_ERR_UNSUPPORTED;
+        p.lay.align = 256;
+        *out = p;
+        return SA_OK;
+    }
     if (cfg->code == SA_INT8) {
         if (cfg->klayout != SA_KLAYOUT_BYTE || cfg->headroom_F != 0) return SA_ERR_UNSUPPORTED;
         p.int8 = true;

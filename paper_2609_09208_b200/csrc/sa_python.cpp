@@ -11,7 +11,7 @@
 
 namespace {
 
-PyObject *g_data_ptr, *g_nbytes, *g_get_device, *g_get_stream;
+PyObject *g_data_ptr, *g_nbytes, *g_get_device, *g_get_stream, *g_shape, *g_stride, *g_dtype, *g_itemsize, *g_device_of;
 
 struct Args {
     PyObject* const* v;
@@ -68,6 +68,37 @@ struct Args {
         *bytes = (size_t)number_of(PyObject_GetAttr(o, g_nbytes));
         return bad ? nullptr : reinterpret_cast<void*>(number_of(PyObject_CallMethodNoArgs(o, g_data_ptr)));
     }
+    bool fail(const char* what) {
+        if (!bad) PyErr_SetString(PyExc_ValueError, what);
+        bad = true;
+        return false;
+    }
+    // Shape and strides (elements) of a tensor of n dimensions, its bytes an element and its device; dtype (unless null): its type.
+    bool describe(PyObject* o, int n, long long* shape, long long* stride, PyObject* dtype, long long* itemsize, long long* device, const char* what) {
+        if (bad) return false;
+        PyObject* sh = PyObject_GetAttr(o, g_shape);
+        PyObject* st = sh ? PyObject_CallMethodNoArgs(o, g_stride) : nullptr;
+        bool ok = st && PyTuple_Check(sh) && PyTuple_Check(st) && PyTuple_GET_SIZE(sh) == n && PyTuple_GET_SIZE(st) == n;
+        for (int i = 0; ok && i < n; ++i) {
+            shape[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(sh, i));
+            stride[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(st, i));
+        }
+        Py_XDECREF(sh);
+        Py_XDECREF(st);
+        PyObject* t = ok ? PyObject_GetAttr(o, g_dtype) : nullptr;
+        ok = t && (!dtype || t == dtype);
+        if (ok) *itemsize = (long long)number_of(PyObject_GetAttr(t, g_itemsize));
+        Py_XDECREF(t);
+        if (ok) {
+            PyObject* d = PyObject_CallMethodNoArgs(o, g_device_of);
+            *device = d ? PyLong_AsLongLong(d) : -1;                  // (-1: not on a CUDA device)
+            Py_XDECREF(d);
+        }
+        if (PyErr_Occurred()) bad = true;
+        return !bad && (ok || fail(what));
+    }
+    // The current device, which tensors and streams of a call belong to.
+    long long current_device() { return bad ? -1 : (long long)number_of(PyObject_CallNoArgs(g_get_device)); }
     int integer() {
         PyObject* o = bad ? nullptr : next();
         const long x = o ? PyLong_AsLong(o) : -1;
@@ -199,7 +230,104 @@ PyObject* fill_kv(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
+// A host array of at least `n` 64-bit integers; None (where it may be): null.
+struct HostArray {
+    Py_buffer b{};
+    bool held = false;
+    const int64_t* p = nullptr;
+    HostArray(Args& a, Py_ssize_t n, bool may_be_none, const char* what) {
+        PyObject* o = a.bad ? nullptr : a.next();
+        if (a.bad || (may_be_none && o == Py_None)) return;
+        if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) {
+            a.bad = true;
+            return;
+        }
+        held = true;
+        if (b.len / (Py_ssize_t)sizeof(int64_t) < n) a.fail(what);
+        else p = static_cast<const int64_t*>(b.buf);
+    }
+    ~HostArray() {
+        if (held) PyBuffer_Release(&b);
+    }
+};
+
+// (cfg, cache, starts, cu_lens, K, V)
+PyObject* read_kv(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a{v, n};
+    const sa_config* cfg = a.structure<sa_config>();
+    const sa_cache* cache = a.structure<sa_cache>();
+    const Py_ssize_t batch = a.bad || cache->batch < 0 ? 0 : cache->batch;
+    HostArray starts(a, batch, true, "starts holds fewer than batch numbers of 8 bytes");
+    HostArray cu(a, batch + 1, false, "cu_lens holds fewer than batch + 1 numbers of 8 bytes");
+    const long long dev = a.current_device();
+    uint16_t* out[2] = {nullptr, nullptr};
+    for (int i = 0; i < 2 && !a.bad; ++i) {
+        PyObject* o = a.next();
+        if (a.bad || o == Py_None) continue;
+        long long shape[3], stride[3], size = 0, device = -1;
+        const long long H = cfg->n_kv_heads, d = cfg->head_dim;
+        if (!a.describe(o, 3, shape, stride, nullptr, &size, &device, "K and V are tensors [rows, n_kv_heads, head_dim]")) break;
+        if (size != 2 || shape[1] != H || shape[2] != d || (shape[0] > 1 && stride[0] != H * d) || (H > 1 && stride[1] != d) || stride[2] != 1 || shape[0] < cu.p[batch])
+            a.fail("K and V are contiguous [rows, n_kv_heads, head_dim] of 2-byte numbers with a row for every token");
+        else if (device != dev) a.fail("K and V lie on the current CUDA device");
+        else out[i] = reinterpret_cast<uint16_t*>(a.number_of(PyObject_CallMethodNoArgs(o, g_data_ptr)));
+    }
+    const sa_stream s = a.stream();
+    SA_RETURN(sa_read_kv(cfg, cache, starts.p, cu.p, out[0], out[1], s));
+}
+
+// (cfg, rotary, dtype, device of the tables, Q, K, V, positions, Q_out, K_out, V_out)
+PyObject* rotate_qkv(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+    Args a{v, n_args};
+    const sa_config* cfg = a.structure<sa_config>();
+    const sa_rotary* rot = a.structure<sa_rotary>();
+    PyObject* dtype = a.bad ? nullptr : a.next();
+    const long long tables = a.integer(), dev = a.current_device();
+    if (!a.bad && tables >= 0 && tables != dev) a.fail("the tables lie on another device than the current one");
+    const void* in[3] = {};
+    uint16_t* out[3] = {};
+    long long stride[3] = {}, n = -1, shape[3], st[3], size = 0, device = -1;
+    const char* rows = "Q, K and V are [n, heads, head_dim] of the rotary's dtype on the current CUDA device, a token's heads one after another, n the same for all";
+    for (int i = 0; i < 3 && !a.bad; ++i) {
+        PyObject* o = a.next();
+        if (a.bad || o == Py_None || !a.describe(o, 3, shape, st, dtype, &size, &device, rows)) continue;
+        const long long H = i == 0 ? cfg->n_q_heads : cfg->n_kv_heads, d = cfg->head_dim;
+        if (device != dev || shape[1] != H || shape[2] != d || (H > 1 && st[1] != d) || st[2] != 1 || (n >= 0 && shape[0] != n)) a.fail(rows);
+        n = shape[0];
+        stride[i] = n > 1 ? st[0] : H * d;
+        in[i] = reinterpret_cast<const void*>(a.bad ? 0 : a.number_of(PyObject_CallMethodNoArgs(o, g_data_ptr)));
+    }
+    const int32_t* positions = nullptr;
+    PyObject* pos = a.bad ? nullptr : a.next();
+    if (!a.bad && pos != Py_None) {
+        PyObject* sh = PyObject_GetAttr(pos, g_shape);
+        const int dims = sh && PyTuple_Check(sh) ? (int)PyTuple_GET_SIZE(sh) : 0;
+        Py_XDECREF(sh);
+        const char* what = "positions are contiguous 4-byte integers [n_axes, n] on the current CUDA device";
+        if (dims != 1 && dims != 2) a.fail(what);
+        else if (a.describe(pos, dims, shape, st, nullptr, &size, &device, what)) {
+            const long long axes = dims == 2 ? shape[0] : 1, len = shape[dims - 1];
+            if (size != 4 || device != dev || axes != rot->n_axes || (n >= 0 && len != n) || (len > 1 && st[dims - 1] != 1) || (axes > 1 && len > 0 && st[0] != len)) a.fail(what);
+            positions = reinterpret_cast<const int32_t*>(a.bad ? 0 : a.number_of(PyObject_CallMethodNoArgs(pos, g_data_ptr)));
+        }
+    }
+    for (int i = 0; i < 3 && !a.bad; ++i) {
+        PyObject* o = a.next();
+        const char* what = "the outputs are contiguous [n, heads, head_dim] of 2-byte numbers on the current CUDA device, one for each of Q, K and V that is given";
+        if (a.bad || o == Py_None || !a.describe(o, 3, shape, st, nullptr, &size, &device, what)) continue;
+        const long long H = i == 0 ? cfg->n_q_heads : cfg->n_kv_heads, d = cfg->head_dim;
+        if (size != 2 || device != dev || shape[0] != n || shape[1] != H || shape[2] != d || (n > 1 && st[0] != H * d) || (H > 1 && st[1] != d) || st[2] != 1) a.fail(what);
+        out[i] = reinterpret_cast<uint16_t*>(a.bad ? 0 : a.number_of(PyObject_CallMethodNoArgs(o, g_data_ptr)));
+    }
+    // (a tensor without elements has no address, which would read as one that is not there)
+    if (!a.bad && n == 0) return PyLong_FromLong(SA_OK);
+    const sa_stream s = a.stream();
+    SA_RETURN(sa_rotate_qkv(cfg, rot, in[0], stride[0], in[1], stride[1], in[2], stride[2], positions, n < 0 ? 0 : n, out[0], out[1], out[2], s));
+}
+
 PyMethodDef kMethods[] = {
+    {"read_kv", (PyCFunction)(void (*)(void))read_kv, METH_FASTCALL, nullptr},
+    {"rotate_qkv", (PyCFunction)(void (*)(void))rotate_qkv, METH_FASTCALL, nullptr},
     {"fill_kv", (PyCFunction)(void (*)(void))fill_kv, METH_FASTCALL, nullptr},
     {"decode_attention", (PyCFunction)(void (*)(void))decode_attention, METH_FASTCALL, nullptr},
     {"decode_attention_fp16", (PyCFunction)(void (*)(void))decode_attention_fp16, METH_FASTCALL, nullptr},
@@ -220,6 +348,11 @@ PyMODINIT_FUNC PyInit__native(void) {
     Py_DECREF(c);
     g_data_ptr = PyUnicode_InternFromString("data_ptr");
     g_nbytes = PyUnicode_InternFromString("nbytes");
-    if (!g_get_device || !g_get_stream || !g_data_ptr || !g_nbytes) return nullptr;
+    g_shape = PyUnicode_InternFromString("shape");
+    g_stride = PyUnicode_InternFromString("stride");
+    g_dtype = PyUnicode_InternFromString("dtype");
+    g_itemsize = PyUnicode_InternFromString("itemsize");
+    g_device_of = PyUnicode_InternFromString("get_device");
+    if (!g_get_device || !g_get_stream || !g_data_ptr || !g_nbytes || !g_shape || !g_stride || !g_dtype || !g_itemsize || !g_device_of) return nullptr;
     return PyModule_Create(&kModule);
 }

@@ -16,6 +16,8 @@
 //                             others into 0; a second lookup with the signs flipped is multiplied by -q.  INT32 sums.
 //   INT8 keys                 as stored.  INT32 sums.
 //   binary16 keys             as stored, with the binary16 query; the sums are rounded like any FP32 sum.
+//   4-bit keys                code times scale, exact in binary16 (one conversion and one packed product for two codes), with the
+//                             binary16 query.
 // So the INT32 scores are those of the shift-and-add datapath (sa_datapath.cuh) bit for bit.  The decode is what a tile
 // costs most: 7 instructions for four codes by way of FP8, 8 for PoT-M4 (11 as binary16).  The pipe of logic, shifts and
 // permutes, which issues every other clock, is the fullest, the pipe of multiply-adds has room (62 and 20 % in a call of 32 x 32 768
@@ -32,13 +34,14 @@
 
 #include "sa_common.cuh"
 #include "sa_datapath.cuh"
+#include "sa_fp4.cuh"
 #include "sa_mma.cuh"
 #include "sa_quant.cuh"
 
 namespace sa {
 
 // FMT_FP16: the unquantised cache; FMT_BYTE3: the byte container of the codes with at most three mantissa bits (all but PoT-M4)
-enum ScoreFormat { FMT_BYTE = 0, FMT_NIBBLE = 1, FMT_PLANAR1 = 2, FMT_PLANAR2 = 3, FMT_INT8 = 4, FMT_BYTE3 = 5, FMT_FP16 = 6 };
+enum ScoreFormat { FMT_BYTE = 0, FMT_NIBBLE = 1, FMT_PLANAR1 = 2, FMT_PLANAR2 = 3, FMT_INT8 = 4, FMT_BYTE3 = 5, FMT_FP16 = 6, FMT_FP4 = 7 };
 
 // Codes I, I + 1 of a word of the byte container (sign << 7 | mantissa << 3 | g) as a pair of bfloat16 values.  With the byte in
 // both halves of its value, the mantissa field and the sign are where bfloat16 has them; g moves to bits 9..7.
@@ -86,8 +89,9 @@ template <int D, int FMT>
 struct ScoreMma {
     static constexpr bool kInt = (FMT == FMT_NIBBLE || FMT == FMT_INT8);
     static constexpr bool kDense = (FMT == FMT_NIBBLE || FMT == FMT_PLANAR1 || FMT == FMT_PLANAR2);
-    static constexpr int E = FMT == FMT_FP16 ? 2 : kDense ? 8 : 4;
-    static constexpr int CH = D / (4 * E);                        // code chunks
+    static constexpr int E = FMT == FMT_FP4 ? 16 : FMT == FMT_FP16 ? 2 : kDense ? 8 : 4;
+    static constexpr int QCH = D / (4 * E);                       // chunks of the query
+    static constexpr int CH = FMT == FMT_FP4 ? D / 32 : QCH;      // code chunks
     static constexpr int NACC = (FMT == FMT_BYTE && D == 128) ? 2 : 1;
     static constexpr int NB = kInt ? D / 16 : D / 8;              // registers of B fragments
     uint32_t q[NB];
@@ -102,14 +106,40 @@ struct ScoreMma {
 #pragma unroll
             for (int k = 0; k < CH; ++k) q[k] = row ? *reinterpret_cast<const uint32_t*>(row + k * 8 + c * 2) : 0u;
             return 1.0f;
+        } else if constexpr (FMT == FMT_FP4) {                    // nothing to quantise; a lane has 16 channels of every 64
+            if (hadamard) {
+                float x[QCH][E];
+#pragma unroll
+                for (int k = 0; k < QCH; ++k)
+#pragma unroll
+                    for (int i = 0; i < E; i += 2) {
+                        const uint32_t w = row ? *reinterpret_cast<const uint32_t*>(row + k * 64 + c * 16 + i) : 0u;
+                        x[k][i] = half_bits_to_float(w & 0xffffu);
+                        x[k][i + 1] = half_bits_to_float(w >> 16);
+                    }
+                rotate(x, c);
+#pragma unroll
+                for (int i = 0; i < NB; ++i) {
+                    const __half2 h = __floats2half2_rn(x[i / 8][2 * (i % 8)], x[i / 8][2 * (i % 8) + 1]);      // exact: rotate rounds
+                    q[i] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < NB; i += 4) {
+                    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                    if (row) w = *reinterpret_cast<const uint4*>(row + i / 8 * 64 + c * 16 + i % 8 * 2);
+                    q[i] = w.x, q[i + 1] = w.y, q[i + 2] = w.z, q[i + 3] = w.w;
+                }
+            }
+            return 1.0f;
         } else {
             return quantise(row, c, hadamard);
         }
     }
     SA_D float quantise(const uint16_t* row, int c, bool hadamard) {
-        float x[CH][E];
+        float x[QCH][E];
 #pragma unroll
-        for (int k = 0; k < CH; ++k)
+        for (int k = 0; k < QCH; ++k)
 #pragma unroll
             for (int i = 0; i < E; i += 4) {
                 uint2 w = make_uint2(0u, 0u);
@@ -122,15 +152,15 @@ struct ScoreMma {
         if (hadamard) rotate(x, c);
         float amax = 0.0f;
 #pragma unroll
-        for (int k = 0; k < CH; ++k)
+        for (int k = 0; k < QCH; ++k)
 #pragma unroll
             for (int i = 0; i < E; ++i) amax = fmaxf(amax, fabsf(x[k][i]));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
         const float inv = amax == 0.0f ? 0.0f : __fdiv_rn(127.0f, amax);
-        int v[CH][E];
+        int v[QCH][E];
 #pragma unroll
-        for (int k = 0; k < CH; ++k)
+        for (int k = 0; k < QCH; ++k)
 #pragma unroll
             for (int i = 0; i < E; ++i) v[k][i] = max(-127, min(127, __float2int_rn(__fmul_rn(x[k][i], inv))));
         pack(v);
@@ -138,11 +168,11 @@ struct ScoreMma {
     }
 
     // D-element Walsh-Hadamard transform of the quad's four lanes (element k * 4E + c * E + i), rounded to binary16.
-    SA_D static void rotate(float (&x)[CH][E], int c) {
+    SA_D static void rotate(float (&x)[QCH][E], int c) {
 #pragma unroll
         for (int h = 1; h < E; h <<= 1)
 #pragma unroll
-            for (int k = 0; k < CH; ++k)
+            for (int k = 0; k < QCH; ++k)
 #pragma unroll
                 for (int i = 0; i < E; ++i)
                     if ((i & h) == 0) {
@@ -153,16 +183,16 @@ struct ScoreMma {
 #pragma unroll
         for (int h = 1; h < 4; h <<= 1)
 #pragma unroll
-            for (int k = 0; k < CH; ++k)
+            for (int k = 0; k < QCH; ++k)
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
                     const float o = __shfl_xor_sync(0xffffffffu, x[k][i], h);
                     x[k][i] = (c & h) ? __fsub_rn(o, x[k][i]) : __fadd_rn(x[k][i], o);
                 }
 #pragma unroll
-        for (int h = 1; h < CH; h <<= 1)
+        for (int h = 1; h < QCH; h <<= 1)
 #pragma unroll
-            for (int k = 0; k < CH; ++k)
+            for (int k = 0; k < QCH; ++k)
                 if ((k & h) == 0)
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
@@ -172,7 +202,7 @@ struct ScoreMma {
                     }
         const float scale = (D == 64) ? 0.125f : 0.088388346f;    // 1/sqrt(64), 1/sqrt(128)
 #pragma unroll
-        for (int k = 0; k < CH; ++k)
+        for (int k = 0; k < QCH; ++k)
 #pragma unroll
             for (int i = 0; i < E; ++i) x[k][i] = __half2float(__float2half_rn(__fmul_rn(x[k][i], scale)));
     }
@@ -190,9 +220,9 @@ struct ScoreMma {
         return *reinterpret_cast<const uint32_t*>(&h);
     }
     // The order of the elements along the contraction: that of tile() below.
-    SA_D void pack(const int (&v)[CH][E]) {
+    SA_D void pack(const int (&v)[QCH][E]) {
 #pragma unroll
-        for (int k = 0; k < CH; ++k) {
+        for (int k = 0; k < QCH; ++k) {
             if constexpr (FMT == FMT_BYTE) {
                 q[2 * k] = bf2(v[k][0], v[k][1]);
                 q[2 * k + 1] = bf2(v[k][2], v[k][3]);
@@ -260,6 +290,31 @@ struct ScoreMma {
                     ldmatrix_x4(w1, row + (k + 1) * 512);
 #pragma unroll
                     for (int t = 0; t < 2; ++t) mma_f16_16816(d[t], w0[2 * t], w0[2 * t + 1], w1[2 * t], w1[2 * t + 1], q[k], q[k + 1]);
+                }
+            } else if constexpr (FMT == FMT_FP4) {
+                const int r = lane >> 2, c = lane & 3;
+#pragma unroll
+                for (int h = 0; h < QCH; ++h) {                                // 64 channels
+                    const uint32_t sw = lds_u32(planes + h * 128 + (c * 8 + r) * 4);
+                    const uint32_t s[4] = {fp4_scale2<0>(sw, one), fp4_scale2<1>(sw, one), fp4_scale2<2>(sw, one), fp4_scale2<3>(sw, one)};
+#pragma unroll
+                    for (int k = 2 * h; k < 2 * h + 2; ++k) {
+                        uint32_t w[4];
+                        ldmatrix_x4(w, row + k * 512);
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            uint32_t x[4], y[4];
+                            fp4_to_half2(w[2 * t], x);
+                            fp4_to_half2(w[2 * t + 1], y);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                x[i] = mul_half2(x[i], s[2 * t]);
+                                y[i] = mul_half2(y[i], s[2 * t + 1]);
+                            }
+                            mma_f16_16816(d[t], x[0], y[0], x[1], y[1], q[4 * k], q[4 * k + 1]);
+                            mma_f16_16816(d[t], x[2], y[2], x[3], y[3], q[4 * k + 2], q[4 * k + 3]);
+                        }
+                    }
                 }
             } else if constexpr (!kDense) {
 #pragma unroll

@@ -256,7 +256,7 @@ extern "C" sa_status sa_shiftav_workspace_bytes(const sa_config* cfg, int batch,
     Plan p;
     const sa_status st = make_plan(cfg, &p);
     if (st != SA_OK) return st;
-    if (p.fp16 || p.int8) return SA_ERR_UNSUPPORTED;
+    if (p.fp16 || p.int8 || p.fp4) return SA_ERR_UNSUPPORTED;
     p.matrix = false;
     p.shape = shift_shape(p.d, p.k);                             // the score pass is the shift-and-add kernel's
     int S, GT;
@@ -273,7 +273,7 @@ extern "C" sa_status sa_decode_attention_shiftav(const sa_config* cfg, const sa_
     Plan p;
     sa_status st = make_plan(cfg, &p);
     if (st != SA_OK) return st;
-    if (p.fp16 || p.int8) return SA_ERR_UNSUPPORTED;
+    if (p.fp16 || p.int8 || p.fp4) return SA_ERR_UNSUPPORTED;
     p.matrix = false;
     p.shape = shift_shape(p.d, p.k);                             // the score pass is the shift-and-add kernel's
     // INT32 tile accumulator: 32 keys x 128 x 2^N < 2^31

@@ -9,7 +9,8 @@
 //   A.V      O^T[dims][queries] += V^T[dims][keys] w[keys][queries] as m16n8k16 products: INT8 values are exact in
 //            binary16, every weight enters as the sum of two binary16 terms (22 significant bits for weights within
 //            2^-17 of the largest, an absolute 2^-38 of it below), accumulation in FP32.  The weights reach the operand layout
-//            through movmatrix, without shared memory.  (Binary16 values: one term, the weights rounded to binary16.)
+//            through movmatrix, without shared memory.  (Binary16 values: one term, the weights rounded to binary16.  4-bit values:
+//            code times scale, exact in binary16, two terms.)
 #pragma once
 #include "sa_common.cuh"
 #include "sa_decode_common.cuh"
@@ -28,9 +29,14 @@ constexpr float kRefMax = 268435456.0f;
 
 template <int FMT>
 constexpr int format_kb() { return FMT == FMT_PLANAR1 ? 1 : FMT == FMT_PLANAR2 ? 2 : FMT == FMT_INT8 ? 8 : 0; }
+// (4-bit cache: the keys' scale bytes in the place of a plane, the values' behind their codes.)
 template <int D, int FMT>
-using MmaStage = TileStage<ScoreMma<D, FMT>::CH, FMT != FMT_FP16, FMT == FMT_FP16 ? 2 * D : D,
-                           FMT == FMT_PLANAR1 ? 1 : FMT == FMT_PLANAR2 ? 2 : 0, D / 8>;
+using MmaStage = TileStage<ScoreMma<D, FMT>::CH, FMT != FMT_FP16 && FMT != FMT_FP4, FMT == FMT_FP16 ? 2 * D : FMT == FMT_FP4 ? D / 2 + D / 16 : D,
+                           FMT == FMT_PLANAR1 || FMT == FMT_FP4 ? 1 : FMT == FMT_PLANAR2 ? 2 : 0, FMT == FMT_FP4 ? D / 16 : D / 8>;
+template <int D, int FMT>
+constexpr int format_half_bytes() {
+    return FMT == FMT_FP16 ? half_block_bytes_fp16(D) : FMT == FMT_FP4 ? half_block_bytes_fp4(D) : half_block_bytes(D, format_kb<FMT>(), ScoreMma<D, FMT>::kDense);
+}
 
 // LONG: for warps with many tiles.  Everything rare (a first tile, a reference that moves, slots past the sequence's end) is
 // then out of the way of the other tiles, behind one vote, which is worth 2.5 % of a call with 55 tiles a warp; of calls with two,
@@ -47,6 +53,8 @@ struct TileMma {
     using Stage = MmaStage<D, FMT>;
     static constexpr int MT = D / 16;              // 16-dim row tiles of O^T
     static constexpr bool kFp16 = FMT == FMT_FP16;
+    static constexpr bool kFp4 = FMT == FMT_FP4;
+    static constexpr bool kPlain = kFp16 || kFp4;  // no scale of a value in its weight; rows r, r + 8 of the operand are dims r, r + 8; l is scaled as O is
     static_assert(!(FINE && kFp16), "binary16 values: the weights' rounding is an error 100 times as large");
     static constexpr int kNever = 0x7fffffff;
 
@@ -103,7 +111,7 @@ struct TileMma {
         uint32_t meta[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if constexpr (kFp16) {                            // no scales
+            if constexpr (kPlain) {                           // no scales
                 meta[j] = 0u;
                 vs[j] = (float)(1 << kWeightShift);
                 zq[j] = qs;
@@ -123,14 +131,15 @@ struct TileMma {
         float p[4][2], w[4][2];
         __half2 h[4];
         auto weights = [&] {
+            const f32x2 from = kFp4 ? add2(nR, pack_f32x2((float)kWeightShift, (float)kWeightShift)) : nR;     // (4 bits: 2^14 in the exponent)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float x0, x1;
-                unpack_f32x2(ffma2(pack_f32x2(z[j][0], z[j][1]), zq[j], nR), &x0, &x1);
+                unpack_f32x2(ffma2(pack_f32x2(z[j][0], z[j][1]), zq[j], from), &x0, &x1);
                 p[j][0] = ex2_approx(x0);
                 p[j][1] = ex2_approx(x1);
-                w[j][0] = p[j][0] * fabsf(vs[j]);
-                w[j][1] = p[j][1] * fabsf(vs[j]);
+                w[j][0] = kFp4 ? p[j][0] : p[j][0] * fabsf(vs[j]);
+                w[j][1] = kFp4 ? p[j][1] : p[j][1] * fabsf(vs[j]);
             }
         };
         // a weight beyond binary16 has become infinite: 0x7c00, the only value that 0x0400 carries into the sign bit
@@ -217,6 +226,7 @@ struct TileMma {
         }
         // ---- A.V: an 8 x 8 block of 16-bit pairs (8 keys x 16 dims of INT8), transposed by ldmatrix: row r of
         // the operand is dim 2 r (bytes 0, 2), row r + 8 dim 2 r + 1 (bytes 1, 3), columns the keys 2 c, 2 c + 1 ----
+        uint32_t codes[4], scales[4];                         // (4 bits)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             uint32_t x[4];
@@ -230,14 +240,38 @@ struct TileMma {
                     // slots past the end may hold anything (even NaN patterns): their weight is zero, but 0 * NaN is not
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const int key = 8 * j + 2 * c;
-                        const uint32_t keep = key >= n_valid ? 0u : key + 1 >= n_valid ? 0x0000ffffu : 0xffffffffu;
+                        const uint32_t keep = keep_pair(8 * j + 2 * c, n_valid);
                         x[j] &= keep;
                         y[j] &= keep;
                     }
                 }
                 mma_f16_16816(acc[mt], x[0], y[0], x[1], y[1], bh[0], bh[1]);
                 mma_f16_16816(acc[mt], x[2], y[2], x[3], y[3], bh[2], bh[3]);
+                continue;
+            }
+            if constexpr (kFp4) {                             // 16 bytes a lane are the codes of 32 channels, 16 their scales
+                if (mt % 2 == 0) {
+                    const uint32_t at = st + Stage::kVOff + mt / 2 * 512 + lane * 16, sc = st + Stage::kVOff + 16 * D + mt / 2 * 64 + c * 16;
+                    lds_u32x4(codes, at);
+                    lds_u32x4(scales, sc);
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    uint32_t v[4], s0 = fp4_pair_scale0(scales[mt % 2 * 2 + k], a.one), s1 = fp4_pair_scale1(scales[mt % 2 * 2 + k]);
+                    if (n_valid < 32) {                       // slots past the end may hold anything: 0 * NaN is not 0
+                        s0 &= keep_pair(16 * k + 2 * c, n_valid);
+                        s1 &= keep_pair(16 * k + 8 + 2 * c, n_valid);
+                    }
+                    fp4_to_half2(codes[mt % 2 * 2 + k], v);
+                    v[0] = mul_half2(v[0], s0);
+                    v[1] = mul_half2(v[1], s0);
+                    v[2] = mul_half2(v[2], s1);
+                    v[3] = mul_half2(v[3], s1);
+                    if (FINE && k == 0) mma_f16_16816_first(sum, v[0], v[1], v[2], v[3], bh[0], bh[1]);
+                    else mma_f16_16816(sum, v[0], v[1], v[2], v[3], bh[2 * k], bh[2 * k + 1]);
+                    mma_f16_16816(sum, v[0], v[1], v[2], v[3], bl[2 * k], bl[2 * k + 1]);
+                }
+                if constexpr (FINE) add_sums(acc[mt], own);
                 continue;
             }
             ldmatrix_x4_trans(x, st + Stage::kVOff + mt * 512 + lane * 16);
@@ -249,11 +283,14 @@ struct TileMma {
                 else mma_f16_16816(sum, a0, a1, a2, a3, bh[2 * k], bh[2 * k + 1]);
                 mma_f16_16816(sum, a0, a1, a2, a3, bl[2 * k], bl[2 * k + 1]);
             }
-            if constexpr (FINE) {
-                unpack_f32x2(add2(pack_f32x2(acc[mt][0], acc[mt][1]), pack_f32x2(own[0], own[1])), &acc[mt][0], &acc[mt][1]);
-                unpack_f32x2(add2(pack_f32x2(acc[mt][2], acc[mt][3]), pack_f32x2(own[2], own[3])), &acc[mt][2], &acc[mt][3]);
-            }
+            if constexpr (FINE) add_sums(acc[mt], own);
         }
+    }
+    // Which of the keys `key`, key + 1 count, as a mask of a pair of binary16.
+    SA_D static uint32_t keep_pair(int key, int n_valid) { return key >= n_valid ? 0u : key + 1 >= n_valid ? 0x0000ffffu : 0xffffffffu; }
+    SA_D static void add_sums(float (&to)[4], const float (&x)[4]) {
+        unpack_f32x2(add2(pack_f32x2(to[0], to[1]), pack_f32x2(x[0], x[1])), &to[0], &to[1]);
+        unpack_f32x2(add2(pack_f32x2(to[2], to[3]), pack_f32x2(x[2], x[3])), &to[2], &to[3]);
     }
 
     // This warp's {R, l} of every query to heads ([warp][8]), its O to its rows ([warp][GT][kRowStep]), as they are (weights' scale
@@ -280,7 +317,7 @@ struct TileMma {
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) {
                     float* row = row0 + e * kRowStep + 16 * mt;
-                    if constexpr (kFp16) {
+                    if constexpr (kPlain) {
                         row[r] = acc[mt][e];
                         row[r + 8] = acc[mt][2 + e];
                     } else {
@@ -323,12 +360,12 @@ struct TileMma {
         const float f0 = seen ? pow2i_neg(__float2int_rn(R0 - Rb0)) : 0.0f, f1 = seen ? pow2i_neg(__float2int_rn(R1 - Rb1)) : 0.0f;
         const float v0 = f0 * (1.0f / (1 << kWeightShift)), v1 = f1 * (1.0f / (1 << kWeightShift));
         if (r == 0) {
-            red_s[warp][2 * c][1] = l0 * (kFp16 ? v0 : f0);
-            red_s[warp][2 * c + 1][1] = l1 * (kFp16 ? v1 : f1);
+            red_s[warp][2 * c][1] = l0 * (kPlain ? v0 : f0);
+            red_s[warp][2 * c + 1][1] = l1 * (kPlain ? v1 : f1);
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-            if constexpr (kFp16) {
+            if constexpr (kPlain) {
                 const int dim = 16 * mt + r;
                 red_s[warp][2 * c][2 + dim] = acc[mt][0] * v0;
                 red_s[warp][2 * c][2 + dim + 8] = acc[mt][2] * v0;
