@@ -17,6 +17,9 @@ namespace sa {
 
 constexpr int kPageTokens = 64;
 constexpr int kTileTokens = 32;           // a page block is two halves of 32 tokens, each laid out like one staged tile
+// What a warp of the matrix kernels takes at a time: 2^5 tokens, half a page, or 2^6, a whole one (4-bit cache at head_dim 64: its halves are
+// small, and what a tile costs beside its products is paid once for 64 tokens).
+constexpr int tile_shift(int d, bool fp4) { return fp4 && d == 64 ? 6 : 5; }
 // Bytes of one half of a (page, KV head) block: code chunks, mantissa bit planes (dense planar container),
 // metadata, value chunks.  kb: mantissa bits (8 for the INT8 comparison code); nib: sub-byte container.
 // The page plan (make_plan) and the kernels' stage plans are both checked against it.
@@ -43,15 +46,15 @@ constexpr KernelShape fp16_shape(int d) { return d == 128 ? KernelShape{6, 2, 1}
 // ... over the 4-bit cache.
 constexpr KernelShape fp4_shape(int d) { return d == 128 ? KernelShape{6, 2, 2} : KernelShape{8, 2, 2}; }
 // The kernel of one block per SM (sa_decode_stream.cuh).
-constexpr KernelShape stream_shape(int d, bool fp16) {
-    return fp16 ? KernelShape{12, 1, d == 128 ? 1 : 2} : d == 128 ? KernelShape{12, 1, 2} : KernelShape{16, 1, 2};
+constexpr KernelShape stream_shape(int d, bool fp16, bool fp4 = false) {
+    return fp4 ? KernelShape{12, 1, 2} : fp16 ? KernelShape{12, 1, d == 128 ? 1 : 2} : d == 128 ? KernelShape{12, 1, 2} : KernelShape{16, 1, 2};
 }
-SA_HD constexpr int stream_unit_cost(int d) { return d == 128 ? 14 : 32; }     // what a block pays for going on to another unit, in tiles
-SA_HD constexpr int stream_merge_cost(int d) { return d == 128 ? 20 : 30; }    // ... for parts of a unit that other blocks have worked on
+SA_HD constexpr int stream_unit_cost(int d, int shift) { return d == 128 ? 14 : 32 >> (shift - 5); }     // what a block pays for going on to another unit, in tiles
+SA_HD constexpr int stream_merge_cost(int d, int shift) { return d == 128 ? 20 : 30 >> (shift - 5); }    // ... for parts of a unit that other blocks have worked on
 // U units of T tiles each on P blocks: parts that every unit is cut into (1: units stay whole), where the busiest block, merges
 // included, is then done sooner than with a cut that takes no notice of units (0).
-SA_HD int stream_parts(int T, int U, int P, int d) {
-    const int unit = stream_unit_cost(d), merge = stream_merge_cost(d), k = P / U < T ? P / U : T, c = (U + P - 1) / P;
+SA_HD int stream_parts(int T, int U, int P, int d, int shift) {
+    const int unit = stream_unit_cost(d, shift), merge = stream_merge_cost(d, shift), k = P / U < T ? P / U : T, c = (U + P - 1) / P;
     const int cut = (U * (T + unit) + P - 1) / P + merge, whole = c * T + (c - 1) * unit, even = k > 1 ? (T + k - 1) / k + merge : 0x7fffffff;
     return (whole < even ? whole : even) > cut ? 0 : even < whole ? k : 1;
 }

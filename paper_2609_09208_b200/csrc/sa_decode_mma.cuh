@@ -11,6 +11,7 @@
 #include "sa_decode_common.cuh"
 #include "sa_mma.cuh"
 #include "sa_stage.cuh"
+#include "sa_tile_fp4.cuh"
 #include "sa_tile_mma.cuh"
 
 namespace sa {
@@ -25,14 +26,15 @@ struct MmaSmem {
     static constexpr int kMbarOff = NW * NS * Stage::kBytes;
     static constexpr int kRefOff = kMbarOff + ((NW * NS * 8 + 127) & ~127);
     static constexpr int kHeadOff = kRefOff + NW * 8 * 4;
-    static constexpr int kBytes = kHeadOff + 8 * 8;
+    static constexpr int kScratchOff = kHeadOff + 8 * 8;      // (4-bit cache) decoded value scales of every warp
+    static constexpr int kBytes = kScratchOff + NW * Tile<D, FMT, false, format_fp4(FMT)>::kScratchBytes;
     static constexpr int kInOff = kBytes;                     // WHOLE: the unit's queries, new key and new value (host_in)
     static constexpr int kWholeBytes = kInOff + 10 * D * 2;
     static constexpr int kSumOff = NW * 8 * (D + 2) * 4;      // the block's O, behind the merge rows (within the stage buffers)
     static_assert(kSumOff + 8 * D * 4 <= NW * NS * Stage::kBytes, "merge rows and sums must fit in the stage buffers");
     static_assert(kHeadOff >= NW * NS * Stage::kBytes, "no copy may land on the marks");
     static_assert(NW * NS * Stage::kBytes >= kPlanScratchInts * 4, "the block plan's scratch must fit in the stage buffers");
-    static_assert(Stage::kBytes == format_half_bytes<D, FMT>(), "a stage buffer is a verbatim copy of half a page block");
+    static_assert(Stage::kHalfBytes == format_half_bytes<D, FMT>(), "a stage buffer is a verbatim copy of half a page block, or a whole one");
 };
 
 // This block's share of the outputs of a cluster (a.cluster blocks, each with the O[D] of its query heads at shared address
@@ -137,7 +139,8 @@ __global__ void __maxnreg__(D == 128 ? 168 : 112) decode_mma_kernel(const __grid
             fetch_inputs<D>(a, smem_addr(smem + SM::kInOff), blockIdx.z, kvh);
             host_rows = reinterpret_cast<const uint16_t*>(smem + SM::kInOff);
         }
-    TileMma<D, FMT, false, false> t;
+    Tile<D, FMT, false, format_fp4(FMT)> t;
+    if constexpr (t.kScratchBytes > 0) t.scratch = smem_addr(smem + SM::kScratchOff) + warp * t.kScratchBytes;
     int b = bp.b, n_tiles_g, first_g, tile1_g, pidx_g, lp_g, pnew_g;
     bool again;
 #pragma unroll 1
@@ -147,25 +150,25 @@ __global__ void __maxnreg__(D == 128 ? 168 : 112) decode_mma_kernel(const __grid
         const int len_g = (ranked ? bp.len : __ldcg(a.seq_lens + bq)) + (a.Knew ? 1 : 0);
         // ---- queries: reads only Q, which no kernel of a decode step writes, so it runs before the wait ----
         const uint16_t* q_rows = WHOLE && host_rows ? host_rows : a.Q + ((size_t)bq * a.Hq + h0) * D;
-        t.load_queries((lane >> 2) < GT ? q_rows + (lane >> 2) * D : nullptr, lane, a.hadamard != 0, a.zscale);
+        t.load_queries((lane >> 2) % t.kQueries < GT ? q_rows + (lane >> 2) % t.kQueries * D : nullptr, lane, a.hadamard != 0, a.zscale);
         // A guess at this warp's first tile, only to ask L2 for it while the preceding kernel drains (loads that bypass
         // L1, so nothing stale can be read back later).
-        n_tiles_g = (min(max(len_g, 0), a.max_pages * kPageTokens) + 31) >> 5;
+        n_tiles_g = (min(max(len_g, 0), a.max_pages * kPageTokens) + Stage::kTokens - 1) >> Stage::kShift;
         first_g = split_begin(n_tiles_g, bp.split, bp.n_splits) + warp;
         tile1_g = split_begin(n_tiles_g, bp.split + 1, bp.n_splits);
         lp_g = a.Knew && len_g > 0 ? (len_g - 1) / kPageTokens : -1;          // the new token's page
         if (lp_g >= a.max_pages) lp_g = -1;
         if (first_g < tile1_g) {
-            const int p_g = __ldcg(a.page_table + (size_t)bq * a.max_pages + (first_g >> 1));
+            const int p_g = __ldcg(a.page_table + (size_t)bq * a.max_pages + (first_g >> Stage::kPageShift));
             if (lane == 0 && p_g >= 0 && p_g < a.n_pages)
-                Stage::prefetch(a.pages + ((size_t)p_g * a.Hkv + kvh) * a.page_bytes, (first_g & 1) * 32, true);
+                Stage::prefetch(a.pages + ((size_t)p_g * a.Hkv + kvh) * a.page_bytes + Stage::part(first_g) * Stage::kBytes);
         }
         pdl_wait();                 // everything below reads what the preceding kernels in the stream wrote (the cache)
         // The pages of the guessed first tile and of the new token, read again now that they are valid, at the same time as
         // the length(s): one round trip where the guess holds, which it does unless a length crossed a tile boundary.  The
         // warp that is to write the new token asks for its rows as well.
         const int32_t* table_g = a.page_table + (size_t)bq * a.max_pages;
-        pidx_g = first_g < tile1_g ? table_g[first_g >> 1] : -1;
+        pidx_g = first_g < tile1_g ? table_g[first_g >> Stage::kPageShift] : -1;
         pnew_g = lp_g >= 0 ? table_g[lp_g] : -1;
         if (lp_g >= 0 && !a.host_in && n_tiles_g - 1 >= first_g && n_tiles_g == tile1_g && (n_tiles_g - 1 - first_g) % NW == 0) {
             const size_t row = ((size_t)bq * a.Hkv + kvh) * D;
@@ -196,11 +199,11 @@ __global__ void __maxnreg__(D == 128 ? 168 : 112) decode_mma_kernel(const __grid
         const int lp = len / kPageTokens;
         pidx_new = (len >= 0 && lp < a.max_pages) ? (lp == lp_g ? pnew_g : table[lp]) : -1;
         if (pidx_new >= 0 && pidx_new < a.n_pages) {
-            tile_new = len >> 5;
+            tile_new = len >> Stage::kShift;
             len += 1;
         }
     }
-    const int n_tiles = (min(len, a.max_pages * kPageTokens) + 31) >> 5;
+    const int n_tiles = (min(len, a.max_pages * kPageTokens) + Stage::kTokens - 1) >> Stage::kShift;
     const bool same = n_tiles == n_tiles_g;                       // the divisions of the guess stand
     const int first = same ? first_g : split_begin(n_tiles, bp.split, bp.n_splits) + warp;
     const int tile1 = same ? tile1_g : split_begin(n_tiles, bp.split + 1, bp.n_splits);
@@ -208,24 +211,24 @@ __global__ void __maxnreg__(D == 128 ? 168 : 112) decode_mma_kernel(const __grid
     // which of my tiles is the new token's (warp-uniform; the others' copies start before the token is encoded)
     const int i_new = (tile_new >= first && tile_new < tile1 && (tile_new - first) % NW == 0) ? (tile_new - first) / NW : -1;
     // Start the copy of a tile of mine, whose page is `pidx`, into the stage buffer at `st` with the mbarrier `mb`; returns how
-    // many of its keys count (32 or more: all).  A tile whose page is not mapped gets a plain arrival instead, which completes
+    // many of its keys count (a tile's or more: all).  A tile whose page is not mapped gets a plain arrival instead, which completes
     // the phase, and counts for none.
-    constexpr bool kEvenStep = NW % 2 == 0;                       // all tiles of a warp are the same half of their pages
-    const uint8_t* pool = a.pages + (size_t)kvh * a.page_bytes + (kEvenStep ? (first & 1) * Stage::kBytes : 0);
+    constexpr bool kEvenStep = NW % 2 == 0;                       // all tiles of a warp are the same part of their pages
+    const uint8_t* pool = a.pages + (size_t)kvh * a.page_bytes + (kEvenStep ? Stage::part(first) * Stage::kBytes : 0);
     const uint32_t page_step = (uint32_t)a.Hkv * (uint32_t)a.page_bytes;      // (the host refuses 2^32 and more)
     auto issue = [&](int tile, int pidx, uint32_t st, uint32_t mb) {
         const bool mapped = (unsigned)pidx < (unsigned)a.n_pages;
         if (lane == 0 && !(LOST && tile == a.lost_tile && b == a.lost_b && kvh == a.lost_kvh)) {     // test hook: that copy never starts
-            if (mapped) Stage::issue(st, pool + (uint64_t)(uint32_t)pidx * page_step, kEvenStep ? 0 : (tile & 1) * 32, mb);
+            if (mapped) Stage::issue(st, pool + (uint64_t)(uint32_t)pidx * page_step + (kEvenStep ? 0 : Stage::part(tile) * Stage::kBytes), mb);
             else mbar_arrive(mb);
         }
-        return mapped ? len - tile * 32 : 0;
+        return mapped ? len - tile * Stage::kTokens : 0;
     };
     int n_keys[NS];                                               // of the tiles in flight, the next one first
 #pragma unroll
     for (int i = 0; i < NS; ++i)
         if (i < n_my && i != i_new) {
-            const int pidx = (same && i == 0) ? pidx_g : table[(first + NW * i) >> 1];
+            const int pidx = (same && i == 0) ? pidx_g : table[(first + NW * i) >> Stage::kPageShift];
             n_keys[i] = issue(first + NW * i, pidx, stage0 + i * Stage::kBytes, mbar0 + i * 8);
         }
     if (i_new >= 0) {                                             // encode / quantise the token, write it into its page, copy its tile
@@ -252,12 +255,12 @@ __global__ void __maxnreg__(D == 128 ? 168 : 112) decode_mma_kernel(const __grid
     t.start();
     bool failed = false;
     uint32_t st = stage0, mb = mbar0;
-    const int32_t* next_page = table + ((first + NW * NS) >> 1);
+    const int32_t* next_page = table + ((first + NW * NS) >> Stage::kPageShift);
     int tile = first;
     for (int i = 0; i < n_my; ++i, tile += NW) {
         // the page of the tile that will take this stage over, fetched while this one is worked on
-        const int pidx_next = (i + NS < n_my) ? (kEvenStep ? *next_page : table[(tile + NW * NS) >> 1]) : -1;
-        next_page += NW / 2;
+        const int pidx_next = (i + NS < n_my) ? (kEvenStep ? *next_page : table[(tile + NW * NS) >> Stage::kPageShift]) : -1;
+        next_page += NW >> Stage::kPageShift;
         // the decision is made warp-uniform: a lane must never leave the loop alone
         const uint32_t parity = (uint32_t)(i / NS) & 1u;
         if (!__all_sync(0xffffffffu, mbar_try_wait(mb, parity)) && !__all_sync(0xffffffffu, mbar_wait_bounded(mb, parity, kPolls))) {

@@ -5,7 +5,8 @@ namespace sa {
 template <int D>
 static void launch(const DecodeArgs& a, dim3 grid, cudaStream_t s) {
     constexpr KernelShape sh = fp4_shape(D);
-    launch_mma<D, FMT_FP4, 33, sh.warps, sh.blocks_per_sm, sh.stages>(a, grid, s);
+    if (a.gt <= 4) launch_mma<D, FMT_FP4_PAIR, 33, sh.warps, sh.blocks_per_sm, sh.stages>(a, grid, s);
+    else launch_mma<D, FMT_FP4, 33, sh.warps, sh.blocks_per_sm, sh.stages>(a, grid, s);
 }
 void launch_mma_fp4(int d, const DecodeArgs& a, dim3 grid, cudaStream_t s) {
     if (d == 64) launch<64>(a, grid, s);

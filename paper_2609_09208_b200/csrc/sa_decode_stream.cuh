@@ -20,6 +20,7 @@
 #include "sa_decode_common.cuh"
 #include "sa_mma.cuh"
 #include "sa_stage.cuh"
+#include "sa_tile_fp4.cuh"
 #include "sa_tile_mma.cuh"
 
 namespace sa {
@@ -35,12 +36,13 @@ struct StreamSmem {
     static constexpr int kLenOff = kMbarOff + ((NW * NS * 8 + 127) & ~127);
     static constexpr int kFactorOff = kLenOff + kRankedBatchMax * 4;
     static constexpr int kHeadOff = kFactorOff + 2 * NW * 8 * 4;
-    static constexpr int kRowOff = kHeadOff + 2 * NW * 8 * 8;
-    __host__ __device__ static constexpr int row_bytes(int heads) { return NW * heads * TileMma<D, FMT, true, false>::kRowStep * 4; }
+    static constexpr int kScratchOff = kHeadOff + 2 * NW * 8 * 8;                // (4-bit cache) decoded value scales of every warp
+    static constexpr int kRowOff = kScratchOff + NW * Tile<D, FMT, true, false>::kScratchBytes;
+    __host__ __device__ static constexpr int row_bytes(int heads) { return NW * heads * Tile<D, FMT, true, false>::kRowStep * 4; }
     __host__ __device__ static constexpr bool apart(int heads) { return kRowOff + row_bytes(heads) <= 227 * 1024; }
     static constexpr int bytes(int heads) { return kRowOff + (apart(heads) ? row_bytes(heads) : 0); }
     static_assert(row_bytes(8) <= NW * NS * Stage::kBytes, "the rows must fit in the stage buffers");
-    static_assert(NW % 2 == 0, "all tiles of a warp are the same half of their pages");
+    static_assert(NW % 2 == 0, "all tiles of a warp are the same part of their pages");
     static_assert(NS <= 2, "the loop swaps two stages");
 };
 
@@ -52,7 +54,7 @@ struct Stretch {
     int free;                     // virtual tiles in front of the real ones of every unit
 };
 // Tiles of a sequence of `len` tokens in the cut: an empty one counts as one, so that a block takes care of its output.
-SA_D int stretch_tiles(int len, int cap) { return max((min(max(len, 0), cap) + 31) >> 5, 1); }
+SA_D int stretch_tiles(int len, int cap, int shift) { return max((min(max(len, 0), cap) + (1 << shift) - 1) >> shift, 1); }
 
 // before, lens: of sequences lane * K .. lane * K + K - 1, without and with the token that the call appends.
 // Every unit has `free` tiles that cost nothing in front of its real ones: a block that goes on to another unit has its merge and
@@ -65,20 +67,20 @@ SA_D int stretch_tiles(int len, int cap) { return max((min(max(len, 0), cap) + 3
 //   d = 128, 32 / 8 heads: 24 x 256 of 4096 20.4 / 14.7 / 11.3, 32 x 512 of 8192 12.9 / 20.7 / 15.7, 32 x 2048 of 8192 32.9 / 37.6 / 34.0.
 // (256 short units are what fills the other kernel's slots once, two units side by side on an SM and no splits; here a block has
 // two of them one after the other.)
-template <int D>
+template <int D, int SHIFT>
 SA_D Stretch cut_stretch(const DecodeArgs& a, const int (&before)[kLaneSeqs], const int (&lens)[kLaneSeqs], int K, int lane, int blk) {
     const int B = a.batch, cap = a.max_pages * kPageTokens, R = a.Hkv * (a.G / a.gt), P = gridDim.x;
     int t[kLaneSeqs], sum = 0;
     bool same = true;
 #pragma unroll
-    for (int k = 0; k < kLaneSeqs; ++k) t[k] = k < K && lane * K + k < B ? stretch_tiles(lens[k], cap) : 0;
+    for (int k = 0; k < kLaneSeqs; ++k) t[k] = k < K && lane * K + k < B ? stretch_tiles(lens[k], cap, SHIFT) : 0;
     const int T = __shfl_sync(0xffffffffu, t[0], 0);
 #pragma unroll
     for (int k = 0; k < kLaneSeqs; ++k) same = same && (t[k] == 0 || t[k] == T);
     same = __all_sync(0xffffffffu, same);
     Stretch s;
-    const int parts = same ? stream_parts(T, R * B, P, D) : 0;
-    s.free = parts ? (parts - T % parts) % parts : stream_unit_cost(D);            // (even parts)
+    const int parts = same ? stream_parts(T, R * B, P, D, SHIFT) : 0;
+    s.free = parts ? (parts - T % parts) % parts : stream_unit_cost(D, SHIFT);            // (even parts)
 #pragma unroll
     for (int k = 0; k < kLaneSeqs; ++k) sum += t[k] ? t[k] + s.free : 0;
     int upto = sum;                                           // inclusive prefix over the lanes
@@ -142,8 +144,8 @@ struct FinishArgs {
 // order of the blocks.
 template <int D, int FMT, int NW>
 SA_D void finish_units(const FinishArgs& a, const UnitSums& j0, const float* rows0, const UnitSums& j1, const float* rows1) {
-    constexpr int NT = 32 * NW, kStep = TileMma<D, FMT, true, false>::kRowStep;
-    constexpr float kValueScale = 1.0f / (1 << kWeightShift), kSumScale = TileMma<D, FMT, true, false>::kPlain ? kValueScale : 1.0f;
+    constexpr int NT = 32 * NW, kStep = Tile<D, FMT, true, false>::kRowStep;
+    constexpr float kValueScale = 1.0f / (1 << kWeightShift), kSumScale = Tile<D, FMT, true, false>::kPlain ? kValueScale : 1.0f;
     const int GT = a.GT;
     if (threadIdx.x < 2 * NW * 8) {                           // every warp's 2^(R - R of the block's largest), and l times that
         float2* h = a.heads + threadIdx.x / (NW * 8) * (NW * 8);
@@ -294,9 +296,10 @@ __global__ void __maxnreg__(NW > 12 ? 128 : 168) decode_stream_kernel(const __gr
     __syncwarp();
     pdl_launch_dependents();
 
-    TileMma<D, FMT, true, FINE> t;
+    Tile<D, FMT, true, FINE> t;
+    if constexpr (t.kScratchBytes > 0) t.scratch = smem_addr(smem + SM::kScratchOff) + warp * t.kScratchBytes;
     auto load_queries = [&](int y, int b) {
-        const int h0 = (y / chunks) * a.G + (y % chunks) * GT, r = lane >> 2;
+        const int h0 = (y / chunks) * a.G + (y % chunks) * GT, r = (lane >> 2) % t.kQueries;
         t.load_queries(r < GT ? a.Q + ((size_t)b * a.Hq + h0 + r) * D : nullptr, lane, a.hadamard != 0, a.zscale);
     };
     Stretch s;
@@ -304,14 +307,14 @@ __global__ void __maxnreg__(NW > 12 ? 128 : 168) decode_stream_kernel(const __gr
     bool again = LOST;                                        // (the test hook makes its first cut for another block)
 #pragma unroll 1
     for (;;) {
-        s = cut_stretch<D>(a, before, lens, K, lane, LOST && again ? (blockIdx.x + 1) % gridDim.x : blockIdx.x);
+        s = cut_stretch<D, Stage::kShift>(a, before, lens, K, lane, LOST && again ? (blockIdx.x + 1) % gridDim.x : blockIdx.x);
         // this warp's first tile: L2 is asked for it while the preceding kernel drains, its page is read behind the wait
         const int32_t* table = a.page_table + (size_t)s.b * a.max_pages;
-        const int first_g = max(s.t0 - s.start - s.free, 0) + warp, end_g = min(min(s.t1 - s.start - s.free, s.tiles), a.max_pages * 2);
-        const int p = first_g < end_g ? __ldcg(table + (first_g >> 1)) : -1;
+        const int first_g = max(s.t0 - s.start - s.free, 0) + warp, end_g = min(min(s.t1 - s.start - s.free, s.tiles), a.max_pages << Stage::kPageShift);
+        const int p = first_g < end_g ? __ldcg(table + (first_g >> Stage::kPageShift)) : -1;
         load_queries(s.y, s.b);                               // reads only Q, which no kernel of a decode step writes
         if (lane == 0 && (unsigned)p < (unsigned)a.n_pages)
-            Stage::prefetch(a.pages + ((size_t)p * a.Hkv + s.y / chunks) * a.page_bytes, (first_g & 1) * 32, true);
+            Stage::prefetch(a.pages + ((size_t)p * a.Hkv + s.y / chunks) * a.page_bytes + Stage::part(first_g) * Stage::kBytes);
         pdl_wait();                 // everything below reads what the preceding kernels in the stream wrote
         // one round trip where the cut stands
         int now[kLaneSeqs], grown[kLaneSeqs];
@@ -321,12 +324,12 @@ __global__ void __maxnreg__(NW > 12 ? 128 : 168) decode_stream_kernel(const __gr
             grown[k] = before[k] + appends(k, before[k]);
         }
 #pragma unroll
-        for (int i = 0; i < NS; ++i) pidx_g[i] = first_g + NW * i < end_g ? table[(first_g + NW * i) >> 1] : -1;
+        for (int i = 0; i < NS; ++i) pidx_g[i] = first_g + NW * i < end_g ? table[(first_g + NW * i) >> Stage::kPageShift] : -1;
         const int lp_g = a.Knew && s.len >= 0 ? s.len / kPageTokens : a.max_pages;           // the new token's page
         pnew_g = lp_g < a.max_pages ? table[lp_g] : -1;
         if (a.Knew && lp_g < a.max_pages) {                   // its rows, for the warp that is to write it
-            const int i = (s.len >> 5) - first_g;
-            if (i >= 0 && (s.len >> 5) < end_g && i % NW == 0) {
+            const int i = (s.len >> Stage::kShift) - first_g;
+            if (i >= 0 && (s.len >> Stage::kShift) < end_g && i % NW == 0) {
                 const size_t row = ((size_t)s.b * a.Hkv + s.y / chunks) * D;
                 asm volatile("prefetch.global.L1 [%0];" ::"l"(a.Knew + row + lane * (D / 32)));
                 asm volatile("prefetch.global.L1 [%0];" ::"l"(a.Vnew + row + lane * (D / 32)));
@@ -367,11 +370,11 @@ __global__ void __maxnreg__(NW > 12 ? 128 : 168) decode_stream_kernel(const __gr
             const int lp = len / kPageTokens;
             pidx_new = !next ? pnew_g : (len >= 0 && lp < a.max_pages) ? table[lp] : -1;
             if (pidx_new >= 0 && pidx_new < a.n_pages) {
-                tile_new = len >> 5;
+                tile_new = len >> Stage::kShift;
                 len += 1;
             }
         }
-        if (next) s.tiles = stretch_tiles(len, a.max_pages * kPageTokens);
+        if (next) s.tiles = stretch_tiles(len, a.max_pages * kPageTokens, Stage::kShift);
         const int lo = max(s.t0 - s.start - s.free, 0), hi = min(s.t1 - s.start - s.free, s.tiles);   // this block's tiles of the unit
         const bool more = s.t1 > s.start + s.free + s.tiles + s.free;        // a unit with tiles for this block follows
         unit.any = lo < hi;
@@ -379,25 +382,25 @@ __global__ void __maxnreg__(NW > 12 ? 128 : 168) decode_stream_kernel(const __gr
             // ---- this warp's tiles (as in decode_mma_kernel), in turn through the units ----
             const int first = lo + (warp + NW - turn) % NW;
             turn = (turn + hi - lo) % NW;
-            const int tile1 = min(hi, (min(len, a.max_pages * kPageTokens) + 31) >> 5);
+            const int tile1 = min(hi, (min(len, a.max_pages * kPageTokens) + Stage::kTokens - 1) >> Stage::kShift);
             const int n_my = first < tile1 && !lost ? (tile1 - first + NW - 1) / NW : 0;
             const int i_new = (tile_new >= first && tile_new < tile1 && (tile_new - first) % NW == 0) ? (tile_new - first) / NW : -1;
-            const uint8_t* pool = a.pages + (size_t)kvh * a.page_bytes + (first & 1) * Stage::kBytes;
+            const uint8_t* pool = a.pages + (size_t)kvh * a.page_bytes + Stage::part(first) * Stage::kBytes;
             const uint32_t page_step = (uint32_t)a.Hkv * (uint32_t)a.page_bytes;
             auto issue = [&](int tile, int pidx, uint32_t st, uint32_t mb) {
                 const bool mapped = (unsigned)pidx < (unsigned)a.n_pages;
                 if (lane == 0 && !(LOST && tile == a.lost_tile && b == a.lost_b && kvh == a.lost_kvh)) {
-                    if (mapped) Stage::issue(st, pool + (uint64_t)(uint32_t)pidx * page_step, 0, mb);
+                    if (mapped) Stage::issue(st, pool + (uint64_t)(uint32_t)pidx * page_step, mb);
                     else mbar_arrive(mb);
                 }
-                return mapped ? len - tile * 32 : 0;
+                return mapped ? len - tile * Stage::kTokens : 0;
             };
             int n_keys[NS];
             if (next && lane == 0) fence_proxy_async();       // (the stages were read, as before every copy in the loop)
 #pragma unroll
             for (int i = 0; i < NS; ++i)
                 if (i < n_my && i != i_new) {
-                    const int pidx = !next ? pidx_g[i] : table[(first + NW * i) >> 1];
+                    const int pidx = !next ? pidx_g[i] : table[(first + NW * i) >> Stage::kPageShift];
                     n_keys[i] = issue(first + NW * i, pidx, stage0 + (done + i) % NS * Stage::kBytes, mbar0 + (done + i) % NS * 8);
                 }
             if (i_new >= 0) {                                 // encode / quantise the token, write it into its page, copy its tile
@@ -421,9 +424,9 @@ __global__ void __maxnreg__(NW > 12 ? 128 : 168) decode_stream_kernel(const __gr
             if (next) load_queries(s.y, b);
             t.start();
             uint32_t st = stage0 + done % NS * Stage::kBytes, mb = mbar0 + done % NS * 8;
-            const int32_t* next_page = table + ((first + NW * NS) >> 1);
+            const int32_t* next_page = table + ((first + NW * NS) >> Stage::kPageShift);
             int tile = first;
-            for (int i = 0; i < n_my; ++i, tile += NW, next_page += NW / 2) {
+            for (int i = 0; i < n_my; ++i, tile += NW, next_page += NW >> Stage::kPageShift) {
                 // the page of the tile that will take this stage over, fetched while this one is worked on
                 const int pidx_next = (i + NS < n_my) ? *next_page : -1;
                 const uint32_t parity = (uint32_t)((done + i) / NS) & 1u;
@@ -491,10 +494,11 @@ __global__ void __maxnreg__(NW > 12 ? 128 : 168) decode_stream_kernel(const __gr
 
 template <int D, int FMT, int CODE, bool FINE, bool LOST>
 static void launch_stream_as(const DecodeArgs& a, cudaStream_t s) {
-    constexpr KernelShape sh = stream_shape(D, FMT == FMT_FP16);
+    constexpr KernelShape sh = stream_shape(D, FMT == FMT_FP16, format_fp4(FMT));
     using SM = StreamSmem<D, FMT, sh.warps, sh.stages>;
     constexpr int most = SM::apart(8) ? SM::bytes(8) : SM::apart(4) ? SM::bytes(4) : SM::bytes(1);
     static_assert(most >= SM::bytes(1) && most >= SM::bytes(2) && most >= SM::bytes(4) && most >= SM::bytes(8), "for any number of heads");
+    static_assert(!format_fp4(FMT) || SM::apart(8), "... of 1 to 8");
     static OncePerDevice once;
     auto kernel = decode_stream_kernel<D, FMT, CODE, sh.warps, sh.stages, FINE, LOST>;
     if (!allow_shared(kernel, most, once)) return;            // (the caller asks for the last error)
@@ -502,7 +506,8 @@ static void launch_stream_as(const DecodeArgs& a, cudaStream_t s) {
 }
 template <int D, int FMT, int CODE, bool LOST = false>
 static void launch_stream(const DecodeArgs& a, cudaStream_t s) {
-    if (FMT != FMT_FP16 && !LOST && a.fine) launch_stream_as<D, FMT, CODE, FMT != FMT_FP16 && !LOST, LOST>(a, s);
+    if constexpr (format_fp4(FMT)) launch_stream_as<D, FMT, CODE, true, LOST>(a, s);
+    else if (FMT != FMT_FP16 && !LOST && a.fine) launch_stream_as<D, FMT, CODE, FMT != FMT_FP16 && !LOST, LOST>(a, s);
     else launch_stream_as<D, FMT, CODE, false, LOST>(a, s);
 }
 

@@ -2,5 +2,7 @@
 #include "sa_decode_stream.cuh"
 
 namespace sa {
-void launch_stream_fp4(int d, const DecodeArgs& a, cudaStream_t s) { d == 64 ? launch_stream<64, FMT_FP4, 33>(a, s) : launch_stream<128, FMT_FP4, 33>(a, s); }
+template <int D>
+static void launch(const DecodeArgs& a, cudaStream_t s) { a.gt <= 4 ? launch_stream<D, FMT_FP4_PAIR, 33>(a, s) : launch_stream<D, FMT_FP4, 33>(a, s); }
+void launch_stream_fp4(int d, const DecodeArgs& a, cudaStream_t s) { d == 64 ? launch<64>(a, s) : launch<128>(a, s); }
 }  // namespace sa

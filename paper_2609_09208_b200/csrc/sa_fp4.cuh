@@ -79,6 +79,10 @@ SA_D uint32_t mul_half2(uint32_t a, uint32_t b) {
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
+// Two floats minus a pair of binary16, exactly where they round to it.
+SA_D void floats_minus_half2(float x, float y, uint32_t h, float* dx, float* dy) {
+    asm("{.reg .b16 l, h, m;\n\tmov.b32 {l, h}, %2;\n\tmov.b16 m, 0xbc00;\n\tfma.rn.f32.f16 %0, l, m, %3;\n\tfma.rn.f32.f16 %1, h, m, %4;}" : "=f"(*dx), "=f"(*dy) : "r"(h), "f"(x), "f"(y));
+}
 // Byte J of a word of scales, twice, as binary16 (one: the value 1, opaque: a shift as a multiplication).
 template <int J>
 SA_D uint32_t fp4_scale2(uint32_t w, uint32_t one) {
@@ -86,7 +90,7 @@ SA_D uint32_t fp4_scale2(uint32_t w, uint32_t one) {
 }
 // Scales of the two pairs of tokens of a word of value scales.
 SA_D uint32_t fp4_pair_scale0(uint32_t w, uint32_t one) { return (w & 0x00ff00ffu) * (one * 128u); }
-SA_D uint32_t fp4_pair_scale1(uint32_t w) { return (w >> 1) & 0x7f807f80u; }
+SA_D uint32_t fp4_pair_scale1(uint32_t w, uint32_t one) { return __byte_perm(w, 0u, 0x4341u) * (one * 128u); }
 
 // Places in half a block, from the start of the key codes (first two) or of the value codes.
 SA_HD int fp4_key_byte(int t, int c) { return (2 * (c / 64) + c / 8 % 2) * 512 + t * 16 + c / 16 % 4 * 4 + c % 8 / 2; }

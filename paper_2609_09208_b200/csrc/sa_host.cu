@@ -146,8 +146,13 @@ int sm_count() {
 // (32 x 4096 tokens, d = 128: 256 blocks on 296 slots, 51.2 us, 56.3 in this kernel when that took 52.6).
 static bool stream_pays(const Plan& p, int batch, long long units, long long tiles, double cost, int S, int sms) {
     if (!p.matrix || batch < 2 || batch > kRankedBatchMax || units < 16) return false;
-    if (units * (tiles + stream_unit_cost(p.d)) >= (1LL << 30)) return false;       // (the kernel counts all tiles in 32 bits)
-    const double rounds = (double)units * (double)tiles / ((double)sms * stream_shape(p.d, p.fp16).warps), u = (double)units / sms;
+    if (units * (tiles + stream_unit_cost(p.d, tile_shift(p.d, p.fp4))) >= (1LL << 30)) return false;       // (the kernel counts all tiles in 32 bits)
+    const double rounds = (double)units * (double)tiles / ((double)sms * stream_shape(p.d, p.fp16, p.fp4).warps), u = (double)units / sms;
+    if (p.fp4) {
+        const long long room = (long long)sms * p.shape.blocks_per_sm;
+        if (S == 1 && units <= room && 5 * units >= 4 * room) return false;
+        return units >= (p.d == 64 ? 16 : 48) && rounds >= 2.0;
+    }
     if (rounds < (p.d == 128 && !p.fp16 ? 4.5 : 9.0)) return false;
     // binary16 tiles come at the copy rate in either kernel: nothing to gain on units that fill the other one's slots, once and unsplit
     // (d = 64, 64 x 4096 tokens 43.5 -> 45.3 us, 64 x 8192 83.5 -> 86.5; 64 x 1024 of 8192 11.5 -> 14.0)
@@ -167,15 +172,16 @@ static bool stream_pays(const Plan& p, int batch, long long units, long long til
 //     9.1e-7 / 1.6e-6 / 3.2e-7 (2.4e-6 / 4.2e-6 / 1.6e-7).
 // (With the line at the other kernel's own number of tiles 20 x 4096 and 13 x 8192 tokens took 39.2 and 45.5 us instead of 36.6 and 43.2.)
 static bool stream_is_fine(const Plan& p, long long units, long long tiles, int sms) {
-    if (p.fp16) return false;
-    const int parts = stream_parts((int)tiles, (int)units, sms, p.d);
+    if (p.fp16 || p.fp4) return false;                        // (4-bit cache: every tile's sums are always added on their own)
+    const int parts = stream_parts((int)tiles, (int)units, sms, p.d, tile_shift(p.d, p.fp4));
     const double most = parts ? (double)tiles / parts : units < sms ? (double)tiles * (double)units / sms : (double)tiles;
-    return most > 15.0 * stream_shape(p.d, false).warps;
+    return most > 15.0 * stream_shape(p.d, false, p.fp4).warps;
 }
 
 void split_plan(const Plan& p, int batch, int max_pages, int* n_splits, int* gt, bool* cluster, int* stream, bool* fine) {
     int GT = 1;
-    for (int c = 8; c >= 1; c >>= 1)
+    // (4-bit cache: any divisor of the group; 40 / 8 heads, 8 x 8192 tokens of head_dim 128: one pass over the cache, not five)
+    for (int c = 8; c >= 1; c = p.fp4 ? c - 1 : c >> 1)
         if (p.G % c == 0) { GT = c; break; }
     // One thread block per (split, KV head x query chunk, sequence); its warps take the 32-key
     // tiles of the block's slice in turn.  S is chosen by a small cost model of the
@@ -195,7 +201,7 @@ void split_plan(const Plan& p, int batch, int max_pages, int* n_splits, int* gt,
     const int bps = p.shape.blocks_per_sm, nw = p.shape.warps;
     const int n_sms = sm_count();
     const long long slots = (long long)n_sms * bps;
-    const long long tiles = (long long)max_pages * (kPageTokens / 32);
+    const long long tiles = (long long)max_pages << (6 - tile_shift(p.d, p.fp4));
     if (stream) *stream = 0;
     if (fine) *fine = false;
     if (cluster) *cluster = false;

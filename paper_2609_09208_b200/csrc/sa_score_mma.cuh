@@ -40,8 +40,10 @@
 
 namespace sa {
 
-// FMT_FP16: the unquantised cache; FMT_BYTE3: the byte container of the codes with at most three mantissa bits (all but PoT-M4)
-enum ScoreFormat { FMT_BYTE = 0, FMT_NIBBLE = 1, FMT_PLANAR1 = 2, FMT_PLANAR2 = 3, FMT_INT8 = 4, FMT_BYTE3 = 5, FMT_FP16 = 6, FMT_FP4 = 7 };
+// FMT_FP16: the unquantised cache; FMT_BYTE3: the byte container of the codes with at most three mantissa bits (all but PoT-M4);
+// FMT_FP4_PAIR: the 4-bit cache in blocks of at most 4 queries, which fill the products' columns twice (sa_tile_mma.cuh)
+enum ScoreFormat { FMT_BYTE = 0, FMT_NIBBLE = 1, FMT_PLANAR1 = 2, FMT_PLANAR2 = 3, FMT_INT8 = 4, FMT_BYTE3 = 5, FMT_FP16 = 6, FMT_FP4 = 7, FMT_FP4_PAIR = 8 };
+SA_HD constexpr bool format_fp4(int fmt) { return fmt == FMT_FP4 || fmt == FMT_FP4_PAIR; }
 
 // Codes I, I + 1 of a word of the byte container (sign << 7 | mantissa << 3 | g) as a pair of bfloat16 values.  With the byte in
 // both halves of its value, the mantissa field and the sign are where bfloat16 has them; g moves to bits 9..7.
@@ -89,9 +91,9 @@ template <int D, int FMT>
 struct ScoreMma {
     static constexpr bool kInt = (FMT == FMT_NIBBLE || FMT == FMT_INT8);
     static constexpr bool kDense = (FMT == FMT_NIBBLE || FMT == FMT_PLANAR1 || FMT == FMT_PLANAR2);
-    static constexpr int E = FMT == FMT_FP4 ? 16 : FMT == FMT_FP16 ? 2 : kDense ? 8 : 4;
+    static constexpr int E = format_fp4(FMT) ? 16 : FMT == FMT_FP16 ? 2 : kDense ? 8 : 4;
     static constexpr int QCH = D / (4 * E);                       // chunks of the query
-    static constexpr int CH = FMT == FMT_FP4 ? D / 32 : QCH;      // code chunks
+    static constexpr int CH = format_fp4(FMT) ? D / 32 : QCH;      // code chunks
     static constexpr int NACC = (FMT == FMT_BYTE && D == 128) ? 2 : 1;
     static constexpr int NB = kInt ? D / 16 : D / 8;              // registers of B fragments
     uint32_t q[NB];
@@ -106,7 +108,7 @@ struct ScoreMma {
 #pragma unroll
             for (int k = 0; k < CH; ++k) q[k] = row ? *reinterpret_cast<const uint32_t*>(row + k * 8 + c * 2) : 0u;
             return 1.0f;
-        } else if constexpr (FMT == FMT_FP4) {                    // nothing to quantise; a lane has 16 channels of every 64
+        } else if constexpr (format_fp4(FMT)) {                    // nothing to quantise; a lane has 16 channels of every 64
             if (hadamard) {
                 float x[QCH][E];
 #pragma unroll
@@ -281,7 +283,10 @@ struct ScoreMma {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sc[2 * t + (e >> 1)][e & 1] = (float)d[t][e];      // below 2^24: exact
         } else {
-            float d[2 * NACC][4] = {};
+            float d[2 * NACC][4];
+            if constexpr (!format_fp4(FMT))
+#pragma unroll
+                for (int i = 0; i < 8 * NACC; ++i) d[i / 4][i % 4] = 0.0f;
             if constexpr (FMT == FMT_FP16) {
 #pragma unroll
                 for (int k = 0; k < CH; k += 2) {
@@ -291,7 +296,7 @@ struct ScoreMma {
 #pragma unroll
                     for (int t = 0; t < 2; ++t) mma_f16_16816(d[t], w0[2 * t], w0[2 * t + 1], w1[2 * t], w1[2 * t + 1], q[k], q[k + 1]);
                 }
-            } else if constexpr (FMT == FMT_FP4) {
+            } else if constexpr (format_fp4(FMT)) {
                 const int r = lane >> 2, c = lane & 3;
 #pragma unroll
                 for (int h = 0; h < QCH; ++h) {                                // 64 channels
@@ -311,7 +316,8 @@ struct ScoreMma {
                                 x[i] = mul_half2(x[i], s[2 * t]);
                                 y[i] = mul_half2(y[i], s[2 * t + 1]);
                             }
-                            mma_f16_16816(d[t], x[0], y[0], x[1], y[1], q[4 * k], q[4 * k + 1]);
+                            if (k == 0) mma_f16_16816_first(d[t], x[0], y[0], x[1], y[1], q[0], q[1]);
+                            else mma_f16_16816(d[t], x[0], y[0], x[1], y[1], q[4 * k], q[4 * k + 1]);
                             mma_f16_16816(d[t], x[2], y[2], x[3], y[3], q[4 * k + 2], q[4 * k + 3]);
                         }
                     }

@@ -9,8 +9,8 @@
 //   A.V      O^T[dims][queries] += V^T[dims][keys] w[keys][queries] as m16n8k16 products: INT8 values are exact in
 //            binary16, every weight enters as the sum of two binary16 terms (22 significant bits for weights within
 //            2^-17 of the largest, an absolute 2^-38 of it below), accumulation in FP32.  The weights reach the operand layout
-//            through movmatrix, without shared memory.  (Binary16 values: one term, the weights rounded to binary16.  4-bit values:
-//            code times scale, exact in binary16, two terms.)
+//            through movmatrix, without shared memory.  (Binary16 values: one term, the weights rounded to binary16.  4-bit cache: the
+//            state is the same, what is done with a tile is in sa_tile_fp4.cuh.)
 #pragma once
 #include "sa_common.cuh"
 #include "sa_decode_common.cuh"
@@ -31,11 +31,25 @@ template <int FMT>
 constexpr int format_kb() { return FMT == FMT_PLANAR1 ? 1 : FMT == FMT_PLANAR2 ? 2 : FMT == FMT_INT8 ? 8 : 0; }
 // (4-bit cache: the keys' scale bytes in the place of a plane, the values' behind their codes.)
 template <int D, int FMT>
-using MmaStage = TileStage<ScoreMma<D, FMT>::CH, FMT != FMT_FP16 && FMT != FMT_FP4, FMT == FMT_FP16 ? 2 * D : FMT == FMT_FP4 ? D / 2 + D / 16 : D,
-                           FMT == FMT_PLANAR1 || FMT == FMT_FP4 ? 1 : FMT == FMT_PLANAR2 ? 2 : 0, FMT == FMT_FP4 ? D / 16 : D / 8>;
+using HalfStage = TileStage<ScoreMma<D, FMT>::CH, FMT != FMT_FP16 && !format_fp4(FMT), FMT == FMT_FP16 ? 2 * D : format_fp4(FMT) ? D / 2 + D / 16 : D,
+                            FMT == FMT_PLANAR1 || format_fp4(FMT) ? 1 : FMT == FMT_PLANAR2 ? 2 : 0, format_fp4(FMT) ? D / 16 : D / 8>;
+// A tile: a half page or, in one piece, both (tile_shift).
+template <int D, int FMT>
+struct MmaStage : HalfStage<D, FMT> {
+    static constexpr int kShift = tile_shift(D, format_fp4(FMT)), kHalves = 1 << (kShift - 5), kHalfBytes = HalfStage<D, FMT>::kBytes;
+    static constexpr int kTokens = 32 * kHalves, kBytes = kHalves * kHalfBytes, kPageShift = 6 - kShift;     // tile >> kPageShift: its page
+    // which tile of its page a tile is
+    SA_D static int part(int tile) { return tile & ((1 << kPageShift) - 1); }
+    // Issued by one lane.  from: the tile's place in the cache.
+    SA_D static void issue(uint32_t dst, const uint8_t* from, uint32_t mbar) {
+        mbar_arrive_expect_tx(mbar, (uint32_t)kBytes);
+        bulk_g2s(dst, from, (uint32_t)kBytes, mbar);
+    }
+    SA_D static void prefetch(const uint8_t* from) { bulk_prefetch_l2(from, (uint32_t)kBytes); }
+};
 template <int D, int FMT>
 constexpr int format_half_bytes() {
-    return FMT == FMT_FP16 ? half_block_bytes_fp16(D) : FMT == FMT_FP4 ? half_block_bytes_fp4(D) : half_block_bytes(D, format_kb<FMT>(), ScoreMma<D, FMT>::kDense);
+    return FMT == FMT_FP16 ? half_block_bytes_fp16(D) : format_fp4(FMT) ? half_block_bytes_fp4(D) : half_block_bytes(D, format_kb<FMT>(), ScoreMma<D, FMT>::kDense);
 }
 
 // LONG: for warps with many tiles.  Everything rare (a first tile, a reference that moves, slots past the sequence's end) is
@@ -53,8 +67,11 @@ struct TileMma {
     using Stage = MmaStage<D, FMT>;
     static constexpr int MT = D / 16;              // 16-dim row tiles of O^T
     static constexpr bool kFp16 = FMT == FMT_FP16;
-    static constexpr bool kFp4 = FMT == FMT_FP4;
-    static constexpr bool kPlain = kFp16 || kFp4;  // no scale of a value in its weight; rows r, r + 8 of the operand are dims r, r + 8; l is scaled as O is
+    // binary16 and 4-bit values: no scale of a value in its weight, l is scaled as O is, rows r, r + 8 of the operand are dims r, r + 8
+    static constexpr bool kPlain = kFp16 || format_fp4(FMT);
+    static constexpr bool kPair = FMT == FMT_FP4_PAIR;     // columns 4 .. 7 hold the second terms of queries 0 .. 3 (sa_tile_fp4.cuh)
+    static constexpr int kQueries = kPair ? 4 : 8;         // rows of queries that a block has room for
+    static constexpr int kScratchBytes = 0;                // shared memory that a warp needs beside its stage buffers
     static_assert(!(FINE && kFp16), "binary16 values: the weights' rounding is an error 100 times as large");
     static constexpr int kNever = 0x7fffffff;
 
@@ -111,7 +128,7 @@ struct TileMma {
         uint32_t meta[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if constexpr (kPlain) {                           // no scales
+            if constexpr (kFp16) {                            // no scales
                 meta[j] = 0u;
                 vs[j] = (float)(1 << kWeightShift);
                 zq[j] = qs;
@@ -131,15 +148,14 @@ struct TileMma {
         float p[4][2], w[4][2];
         __half2 h[4];
         auto weights = [&] {
-            const f32x2 from = kFp4 ? add2(nR, pack_f32x2((float)kWeightShift, (float)kWeightShift)) : nR;     // (4 bits: 2^14 in the exponent)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 float x0, x1;
-                unpack_f32x2(ffma2(pack_f32x2(z[j][0], z[j][1]), zq[j], from), &x0, &x1);
+                unpack_f32x2(ffma2(pack_f32x2(z[j][0], z[j][1]), zq[j], nR), &x0, &x1);
                 p[j][0] = ex2_approx(x0);
                 p[j][1] = ex2_approx(x1);
-                w[j][0] = kFp4 ? p[j][0] : p[j][0] * fabsf(vs[j]);
-                w[j][1] = kFp4 ? p[j][1] : p[j][1] * fabsf(vs[j]);
+                w[j][0] = p[j][0] * fabsf(vs[j]);
+                w[j][1] = p[j][1] * fabsf(vs[j]);
             }
         };
         // a weight beyond binary16 has become infinite: 0x7c00, the only value that 0x0400 carries into the sign bit
@@ -226,7 +242,6 @@ struct TileMma {
         }
         // ---- A.V: an 8 x 8 block of 16-bit pairs (8 keys x 16 dims of INT8), transposed by ldmatrix: row r of
         // the operand is dim 2 r (bytes 0, 2), row r + 8 dim 2 r + 1 (bytes 1, 3), columns the keys 2 c, 2 c + 1 ----
-        uint32_t codes[4], scales[4];                         // (4 bits)
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             uint32_t x[4];
@@ -240,38 +255,14 @@ struct TileMma {
                     // slots past the end may hold anything (even NaN patterns): their weight is zero, but 0 * NaN is not
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const uint32_t keep = keep_pair(8 * j + 2 * c, n_valid);
+                        const int key = 8 * j + 2 * c;
+                        const uint32_t keep = key >= n_valid ? 0u : key + 1 >= n_valid ? 0x0000ffffu : 0xffffffffu;
                         x[j] &= keep;
                         y[j] &= keep;
                     }
                 }
                 mma_f16_16816(acc[mt], x[0], y[0], x[1], y[1], bh[0], bh[1]);
                 mma_f16_16816(acc[mt], x[2], y[2], x[3], y[3], bh[2], bh[3]);
-                continue;
-            }
-            if constexpr (kFp4) {                             // 16 bytes a lane are the codes of 32 channels, 16 their scales
-                if (mt % 2 == 0) {
-                    const uint32_t at = st + Stage::kVOff + mt / 2 * 512 + lane * 16, sc = st + Stage::kVOff + 16 * D + mt / 2 * 64 + c * 16;
-                    lds_u32x4(codes, at);
-                    lds_u32x4(scales, sc);
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    uint32_t v[4], s0 = fp4_pair_scale0(scales[mt % 2 * 2 + k], a.one), s1 = fp4_pair_scale1(scales[mt % 2 * 2 + k]);
-                    if (n_valid < 32) {                       // slots past the end may hold anything: 0 * NaN is not 0
-                        s0 &= keep_pair(16 * k + 2 * c, n_valid);
-                        s1 &= keep_pair(16 * k + 8 + 2 * c, n_valid);
-                    }
-                    fp4_to_half2(codes[mt % 2 * 2 + k], v);
-                    v[0] = mul_half2(v[0], s0);
-                    v[1] = mul_half2(v[1], s0);
-                    v[2] = mul_half2(v[2], s1);
-                    v[3] = mul_half2(v[3], s1);
-                    if (FINE && k == 0) mma_f16_16816_first(sum, v[0], v[1], v[2], v[3], bh[0], bh[1]);
-                    else mma_f16_16816(sum, v[0], v[1], v[2], v[3], bh[2 * k], bh[2 * k + 1]);
-                    mma_f16_16816(sum, v[0], v[1], v[2], v[3], bl[2 * k], bl[2 * k + 1]);
-                }
-                if constexpr (FINE) add_sums(acc[mt], own);
                 continue;
             }
             ldmatrix_x4_trans(x, st + Stage::kVOff + mt * 512 + lane * 16);
@@ -283,20 +274,25 @@ struct TileMma {
                 else mma_f16_16816(sum, a0, a1, a2, a3, bh[2 * k], bh[2 * k + 1]);
                 mma_f16_16816(sum, a0, a1, a2, a3, bl[2 * k], bl[2 * k + 1]);
             }
-            if constexpr (FINE) add_sums(acc[mt], own);
+            if constexpr (FINE) {
+                unpack_f32x2(add2(pack_f32x2(acc[mt][0], acc[mt][1]), pack_f32x2(own[0], own[1])), &acc[mt][0], &acc[mt][1]);
+                unpack_f32x2(add2(pack_f32x2(acc[mt][2], acc[mt][3]), pack_f32x2(own[2], own[3])), &acc[mt][2], &acc[mt][3]);
+            }
         }
     }
-    // Which of the keys `key`, key + 1 count, as a mask of a pair of binary16.
-    SA_D static uint32_t keep_pair(int key, int n_valid) { return key >= n_valid ? 0u : key + 1 >= n_valid ? 0x0000ffffu : 0xffffffffu; }
-    SA_D static void add_sums(float (&to)[4], const float (&x)[4]) {
-        unpack_f32x2(add2(pack_f32x2(to[0], to[1]), pack_f32x2(x[0], x[1])), &to[0], &to[1]);
-        unpack_f32x2(add2(pack_f32x2(to[2], to[3]), pack_f32x2(x[2], x[3])), &to[2], &to[3]);
-    }
 
+    SA_D void join_terms() {
+        if constexpr (kPair)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[mt][e] += __shfl_xor_sync(0xffffffffu, acc[mt][e], 2);
+    }
     // This warp's {R, l} of every query to heads ([warp][8]), its O to its rows ([warp][GT][kRowStep]), as they are (weights' scale
     // 2^14 included).  The row step keeps the lanes of a quad out of each other's banks.
     static constexpr int kRowStep = D + 8;
     SA_D void store_rows(float2* heads, float* rows, int GT, int lane, int warp) {
+        join_terms();
         const int r = lane >> 2, c = lane & 3;
         float l0, l1, nR0, nR1;
         unpack_f32x2(l, &l0, &l1);
@@ -334,6 +330,7 @@ struct TileMma {
     // (a copy that was merely late could still land in them).  after_barrier: what one warp does once all have come.
     template <int NW, typename After>
     SA_D bool merge_rows(float* ref_s, float (*red_s)[8][D + 2], int lane, int warp, bool failed, After after_barrier) {
+        join_terms();
         const int r = lane >> 2, c = lane & 3;
         float l0, l1, R0, R1;
         unpack_f32x2(l, &l0, &l1);

@@ -136,7 +136,7 @@ def run(d, Hq, Hkv, lens, *, hadamard=False, room=0, seed=0, scale=1.0, K=None, 
 
 SHAPES = [(64, 32, 4, [1024], False), (64, 1, 1, [1], False), (64, 32, 4, EDGES, True), (64, 6, 2, [95, 1, 0, 700], False), (64, 12, 1, [333], False),
           (64, 16, 1, [64, 63, 1000], True), (64, 5, 5, [129] * 3, False), (128, 32, 8, EDGES + [5000], False), (128, 1, 1, [4097], True),
-          (128, 16, 16, [31, 257], False), (128, 40, 8, [2000, 17], False), (64, 32, 4, [20000], False), (64, 8, 2, [(37 * i) % 400 for i in range(130)], False)]
+          (128, 16, 16, [31, 257], False), (128, 40, 8, [2000, 17], False), (128, 7, 1, [700, 64, 3], False), (64, 24, 2, [300, 65], True), (64, 11, 1, [200], False), (64, 32, 4, [20000], False), (64, 8, 2, [(37 * i) % 400 for i in range(130)], False)]
 
 
 @pytest.mark.parametrize("d,Hq,Hkv,lens,hadamard", SHAPES)
@@ -147,7 +147,7 @@ def test_decode_against_64_bits(d, Hq, Hkv, lens, hadamard):
         assert n or not O[b].any()
 
 
-STREAM = [(64, 32, 4, MIX, 16384, False), (64, 16, 1, MIX * 2, 16384, True),
+STREAM = [(64, 32, 4, MIX, 16384, False), (64, 32, 4, [777] * 36 + [900], 16384, False), (64, 32, 4, [95] * 127 + [300], 2048, True), (64, 16, 1, MIX * 2, 16384, True),
           (64, 8, 1, [(37 * i) % 400 for i in range(128)], 16384, False), (128, 32, 8, MIX, 16384, False), (128, 16, 16, MIX[:8] * 2, 8192, True),
           (64, 5, 5, MIX * 2, 16384, False), (128, 64, 8, MIX, 16384, False)]
 
@@ -287,7 +287,11 @@ def test_static_scratch_stages_and_repeats_give_the_same_bits():
     c.workspace.fill_(255)
     attend(cfg, c, Q, O[3])
     torch.cuda.synchronize()
-    assert all(torch.equal(O[0], o) for o in O[1:]) and not O[0][1].any()
+    assert torch.equal(O[0], O[1]) and torch.equal(O[0], O[3]) and not O[0][1].any()
+    # (in stages the merge kernel may add the same partials, at most 8 here, in another order than the blocks themselves: 7 roundings of 2^-24 each in the sums of
+    # either, two for the quotient, on both sides)
+    _, (_, size, _) = fp4.attention(case.Q, fp4.quantised(case.K), fp4.quantised(case.V), case.cu_lens, 8)
+    assert (np.abs((O[0] - O[2]).cpu().numpy()) <= 32 * 2.0 ** -24 * size).all()
     with pytest.raises(sa.SaError) as err:
         attend(cfg, c, Q, O[0], dbg_scores=torch.zeros(4 * 32 * 5056, dtype=torch.int32, device="cuda"))
     assert err.value.status == 2
