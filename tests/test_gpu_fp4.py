@@ -147,8 +147,8 @@ def test_decode_against_64_bits(d, Hq, Hkv, lens, hadamard):
         assert n or not O[b].any()
 
 
-STREAM = [(64, 32, 4, MIX, 16384, False), (64, 32, 4, [777] * 36 + [900], 16384, False), (64, 32, 4, [95] * 127 + [300], 2048, True), (64, 16, 1, MIX * 2, 16384, True),
-          (64, 8, 1, [(37 * i) % 400 for i in range(128)], 16384, False), (128, 32, 8, MIX, 16384, False), (128, 16, 16, MIX[:8] * 2, 8192, True),
+STREAM = [(64, 32, 4, MIX, 16384, False), (64, 32, 4, [777] * 30 + [9000] * 7, 16384, False), (64, 32, 4, [95] * 125 + [2000] * 3, 2048, True), (64, 16, 1, MIX * 2, 16384, True),
+          (64, 8, 1, [(37 * i) % 400 for i in range(128)], 16384, False), (128, 32, 8, MIX, 16384, False), (128, 16, 16, MIX[:12], 16384, True),
           (64, 5, 5, MIX * 2, 16384, False), (128, 64, 8, MIX, 16384, False)]
 
 
