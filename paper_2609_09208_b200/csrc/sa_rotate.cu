@@ -4,11 +4,16 @@
 // the token's positions, FP32 throughout, one rounding to binary16; values are converted.  Bound by memory (each input read, each
 // output written once); single tokens by latency.
 //
-// A block takes one token.  d / 8 lanes share a head vector; a lane holds two pieces of four channels whose pairs lie in the lane:
-// pairing halves, channels u .. u + 3 and their partners; pairing neighbours, eight channels in a row.  The rotation needs no
-// exchange, the norm one sum over the lanes.  The angles are the same for all heads: each is worked out by one thread of the
-// block, in 64 bits up to the fraction of a turn (position times frequency in 32 bits would be off by 0.01 rad at position 131 072),
-// and handed over in shared memory while the first vectors are on their way.
+// d / (2 P) lanes share a head vector; a lane holds two pieces of P channels whose pairs lie in the lane: pairing halves, channels
+// u .. u + P - 1 and their partners; pairing neighbours, 2 P channels in a row.  So the rotation needs no exchange, the norm one
+// sum over the lanes.  P = 8, 16-byte loads; 4 where halves are no multiple of 8 channels.  The angles are the same for all heads: each is worked out by one thread
+// of the block, in 64 bits up to the fraction of a turn (position times frequency in 32 bits would be off by 0.01 rad at position
+// 131 072), while the first vectors are on their way, and handed over in shared memory.
+// The threads of a block are dealt to tokens, and a thread stays with its token: the weights of a projection stay in its registers, packed FP32
+// pairs do the arithmetic.  Decode steps: a block of 256 threads per token; prompts: 8 tokens of a block (4 at head_dim 128), so that all
+// lanes have several vectors, the next one under way while one is worked on.  What is left above the copy rate are instructions, 14 for a channel.  us, 32 / 8 heads
+// of 128: 8192 tokens in bfloat16 with norms 51.1 -> 39.4 (5.1 TB/s), in FP32 53.7 (5.6 TB/s); one token of 32 / 4 heads of 64 2.0.  With sines and cosines
+// in registers (fewer threads) 42.6, with their negatives in a third table 41.5.
 #include "sa_cache_write.cuh"
 #include "sa_common.cuh"
 #include <cuda_bf16.h>
@@ -31,106 +36,171 @@ struct RotateArgs {
 constexpr int kRotateThreads = 256;
 constexpr int kRotateMost = 64;           // pairs
 
-template <typename T>
-SA_D void load4(const T* p, float (&x)[4]) {
-    if constexpr (sizeof(T) == 4) {
-        const float4 v = *reinterpret_cast<const float4*>(p);
-        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-    } else {
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
-        float2 a, b;
-        if constexpr (std::is_same_v<T, __half>) {
-            a = __half22float2(*reinterpret_cast<const __half2*>(&v.x));
-            b = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
-        } else {
-            a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.x));
-            b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.y));
-        }
-        x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+// P channels as they lie in memory, and as pairs of FP32.
+template <typename T, int P>
+struct Piece {
+    static constexpr int kWords = P * (int)sizeof(T) / 4;
+    uint32_t w[kWords];
+    SA_D void load(const T* p) {
+        if constexpr (kWords == 2) {
+            const uint2 v = *reinterpret_cast<const uint2*>(p);
+            w[0] = v.x, w[1] = v.y;
+        } else
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const uint4 v = reinterpret_cast<const uint4*>(p)[i / 4];
+                w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+            }
     }
-}
-SA_D void store4(uint16_t* p, const float (&x)[4]) {
-    const __half2 a = __floats2half2_rn(x[0], x[1]), b = __floats2half2_rn(x[2], x[3]);
-    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    SA_D void get(f32x2 (&x)[P / 2]) const {
+#pragma unroll
+        for (int i = 0; i < P / 2; ++i) {
+            if constexpr (sizeof(T) == 4) x[i] = pack_f32x2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+            else if constexpr (std::is_same_v<T, __half>) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+                x[i] = pack_f32x2(f.x, f.y);
+            } else x[i] = pack_f32x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));      // bfloat16: the upper half of an FP32 number
+        }
+    }
+};
+template <int P>
+SA_D void store_halves(uint16_t* p, const f32x2 (&x)[P / 2]) {
+    uint32_t h[P / 2];
+#pragma unroll
+    for (int i = 0; i < P / 2; ++i) {
+        float lo, hi;
+        unpack_f32x2(x[i], &lo, &hi);
+        const __half2 v = __floats2half2_rn(lo, hi);
+        h[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    if constexpr (P == 8) *reinterpret_cast<uint4*>(p) = make_uint4(h[0], h[1], h[2], h[3]);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(h[0], h[1]);
 }
 
-template <int D, typename T>
-__global__ void __launch_bounds__(kRotateThreads) rotate_kernel(const __grid_constant__ RotateArgs a) {
-    constexpr int L = D / 8, GROUPS = kRotateThreads / L;                          // lanes of a vector, vectors at a time
-    __shared__ float2 turn[kRotateMost];                                           // scale * (cos, sin) of every pair
-    const int64_t token = blockIdx.x;
-    const int l = threadIdx.x % L, half = a.R / 2;
-    const int pa = a.neighbours ? 8 * l : 4 * l < half ? 4 * l : a.R + 4 * l - half;                                 // first channels of the pieces
-    const int pb = a.neighbours ? 8 * l + 4 : 4 * l < half ? 4 * l + half : (a.R + D) / 2 + 4 * l - half;
+// TOKENS: of a block.  NEIGHBOURS: how channels pair.
+template <int D, typename T, int P, int TOKENS, bool NEIGHBOURS>
+__global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 4 ? 3 : 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
+    constexpr int L = D / (2 * P), THREADS = kRotateThreads / TOKENS, GROUPS = THREADS / L, H = P / 2;   // lanes of a vector; threads, vectors of a token
+    __shared__ __align__(16) float turn[TOKENS][2][kRotateMost];                               // scale * cos, scale * sin of every pair
+    const int64_t token0 = (int64_t)blockIdx.x * TOKENS;
+    const int slot = TOKENS == 1 ? 0 : threadIdx.x / THREADS, l = threadIdx.x % L, half = a.R / 2;
+    const int64_t token = token0 + slot;
+    const int pa = NEIGHBOURS ? 2 * P * l : P * l < half ? P * l : a.R + P * l - half;                               // first channels of the pieces
+    const int pb = NEIGHBOURS ? 2 * P * l + P : P * l < half ? P * l + half : (a.R + D) / 2 + P * l - half;
+    const uint32_t mine = ((1u << L) - 1u) << (threadIdx.x & 31 & ~(L - 1));       // the lanes of this vector
+    const int per = token < a.n ? a.heads[0] + a.heads[1] + a.heads[2] : 0;
+    Piece<T, P> first, second;
+    auto kind_of = [&](int v) { return v < a.heads[0] ? 0 : v < a.heads[0] + a.heads[1] ? 1 : 2; };
+    auto head_of = [&](int v, int kind) { return v - (kind == 0 ? 0 : kind == 1 ? a.heads[0] : a.heads[0] + a.heads[1]); };
+    auto load = [&](int v) {                                                       // vector v of the token
+        const int kind = kind_of(v);
+        const T* in = static_cast<const T*>(a.in[kind]) + token * a.stride[kind] + head_of(v, kind) * D;
+        first.load(in + pa);
+        second.load(in + pb);
+    };
+    int v = threadIdx.x % THREADS / L;
     pdl_wait();                                                                    // the projections may come from the kernel before
-    if ((int)threadIdx.x < half) {
-        const int j = threadIdx.x, axis = a.pair_axis ? min((int)a.pair_axis[j], a.axes - 1) : 0;
-        const double turns = (double)a.positions[axis * a.n + token] * (double)a.inv_freq[j] * 0.15915494309189535;
-        float s, c;
-        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-        turn[j] = make_float2(c * a.scale, s * a.scale);
+    if (v < per) load(v);
+    const int tokens = TOKENS == 1 ? 1 : (int)min((int64_t)TOKENS, a.n - token0);
+    for (int i = threadIdx.x; i < half * tokens; i += kRotateThreads) {
+        const int j = TOKENS == 1 ? i : i % half, k = TOKENS == 1 ? 0 : i / half;
+        const int axis = a.pair_axis ? min((int)a.pair_axis[j], a.axes - 1) : 0;
+        const double turns = (double)a.positions[axis * a.n + token0 + k] * (double)a.inv_freq[j] * 0.15915494309189535;
+        // within half a turn the fast functions are off by 2^-21.2 at most, a thousandth of what binary16 rounds away
+        const float x = (float)(turns - rint(turns)) * 6.2831853f;
+        turn[k][0][j] = __cosf(x) * a.scale;
+        turn[k][1][j] = __sinf(x) * a.scale;
     }
     __syncthreads();
-    const uint32_t mine = ((1u << L) - 1u) << (threadIdx.x & 31 & ~(L - 1));       // the lanes of this vector
-    const int total = a.heads[0] + a.heads[1] + a.heads[2];
-    for (int v = threadIdx.x / L; v < total; v += GROUPS) {
-        const int kind = v < a.heads[0] ? 0 : v < a.heads[0] + a.heads[1] ? 1 : 2;
-        const int h = kind == 0 ? v : kind == 1 ? v - a.heads[0] : v - a.heads[0] - a.heads[1];
-        const T* in = static_cast<const T*>(a.in[kind]) + token * a.stride[kind] + h * D;
-        uint16_t* out = a.out[kind] + (token * a.heads[kind] + h) * D;
-        float x[4], y[4];
-        load4(in + pa, x);
-        load4(in + pb, y);
+    const bool turns_a = pa < (NEIGHBOURS ? a.R : half), turns_b = NEIGHBOURS ? pb < a.R : turns_a;
+    // from shared memory for every vector: in registers they would cost a third of the threads, and with them of the bytes under way
+    const float *ca = turn[slot][0] + (NEIGHBOURS ? pa / 2 : pa), *sa = turn[slot][1] + (NEIGHBOURS ? pa / 2 : pa);
+    const float *cb = turn[slot][0] + pb / 2, *sb = turn[slot][1] + pb / 2;
+    Piece<T, P> wa, wb;
+    int weights_of = -1;
+    while (v < per) {
+        const int kind = kind_of(v);
+        f32x2 x[H], y[H];
+        first.get(x);
+        second.get(y);
+        uint16_t* out = a.out[kind] + (token * a.heads[kind] + head_of(v, kind)) * D;
+        v += GROUPS;
+        if (v < per) load(v);                                                      // (the next vector is under way while this one is worked on)
         if (kind < 2) {
             if (a.norm) {
-                float sum = 0.0f;
+                f32x2 sum2 = mul2(x[0], x[0]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum += x[i] * x[i] + y[i] * y[i];
+                for (int i = 1; i < H; ++i) sum2 = ffma2(x[i], x[i], sum2);
+#pragma unroll
+                for (int i = 0; i < H; ++i) sum2 = ffma2(y[i], y[i], sum2);
+                float lo, hi;
+                unpack_f32x2(sum2, &lo, &hi);
+                float sum = lo + hi;
 #pragma unroll
                 for (int o = 1; o < L; o <<= 1) sum += __shfl_xor_sync(mine, sum, o);
                 const float r = rsqrtf(sum * (1.0f / D) + a.eps);
-                float wx[4] = {1.0f, 1.0f, 1.0f, 1.0f}, wy[4] = {1.0f, 1.0f, 1.0f, 1.0f};
-                if (a.weight[kind]) {
-                    load4(static_cast<const T*>(a.weight[kind]) + pa, wx);
-                    load4(static_cast<const T*>(a.weight[kind]) + pb, wy);
+                const f32x2 rr = pack_f32x2(r, r);
+                if (weights_of != kind && a.weight[kind]) {
+                    weights_of = kind;
+                    wa.load(static_cast<const T*>(a.weight[kind]) + pa);
+                    wb.load(static_cast<const T*>(a.weight[kind]) + pb);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[i] = x[i] * r * wx[i];
-                    y[i] = y[i] * r * wy[i];
+                for (int i = 0; i < H; ++i) {
+                    x[i] = mul2(x[i], rr);
+                    y[i] = mul2(y[i], rr);
+                }
+                if (a.weight[kind]) {
+                    f32x2 w[H];
+                    wa.get(w);
+#pragma unroll
+                    for (int i = 0; i < H; ++i) x[i] = mul2(x[i], w[i]);
+                    wb.get(w);
+#pragma unroll
+                    for (int i = 0; i < H; ++i) y[i] = mul2(y[i], w[i]);
                 }
             }
-            if (a.neighbours) {
+            if constexpr (NEIGHBOURS) {
+                auto rotate = [](f32x2& p, float cs, float sn) {
+                    float u, w;
+                    unpack_f32x2(p, &u, &w);
+                    p = ffma2(pack_f32x2(w, u), pack_f32x2(-sn, sn), mul2(p, pack_f32x2(cs, cs)));
+                };
 #pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    if (pa + i < a.R) {
-                        const float2 t = turn[(pa + i) / 2];
-                        const float p = x[i], q = x[i + 1];
-                        x[i] = p * t.x - q * t.y;
-                        x[i + 1] = p * t.y + q * t.x;
-                    }
-                    if (pb + i < a.R) {
-                        const float2 t = turn[(pb + i) / 2];
-                        const float p = y[i], q = y[i + 1];
-                        y[i] = p * t.x - q * t.y;
-                        y[i + 1] = p * t.y + q * t.x;
-                    }
+                for (int i = 0; i < H; ++i) {
+                    if (turns_a) rotate(x[i], ca[i], sa[i]);
+                    if (turns_b) rotate(y[i], cb[i], sb[i]);
                 }
-            } else if (pa < half) {
+            } else if (turns_a) {
+                const f32x2 minus = pack_f32x2(-1.0f, -1.0f);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 t = turn[pa + i];
-                    const float p = x[i], q = y[i];
-                    x[i] = p * t.x - q * t.y;
-                    y[i] = p * t.y + q * t.x;
+                for (int i = 0; i < H; ++i) {
+                    const f32x2 c = reinterpret_cast<const f32x2*>(ca)[i], t = reinterpret_cast<const f32x2*>(sa)[i];
+                    const f32x2 u = ffma2(mul2(y[i], t), minus, mul2(x[i], c));
+                    y[i] = ffma2(y[i], c, mul2(x[i], t));
+                    x[i] = u;
                 }
             }
         }
-        store4(out + pa, x);
-        store4(out + pb, y);
+        store_halves<P>(out + pa, x);
+        store_halves<P>(out + pb, y);
     }
     // a decode kernel behind this one reads its queries before it waits for it
     __threadfence();
+}
+
+template <int D, typename T, int P, bool NEIGHBOURS>
+static void launch_rotate(const RotateArgs& a, cudaStream_t s) {
+        constexpr int kTokens = D == 64 ? 8 : 4;
+    const dim3 block(kRotateThreads);
+    if (a.n <= 512) (void)launch_pdl(rotate_kernel<D, T, P, 1, NEIGHBOURS>, dim3((unsigned)a.n), block, 0, s, a);
+    else (void)launch_pdl(rotate_kernel<D, T, P, kTokens, NEIGHBOURS>, dim3((unsigned)((a.n + kTokens - 1) / kTokens)), block, 0, s, a);
+}
+template <int D, typename T>
+static void launch_rotate(const RotateArgs& a, cudaStream_t s) {
+    if (a.neighbours) launch_rotate<D, T, 8, true>(a, s);
+    else if (a.R % 16 == 0) launch_rotate<D, T, 8, false>(a, s);
+    else launch_rotate<D, T, 4, false>(a, s);
 }
 
 }  // namespace sa
@@ -184,17 +254,14 @@ extern "C" sa_status sa_rotate_qkv(const sa_config* cfg, const sa_rotary* rot, c
     a.eps = rot->eps;
     a.scale = rot->scale;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    const dim3 grid((unsigned)n), block(kRotateThreads);
-#define CALL(D, T) (void)launch_pdl(rotate_kernel<D, T>, grid, block, 0, s, a)
     if (p.d == 64) {
-        if (rot->dtype == SA_F16) CALL(64, __half);
-        else if (rot->dtype == SA_BF16) CALL(64, __nv_bfloat16);
-        else CALL(64, float);
+        if (rot->dtype == SA_F16) launch_rotate<64, __half>(a, s);
+        else if (rot->dtype == SA_BF16) launch_rotate<64, __nv_bfloat16>(a, s);
+        else launch_rotate<64, float>(a, s);
     } else {
-        if (rot->dtype == SA_F16) CALL(128, __half);
-        else if (rot->dtype == SA_BF16) CALL(128, __nv_bfloat16);
-        else CALL(128, float);
+        if (rot->dtype == SA_F16) launch_rotate<128, __half>(a, s);
+        else if (rot->dtype == SA_BF16) launch_rotate<128, __nv_bfloat16>(a, s);
+        else launch_rotate<128, float>(a, s);
     }
-#undef CALL
     return cudaGetLastError() == cudaSuccess ? SA_OK : SA_ERR_CUDA;
 }
