@@ -269,65 +269,6 @@ SA_D void fill_values(uint8_t* half, const CacheArgs& a, int t, const uint4* src
     *reinterpret_cast<uint16_t*>(half + a.meta_off + (size_t)t * 4 + 2) = (uint16_t)(g & 0xff);
 }
 
-// 4-bit cache.  Keys: lane = token, as above.  Values: the lane's codes of 32 channels, 8 to a word, change places with those of the
-// seven tokens with which it shares bytes and words (fp4_transpose), and the warp's 16-byte stores are 512 contiguous bytes.
-// n: tokens of the tile that are written; the nibbles and scales of the others stay.
-template <int D, bool HAD>
-SA_D void fill_keys_fp4(uint8_t* half, int t, const uint4* src) {
-    VecRow<D, HAD> row(src, t);
-#pragma unroll(HAD ? D / 64 : 1)
-    for (int h = 0; h < D / 64; ++h) {
-        uint32_t w[2][4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            uint32_t x[8];
-            row.get(8 * h + 2 * b, x);
-            row.get(8 * h + 2 * b + 1, x + 4);
-            w[0][b] = fp4_block(x, &w[1][b], half + fp4_key_scale(D, t, 64 * h + 16 * b));
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            *reinterpret_cast<uint4*>(half + ((2 * h + k) * kTileTokens + t) * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
-    }
-}
-template <int D>
-SA_D void fill_values_fp4(uint8_t* v, int t, int n, const uint4* src) {
-    VecRow<D, false> row(src, t);
-    const int piece = fp4_piece_of(t), pair = (t & 7) >> 1;
-    // of the bytes [t / 16][t / 8 % 2], two nibbles each, that this pair of tokens has in a word: those of written tokens
-    uint32_t written = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) written |= (16 * (i >> 2) + 8 * (i >> 1 & 1) + 2 * pair + (i & 1) < n ? 0xfu : 0u) << (4 * i);
-#pragma unroll 1
-    for (int p = 0; p < D / 32; ++p) {
-        uint32_t w[2][2];                                      // [channel / 16 % 2][channel / 8 % 2]
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            uint32_t x[8];
-            row.get(4 * p + 2 * m, x);
-            row.get(4 * p + 2 * m + 1, x + 4);
-            w[m][0] = fp4_block(x, &w[m][1], t < n ? v + fp4_value_scale(D, t, 32 * p + 16 * m) : nullptr);
-        }
-        uint32_t out[4], mask[4];
-#pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const uint32_t a = fp4_transpose(w[m][0], t), b = fp4_transpose(w[m][1], t);
-            out[2 * m] = __byte_perm(a, b, 0x5140);
-            out[2 * m + 1] = __byte_perm(a, b, 0x7362);
-            mask[2 * m] = __byte_perm(written, 0u, 0x1100);
-            mask[2 * m + 1] = __byte_perm(written, 0u, 0x3322);
-        }
-        uint4* at = reinterpret_cast<uint4*>(v + p * 512 + piece * 64 + pair * 16);
-        if (n < kTileTokens) {
-            const uint4 old = *at;
-            const uint32_t o[4] = {old.x, old.y, old.z, old.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) out[i] = (out[i] & mask[i]) | (o[i] & ~mask[i]);
-        }
-        *at = make_uint4(out[0], out[1], out[2], out[3]);
-    }
-}
-
 template <int D, int MODE, bool HAD>                          // HAD on its own: the rotation needs twice the registers
 __global__ void __launch_bounds__(128) fill_kernel(CacheArgs a, const uint16_t* __restrict__ Kin, const uint16_t* __restrict__ Vin,
                                                    const __grid_constant__ FillSeqs seqs) {
@@ -347,38 +288,35 @@ __global__ void __launch_bounds__(128) fill_kernel(CacheArgs a, const uint16_t* 
     uint8_t* block = page_block(a, seqs.b0 + i, t / kPageTokens, head);
     if (!block) return;
     uint8_t* half = block + (size_t)((t % kPageTokens) >> 5) * (a.page_bytes >> 1);
-    // the tile's rows, a 16-byte chunk per lane: whole 128-byte lines per load
-    constexpr int C = D / 8, R = 32 / C;
-    __shared__ uint4 buffers[4][32 * C];
-    uint4* src = buffers[threadIdx.x >> 5];
-    const int n = seqs.len[i] - t, ch = lane % C;
-    const uint4* in = reinterpret_cast<const uint4*>(((rest & 1) ? Vin : Kin) + ((size_t)(seqs.row0[i] + t) * a.Hkv + head) * D) + ch;
-    const size_t pitch = (size_t)a.Hkv * C;
-    uint4 v[C];
-#pragma unroll
-    for (int k = 0; k < C; ++k)
-        if (k * R + lane / C < n) v[k] = __ldg(in + (size_t)(k * R + lane / C) * pitch);
-#pragma unroll
-    for (int k = 0; k < C; ++k) {
-        const int row = k * R + lane / C;
-        if (row < n) src[row * C + (ch ^ (row & 7))] = v[k];
-    }
-    __syncwarp();
-    if constexpr (MODE == 33)
-        if (rest & 1) {                                                       // (all lanes: they exchange codes)
-            fill_values_fp4<D>(half + a.v_off, lane, n, src);
-            return;
-        }
-    if (lane >= n) return;
-    if constexpr (MODE == 33) {
-        fill_keys_fp4<D, HAD>(half, lane, src);
-    } else if constexpr (MODE == 16) {                                               // unquantised: 16-byte chunks of 8 elements
-        uint8_t* dst = half + ((rest & 1) ? a.v_off : a.kcode_off);
-#pragma unroll
-        for (int k = 0; k < D / 8; ++k) *reinterpret_cast<uint4*>(dst + (size_t)(k * kTileTokens + lane) * 16) = src[lane * C + (k ^ (lane & 7))];
+    if constexpr (MODE == 33) {                                               // 4 bits: a lane has a block of 16 channels (sa_fp4.cuh)
+        fp4_fill<D, HAD>(half, a.v_off, rest & 1, ((rest & 1) ? Vin : Kin) + ((size_t)(seqs.row0[i] + t) * a.Hkv + head) * D, (size_t)a.Hkv * D, min(seqs.len[i] - t, kTileTokens), lane);
     } else {
-        if (rest & 1) fill_values<D>(half, a, lane, src);
-        else fill_keys<D, MODE, HAD>(half, a, lane, src);
+        // the tile's rows, a 16-byte chunk per lane: whole 128-byte lines per load
+        constexpr int C = D / 8, R = 32 / C;
+        __shared__ uint4 buffers[4][32 * C];
+        uint4* src = buffers[threadIdx.x >> 5];
+        const int n = seqs.len[i] - t, ch = lane % C;
+        const uint4* in = reinterpret_cast<const uint4*>(((rest & 1) ? Vin : Kin) + ((size_t)(seqs.row0[i] + t) * a.Hkv + head) * D) + ch;
+        const size_t pitch = (size_t)a.Hkv * C;
+        uint4 v[C];
+#pragma unroll
+        for (int k = 0; k < C; ++k)
+            if (k * R + lane / C < n) v[k] = __ldg(in + (size_t)(k * R + lane / C) * pitch);
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+            const int row = k * R + lane / C;
+            if (row < n) src[row * C + (ch ^ (row & 7))] = v[k];
+        }
+        __syncwarp();
+        if (lane >= n) return;
+        if constexpr (MODE == 16) {                                               // unquantised: 16-byte chunks of 8 elements
+            uint8_t* dst = half + ((rest & 1) ? a.v_off : a.kcode_off);
+#pragma unroll
+            for (int k = 0; k < D / 8; ++k) *reinterpret_cast<uint4*>(dst + (size_t)(k * kTileTokens + lane) * 16) = src[lane * C + (k ^ (lane & 7))];
+        } else {
+            if (rest & 1) fill_values<D>(half, a, lane, src);
+            else fill_keys<D, MODE, HAD>(half, a, lane, src);
+        }
     }
 }
 

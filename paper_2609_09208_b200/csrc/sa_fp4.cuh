@@ -39,13 +39,15 @@ SA_D uint32_t fp4_scale_byte(uint32_t amax) {
     return min(b, kFp4ScaleMost);
 }
 SA_D float fp4_scale(uint32_t byte) { return half_bits_to_float(byte << 7); }
-// Codes of 8 channels (pairs of binary16), the first in the lowest nibble.
+// Codes of 8 channels (pairs of binary16), the first in the lowest nibble.  The quotients as fp4_quotient's, two at a time.
 SA_D uint32_t fp4_codes(const uint32_t (&x)[4], float s, float inv) {
     float q[8];
+    const f32x2 minus = pack_f32x2(-s, -s), i2 = pack_f32x2(inv, inv);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        q[2 * i] = fp4_quotient(half_bits_to_float(x[i] & 0xffffu), s, inv);
-        q[2 * i + 1] = fp4_quotient(half_bits_to_float(x[i] >> 16), s, inv);
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[i]));
+        const f32x2 v = pack_f32x2(f.x, f.y), r = mul2(v, i2);
+        unpack_f32x2(ffma2(ffma2(r, minus, v), i2, r), &q[2 * i], &q[2 * i + 1]);
     }
     uint32_t w;
     asm("{.reg .b8 a, b, c, d;\n\t"
@@ -55,17 +57,17 @@ SA_D uint32_t fp4_codes(const uint32_t (&x)[4], float s, float inv) {
         : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
     return w;
 }
-// A block of 16 channels (pairs of binary16): codes of the first 8, and of the others to `second`; its scale byte to `scale` (unless null).
-SA_D uint32_t fp4_block(const uint32_t (&x)[8], uint32_t* second, uint8_t* scale) {
+// A block of 16 channels (pairs of binary16): codes of 8 and 8 channels; returns its scale byte.
+SA_D uint32_t fp4_block(const uint32_t (&x)[8], uint32_t (&w)[2]) {
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = __vmaxu2(top, x[i] & 0x7fff7fffu);       // two magnitudes at a time; they order like their bits
     const uint32_t b = fp4_scale_byte(max(top & 0xffffu, top >> 16));
     const float s = fp4_scale(b), inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
-    if (scale) *scale = (uint8_t)b;
     const uint32_t lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
-    *second = fp4_codes(hi, s, inv);
-    return fp4_codes(lo, s, inv);
+    w[0] = fp4_codes(lo, s, inv);
+    w[1] = fp4_codes(hi, s, inv);
+    return b;
 }
 // The 8 codes of a word as pairs of binary16.
 SA_D void fp4_to_half2(uint32_t w, uint32_t (&h)[4]) {
@@ -148,17 +150,226 @@ SA_D void write_token_fp4(uint8_t* half, size_t v_off, bool hadamard, int t, int
     if (m % 16 == 0) v[fp4_value_scale(D, t, m)] = (uint8_t)scale;
 }
 
-// The 8 x 8 nibbles that the lanes t, t ^ 1, t ^ 8, t ^ 16, ... hold in a word each, transposed: nibble i of the lane whose bits
-// 0, 3, 4 are the bits of j goes to nibble j of the lane of i.
-SA_D uint32_t fp4_transpose(uint32_t w, int lane) {
-    uint32_t p = __shfl_xor_sync(0xffffffffu, w, 1);
-    w = (lane & 1) ? (w & 0xf0f0f0f0u) | ((p >> 4) & 0x0f0f0f0fu) : (w & 0x0f0f0f0fu) | ((p << 4) & 0xf0f0f0f0u);
-    p = __shfl_xor_sync(0xffffffffu, w, 8);
-    w = __byte_perm(w, p, (lane & 8) ? 0x3715u : 0x6240u);
-    p = __shfl_xor_sync(0xffffffffu, w, 16);
-    return __byte_perm(w, p, (lane & 16) ? 0x3276u : 0x5410u);
+// Half a page at once, keys or values of one head, by a warp.  A lane has a block of 16 channels, LPV lanes a vector, and the
+// tokens t8, t8 + 8, t8 + 16, t8 + 24: whole rows are loaded and stored without shared memory, a lane's four key scales are one word of the page.
+template <int D>
+struct Fp4Half {
+    static constexpr int LPV = D / 16, TPW = 32 / LPV, PARTS = 8 / TPW;      // lanes of a vector, tokens at a time, times to come to all of 8
+    int blk, t8, lane;
+    SA_D Fp4Half(int lane_, int part) : blk(lane_ % LPV), t8(part * TPW + lane_ / LPV), lane(lane_) {}
+    SA_D uint8_t* key_words(uint8_t* half, int t) const { return half + (2 * (blk / 4)) * 512 + t * 16 + blk % 4 * 4; }     // + 512: the other 8 channels
+    SA_D uint8_t* key_scales(uint8_t* half) const { return half + fp4_key_scale(D, t8, 16 * blk); }                          // of tokens t8 + 8 k
+    SA_D uint8_t* value_words(uint8_t* v, int g) const { return v + blk / 2 * 512 + (4 * (t8 & 1) + g) * 64 + (t8 >> 1) * 16 + blk % 2 * 8; }
+    SA_D uint8_t* value_scales(uint8_t* v) const { return v + 16 * D + blk / 2 * 64 + (t8 >> 1) * 16 + blk % 2 * 8; }
+
+    // Walsh-Hadamard transform of the vectors, in the order of hadamard_warp, without its rounding.
+    SA_D void rotate(float (&x)[16]) const {
+#pragma unroll
+        for (int h = 1; h < 16; h <<= 1)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if ((i & h) == 0) {
+                    const float a = x[i], b = x[i + h];
+                    x[i] = __fadd_rn(a, b);
+                    x[i + h] = __fsub_rn(a, b);
+                }
+#pragma unroll
+        for (int h = 1; h < LPV; h <<= 1)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float o = __shfl_xor_sync(0xffffffffu, x[i], h);
+                x[i] = (lane & h) ? __fsub_rn(o, x[i]) : __fadd_rn(x[i], o);
+            }
+        const float scale = (D == 64) ? 0.125f : 0.088388346f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = __fmul_rn(x[i], scale);
+    }
+    SA_D void rotate(uint32_t (&h)[8]) const {                               // ... of binary16, rounded to it
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+            x[2 * i] = f.x;
+            x[2 * i + 1] = f.y;
+        }
+        rotate(x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const __half2 v = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+            h[i] = *reinterpret_cast<const uint32_t*>(&v);
+        }
+    }
+    // Codes of the lane's values w[k][channel / 8 % 2] (8 channels c % 8 in a word) -> bytes of pairs of tokens, out[g][t / 16] for the channels c % 8 =
+    // 4 (t8 & 1) + g: the lanes of tokens t and t + 1 exchange halves of their words.
+    SA_D void pair_tokens(const uint32_t (&w)[4][2], uint32_t (&out)[4][2]) const {
+        const bool odd_token = t8 & 1;
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t mine = __byte_perm(w[k][0], w[k][1], odd_token ? 0x7632u : 0x5410u);
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, __byte_perm(w[k][0], w[k][1], odd_token ? 0x5410u : 0x7632u), LPV);
+            const uint32_t even = odd_token ? other : mine, odd = odd_token ? mine : other;
+            lo[k] = (even & 0x0f0f0f0fu) | ((odd << 4) & 0xf0f0f0f0u);       // channels g = 0, 2 of either half of the block
+            hi[k] = ((even >> 4) & 0x0f0f0f0fu) | (odd & 0xf0f0f0f0u);       // g = 1, 3
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            out[0][k] = __byte_perm(lo[2 * k], lo[2 * k + 1], 0x6420);
+            out[2][k] = __byte_perm(lo[2 * k], lo[2 * k + 1], 0x7531);
+            out[1][k] = __byte_perm(hi[2 * k], hi[2 * k + 1], 0x6420);
+            out[3][k] = __byte_perm(hi[2 * k], hi[2 * k + 1], 0x7531);
+        }
+    }
+    SA_D void part_tokens(const uint32_t (&in)[4][2], uint32_t (&w)[4][2]) const {         // the way back
+        const bool odd_token = t8 & 1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t sel = k % 2 ? 0x7362u : 0x5140u;
+            const uint32_t lo = __byte_perm(in[0][k / 2], in[2][k / 2], sel), hi = __byte_perm(in[1][k / 2], in[3][k / 2], sel);
+            const uint32_t even = (lo & 0x0f0f0f0fu) | ((hi << 4) & 0xf0f0f0f0u), odd = ((lo >> 4) & 0x0f0f0f0fu) | (hi & 0xf0f0f0f0u);
+            const uint32_t mine = odd_token ? odd : even, other = __shfl_xor_sync(0xffffffffu, odd_token ? even : odd, LPV);
+            const uint32_t low = odd_token ? other : mine, high = odd_token ? mine : other;
+            w[k][0] = __byte_perm(low, high, 0x5410);
+            w[k][1] = __byte_perm(low, high, 0x7632);
+        }
+    }
+    // Which nibbles of out[.][k] are tokens below n, which bytes of the scale words.
+    SA_D uint32_t value_mask(int k, int n) const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                                        // (k: t / 16; i: t / 8 % 2 and t % 2)
+            const int t = 16 * k + 8 * (i >> 1) + (t8 & ~1) + (i & 1);
+            if (t < n) m |= (i & 1 ? 0xf0f0u : 0x0f0fu) << (16 * (i >> 1));
+        }
+        return m;
+    }
+    SA_D static void store_masked(uint8_t* at, uint32_t x, uint32_t mask) {
+        uint32_t* p = reinterpret_cast<uint32_t*>(at);
+        if (mask) *p = mask == 0xffffffffu ? x : (x & mask) | (*p & ~mask);
+    }
+};
+// The tile's first n tokens of K or V (rows of `pitch` elements) into the half page at `half`, whose value codes start at v_off.  What
+// belongs to other tokens stays as it is.
+template <int D, bool HAD>
+SA_D void fp4_fill(uint8_t* half, size_t v_off, bool values, const uint16_t* rows, size_t pitch, int n, int lane) {
+    using F = Fp4Half<D>;
+    uint4 in[F::PARTS][4][2];
+#pragma unroll
+    for (int part = 0; part < F::PARTS; ++part) {
+        const F f(lane, part);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint4* p = reinterpret_cast<const uint4*>(rows + (size_t)(8 * k + f.t8) * pitch + 16 * f.blk);
+            in[part][k][0] = in[part][k][1] = make_uint4(0u, 0u, 0u, 0u);
+            if (8 * k + f.t8 < n) {
+                in[part][k][0] = __ldg(p);
+                in[part][k][1] = __ldg(p + 1);
+            }
+        }
+    }
+#pragma unroll
+    for (int part = 0; part < F::PARTS; ++part) {
+        const F f(lane, part);
+        uint32_t w[4][2], scale[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint4 a = in[part][k][0], b = in[part][k][1];
+            uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+            if constexpr (HAD)
+                if (!values) f.rotate(x);
+            scale[k] = fp4_block(x, w[k]);
+        }
+        if (!values) {
+            uint32_t mask = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (8 * k + f.t8 < n) {
+                    uint8_t* at = f.key_words(half, 8 * k + f.t8);
+                    *reinterpret_cast<uint32_t*>(at) = w[k][0];
+                    *reinterpret_cast<uint32_t*>(at + 512) = w[k][1];
+                    mask |= 0xffu << (8 * k);
+                }
+            F::store_masked(f.key_scales(half), scale[0] | scale[1] << 8 | scale[2] << 16 | scale[3] << 24, mask);
+        } else {
+            uint8_t* v = half + v_off;
+            uint32_t out[4][2];
+            f.pair_tokens(w, out);
+            const uint32_t m0 = n < kTileTokens ? f.value_mask(0, n) : 0xffffffffu, m1 = n < kTileTokens ? f.value_mask(1, n) : 0xffffffffu;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                if (n == kTileTokens) *reinterpret_cast<uint2*>(f.value_words(v, g)) = make_uint2(out[g][0], out[g][1]);
+                else {
+                    F::store_masked(f.value_words(v, g), out[g][0], m0);
+                    F::store_masked(f.value_words(v, g) + 4, out[g][1], m1);
+                }
+            }
+            // scales: [t / 16][t % 2][t / 8 % 2]; the even token's lane stores those of the first 16 tokens, the odd one's the others
+            const bool odd = f.t8 & 1;
+            const uint32_t s0 = scale[0] | scale[1] << 8, s1 = scale[2] | scale[3] << 8;
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? s0 : s1, F::LPV);
+            uint32_t mask = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)                                      // byte i: t % 2 = i / 2, t / 8 % 2 = i % 2
+                if (16 * odd + 8 * (i & 1) + (f.t8 & ~1) + (i >> 1) < n) mask |= 0xffu << (8 * i);
+            F::store_masked(f.value_scales(v) + 4 * odd, odd ? other | s1 << 16 : s0 | other << 16, mask);
+        }
+    }
 }
-// The lane's number among the eight that share a piece of 16 bytes of value codes: also the channel (mod 8) whose piece it moves.
-SA_D int fp4_piece_of(int lane) { return (lane & 1) | (lane >> 2 & 2) | (lane >> 2 & 4); }
+// The way back: tokens first .. end - 1 of the half page to their rows (rows: that of token 0, from which only these are touched).
+template <int D, bool HAD>
+SA_D void fp4_read(const uint8_t* half_, size_t v_off, bool values, uint16_t* rows, int64_t pitch, int first, int end, int lane) {
+    using F = Fp4Half<D>;
+    uint8_t* half = const_cast<uint8_t*>(half_);
+    uint32_t w[F::PARTS][4][2], scales[F::PARTS][2];
+#pragma unroll
+    for (int part = 0; part < F::PARTS; ++part) {
+        const F f(lane, part);
+        if (!values) {
+            scales[part][0] = *reinterpret_cast<const uint32_t*>(f.key_scales(half));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                w[part][k][0] = *reinterpret_cast<const uint32_t*>(f.key_words(half, 8 * k + f.t8));
+                w[part][k][1] = *reinterpret_cast<const uint32_t*>(f.key_words(half, 8 * k + f.t8) + 512);
+            }
+        } else {
+            uint8_t* v = half + v_off;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) scales[part][k] = *reinterpret_cast<const uint16_t*>(f.value_scales(v) + 4 * k + 2 * (f.t8 & 1));
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const uint2 x = *reinterpret_cast<const uint2*>(f.value_words(v, g));
+                w[part][g][0] = x.x;
+                w[part][g][1] = x.y;
+            }
+        }
+    }
+#pragma unroll
+    for (int part = 0; part < F::PARTS; ++part) {
+        const F f(lane, part);
+        uint32_t c[4][2];
+        if (values) f.part_tokens(w[part], c);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t b = values ? scales[part][k / 2] >> (8 * (k & 1)) & 0xffu : scales[part][0] >> (8 * k) & 0xffu;
+            const uint32_t s = b << 7 | b << 23;
+            uint32_t x[8], lo[4], hi[4];
+            fp4_to_half2(values ? c[k][0] : w[part][k][0], lo);
+            fp4_to_half2(values ? c[k][1] : w[part][k][1], hi);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[i] = mul_half2(lo[i], s);
+                x[4 + i] = mul_half2(hi[i], s);
+            }
+            if constexpr (HAD)
+                if (!values) f.rotate(x);
+            const int t = 8 * k + f.t8;
+            if (t >= first && t < end) {
+                uint4* out = reinterpret_cast<uint4*>(rows + t * pitch + 16 * f.blk);
+                out[0] = make_uint4(x[0], x[1], x[2], x[3]);
+                out[1] = make_uint4(x[4], x[5], x[6], x[7]);
+            }
+        }
+    }
+}
 
 }  // namespace sa

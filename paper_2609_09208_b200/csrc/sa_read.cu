@@ -43,9 +43,9 @@ struct KeyReader {
     size_t plane_off;
     int t;
     float s;                              // scale of the vector
-    uint4 w, w2;                          // the chunk at hand (4 bits: two)
+    uint4 w;                              // the chunk at hand
     SA_D KeyReader(const uint8_t* half_, const CacheArgs& a, int t_) : half(half_), plane_off(a.plane_off), t(t_), s(1.0f) {
-        if constexpr (MODE != 16 && MODE != 33) s = half_bits_to_float(*reinterpret_cast<const uint16_t*>(half + a.meta_off + t * 4));
+        if constexpr (MODE != 16) s = half_bits_to_float(*reinterpret_cast<const uint16_t*>(half + a.meta_off + t * 4));
     }
     SA_D uint4 chunk(int k) const { return __ldg(reinterpret_cast<const uint4*>(half + ((size_t)k * kTileTokens + t) * 16)); }
     SA_D void get(int c, float (&x)[8]) {
@@ -54,18 +54,6 @@ struct KeyReader {
             const uint32_t h[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = half_bits_to_float((h[i / 2] >> (16 * (i & 1))) & 0xffffu);
-        } else if constexpr (MODE == 33) {
-            if (c % 8 == 0) {
-                w = chunk(c / 4);
-                w2 = chunk(c / 4 + 1);
-            }
-            const uint4& v = c % 2 ? w2 : w;
-            const int i = c % 8 / 2;
-            uint32_t h[4];
-            fp4_to_half2(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w, h);
-            const float f = fp4_scale(half[fp4_key_scale(D, t, 8 * c)]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = half_bits_to_float((h[i / 2] >> (16 * (i & 1))) & 0xffffu) * f;
         } else if constexpr (MODE < 8 || MODE == 32) {                            // a byte a channel
             if (c % 2 == 0) w = chunk(c / 2);
             const uint32_t h[2] = {c % 2 ? w.z : w.x, c % 2 ? w.w : w.y};
@@ -131,23 +119,6 @@ SA_D void read_values(const uint8_t* half, const CacheArgs& a, int t, uint4* row
     if constexpr (MODE == 16) {
 #pragma unroll
         for (int c = 0; c < D / 8; ++c) row[c ^ (t & 7)] = __ldg(reinterpret_cast<const uint4*>(v + ((size_t)c * kTileTokens + t) * 16));
-    } else if constexpr (MODE == 33) {                                            // the way back of fill_values_fp4
-        const int piece = fp4_piece_of(t), pair = (t & 7) >> 1;
-#pragma unroll
-        for (int p = 0; p < D / 32; ++p) {
-            const uint4 in = __ldg(reinterpret_cast<const uint4*>(v + p * 512 + piece * 64 + pair * 16));
-            const uint32_t w[4] = {in.x, in.y, in.z, in.w};
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const uint32_t s = fp4_scale2<0>(v[fp4_value_scale(D, t, 32 * p + 16 * m)], 1u);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    uint32_t h[4];
-                    fp4_to_half2(fp4_transpose(__byte_perm(w[2 * m], w[2 * m + 1], e ? 0x7531 : 0x6420), t), h);
-                    row[(4 * p + 2 * m + e) ^ (t & 7)] = make_uint4(mul_half2(h[0], s), mul_half2(h[1], s), mul_half2(h[2], s), mul_half2(h[3], s));
-                }
-            }
-        }
     } else {
         const float f = pow2i(-(int)(int8_t)half[a.meta_off + t * 4 + 2]);
 #pragma unroll 2
@@ -183,16 +154,22 @@ __global__ void __launch_bounds__(128) read_kernel(CacheArgs a, uint16_t* __rest
     pdl_wait();                                                                   // earlier kernels may still write this cache
     const uint8_t* block = page_block(a, seqs.b0 + i, t0 / kPageTokens, head);
     constexpr int C = D / 8, R = 32 / C;
-    __shared__ uint4 buffers[4][32 * C];
+    const int64_t row0 = seqs.row0[i] + t0 - start;                               // (of the half page's first token)
+    if constexpr (MODE == 33)                                                     // 4 bits: a lane has a block of 16 channels (sa_fp4.cuh)
+        if (block) {
+            fp4_read<D, HAD>(block + (size_t)((t0 % kPageTokens) >> 5) * (a.page_bytes >> 1), a.v_off, values,
+                             (values ? Vout : Kout) + (row0 * a.Hkv + head) * D, (int64_t)a.Hkv * D, first, end, lane);
+            return;
+        }
+    __shared__ uint4 buffers[4][MODE == 33 ? 1 : 32 * C];
     uint4* rows = buffers[threadIdx.x >> 5];
-    if (block) {
+    if (MODE != 33 && block) {
         const uint8_t* half = block + (size_t)((t0 % kPageTokens) >> 5) * (a.page_bytes >> 1);
         if (values) read_values<D, MODE>(half, a, lane, rows + lane * C);
         else read_keys<D, MODE, HAD>(half, a, lane, rows + lane * C);
     }
     __syncwarp();
     const int ch = lane % C;
-    const int64_t row0 = seqs.row0[i] + t0 - start;                               // (of the half page's first token)
     uint4* out = reinterpret_cast<uint4*>(values ? Vout : Kout) + head * C + ch;
 #pragma unroll
     for (int k = 0; k < C; ++k) {
