@@ -4,6 +4,7 @@
 #include "sa_common.cuh"
 #include "sa_cache_write.cuh"
 #include "sa_quant.cuh"
+#include <type_traits>
 
 namespace sa {
 
@@ -270,11 +271,12 @@ SA_D void fill_values(uint8_t* half, const CacheArgs& a, int t, const uint4* src
 }
 
 template <int D, int MODE, bool HAD>                          // HAD on its own: the rotation needs twice the registers
-__global__ void __launch_bounds__(128) fill_kernel(CacheArgs a, const uint16_t* __restrict__ Kin, const uint16_t* __restrict__ Vin,
+__global__ void __launch_bounds__(128, MODE == 33 ? (D == 128 ? 6 : 8) : 1) fill_kernel(CacheArgs a, const uint16_t* __restrict__ Kin, const uint16_t* __restrict__ Vin,
                                                    const __grid_constant__ FillSeqs seqs) {
     const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);        // (tile, head, keys or values)
-    const int tile = (int)(unit / (2 * a.Hkv)), rest = (int)(unit % (2 * a.Hkv));
+    using Unit = std::conditional_t<MODE == 33, uint32_t, int64_t>;           // (a 64-bit division is a long routine; 4 bits: the host sees to it that 32 do)
+    const Unit unit = (Unit)blockIdx.x * 4 + (threadIdx.x >> 5);              // (tile, head, keys or values)
+    const int tile = (int)(unit / (Unit)(2 * a.Hkv)), rest = (int)(unit % (Unit)(2 * a.Hkv));
     const int head = rest >> 1;
     if (tile >= seqs.tiles[seqs.n]) return;
     int i = 0;                                                                // the sequence: the last one that starts at or before the tile
@@ -521,7 +523,7 @@ sa_status sa_fill_kv(const sa_config* cfg, const sa_cache* cache, const uint16_t
         }
         const int64_t units = (int64_t)seqs.tiles[seqs.n] * 2 * a.Hkv;
         if (units == 0) continue;
-        if ((units + 3) / 4 > 0x7fffffffLL) return SA_ERR_CAPACITY;
+        if ((units + 3) / 4 > (p.fp4 ? 0x3fffffffLL : 0x7fffffffLL)) return SA_ERR_CAPACITY;
         const unsigned grid = (unsigned)((units + 3) / 4);
 #define CALL(D, M)                                                                               \
     if (M != 16 && a.hadamard) (void)launch_pdl(fill_kernel<D, M, M != 16>, dim3(grid), dim3(128), 0, s, a, K, V, seqs);        \

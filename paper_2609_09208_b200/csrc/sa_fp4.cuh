@@ -30,6 +30,12 @@ SA_HD float fp4_quotient(float x, float s, float inv) {
     return fmaf(fmaf(-r, s, x), inv, r);
 #endif
 }
+// 1 / s within two units in the last place, which the step of fp4_quotient makes good; 0 for 0.
+SA_D float fp4_inverse(float s) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+    return s > 0.0f ? r : 0.0f;
+}
 // Scale byte of a block whose largest magnitude has the binary16 bits `amax`.
 SA_D uint32_t fp4_scale_byte(uint32_t amax) {
     const float t = fp4_quotient(half_bits_to_float(amax), 6.0f, 1.0f / 6.0f);
@@ -59,11 +65,11 @@ SA_D uint32_t fp4_codes(const uint32_t (&x)[4], float s, float inv) {
 }
 // A block of 16 channels (pairs of binary16): codes of 8 and 8 channels; returns its scale byte.
 SA_D uint32_t fp4_block(const uint32_t (&x)[8], uint32_t (&w)[2]) {
-    uint32_t top = 0;
+    uint32_t top = x[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = __vmaxu2(top, x[i] & 0x7fff7fffu);       // two magnitudes at a time; they order like their bits
-    const uint32_t b = fp4_scale_byte(max(top & 0xffffu, top >> 16));
-    const float s = fp4_scale(b), inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+    for (int i = 1; i < 8; ++i) asm("max.xorsign.abs.f16x2 %0, %0, %1;" : "+r"(top) : "r"(x[i]));      // two magnitudes at a time, with signs that do not matter
+    const uint32_t b = fp4_scale_byte(max(top & 0x7fffu, (top >> 16) & 0x7fffu));
+    const float s = fp4_scale(b), inv = fp4_inverse(s);
     const uint32_t lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};
     w[0] = fp4_codes(lo, s, inv);
     w[1] = fp4_codes(hi, s, inv);
@@ -111,7 +117,7 @@ SA_D uint32_t fp4_encode_vec(const uint32_t (&bits)[EPL], uint8_t (&codes)[EPL /
 #pragma unroll
     for (int o = 1; o < 16 / EPL; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     const uint32_t b = fp4_scale_byte(top);
-    const float s = fp4_scale(b), inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+    const float s = fp4_scale(b), inv = fp4_inverse(s);
     uint32_t x[4] = {};
 #pragma unroll
     for (int i = 0; i < EPL / 2; ++i) x[i] = bits[2 * i] | bits[2 * i + 1] << 16;
@@ -150,6 +156,27 @@ SA_D void write_token_fp4(uint8_t* half, size_t v_off, bool hadamard, int t, int
     if (m % 16 == 0) v[fp4_value_scale(D, t, m)] = (uint8_t)scale;
 }
 
+// 32 bytes of global memory, in one piece where the address allows (wide): rows of 16-byte pieces 32 bytes apart fill every sector in two goes.
+SA_D void load_32_bytes(const void* p, bool wide, uint32_t (&x)[8]) {
+    if (wide) {
+        asm("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+            : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7])
+            : "l"(p));
+    } else {
+        const uint4 a = __ldg(static_cast<const uint4*>(p)), b = __ldg(static_cast<const uint4*>(p) + 1);
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    }
+}
+SA_D void store_32_bytes(void* p, bool wide, const uint32_t (&x)[8]) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7])
+                     : "memory");
+    } else {
+        static_cast<uint4*>(p)[0] = make_uint4(x[0], x[1], x[2], x[3]);
+        static_cast<uint4*>(p)[1] = make_uint4(x[4], x[5], x[6], x[7]);
+    }
+}
+
 // Half a page at once, keys or values of one head, by a warp.  A lane has a block of 16 channels, LPV lanes a vector, and the
 // tokens t8, t8 + 8, t8 + 16, t8 + 24: whole rows are loaded and stored without shared memory, a lane's four key scales are one word of the page.
 template <int D>
@@ -162,40 +189,41 @@ struct Fp4Half {
     SA_D uint8_t* value_words(uint8_t* v, int g) const { return v + blk / 2 * 512 + (4 * (t8 & 1) + g) * 64 + (t8 >> 1) * 16 + blk % 2 * 8; }
     SA_D uint8_t* value_scales(uint8_t* v) const { return v + 16 * D + blk / 2 * 64 + (t8 >> 1) * 16 + blk % 2 * 8; }
 
-    // Walsh-Hadamard transform of the vectors, in the order of hadamard_warp, without its rounding.
-    SA_D void rotate(float (&x)[16]) const {
+    // Walsh-Hadamard rotation of the vectors as hadamard_warp has it (the same sums in the same order), binary16 in and out; pairs of channels packed.
+    SA_D void rotate(uint32_t (&h)[8]) const {
+        f32x2 x[8];
+        const f32x2 minus = pack_f32x2(-1.0f, -1.0f);
 #pragma unroll
-        for (int h = 1; h < 16; h <<= 1)
+        for (int i = 0; i < 8; ++i) {                                        // channels 1 apart
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+            x[i] = pack_f32x2(__fadd_rn(f.x, f.y), __fsub_rn(f.x, f.y));
+        }
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if ((i & h) == 0) {
-                    const float a = x[i], b = x[i + h];
-                    x[i] = __fadd_rn(a, b);
-                    x[i + h] = __fsub_rn(a, b);
+        for (int st = 1; st < 8; st <<= 1)                                   // 2, 4, 8 apart
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if ((i & st) == 0) {
+                    const f32x2 a = x[i], b = x[i + st];
+                    x[i] = add2(a, b);
+                    x[i + st] = ffma2(b, minus, a);                          // (a - b with the one rounding of a difference)
                 }
 #pragma unroll
-        for (int h = 1; h < LPV; h <<= 1)
+        for (int st = 1; st < LPV; st <<= 1) {                               // other lanes
+            const float sign = (lane & st) ? -1.0f : 1.0f;
+            const f32x2 s2 = pack_f32x2(sign, sign);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float o = __shfl_xor_sync(0xffffffffu, x[i], h);
-                x[i] = (lane & h) ? __fsub_rn(o, x[i]) : __fadd_rn(x[i], o);
+            for (int i = 0; i < 8; ++i) {
+                float lo, hi;
+                unpack_f32x2(x[i], &lo, &hi);
+                x[i] = ffma2(x[i], s2, pack_f32x2(__shfl_xor_sync(0xffffffffu, lo, st), __shfl_xor_sync(0xffffffffu, hi, st)));
             }
+        }
         const float scale = (D == 64) ? 0.125f : 0.088388346f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = __fmul_rn(x[i], scale);
-    }
-    SA_D void rotate(uint32_t (&h)[8]) const {                               // ... of binary16, rounded to it
-        float x[16];
-#pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-            x[2 * i] = f.x;
-            x[2 * i + 1] = f.y;
-        }
-        rotate(x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const __half2 v = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+            float lo, hi;
+            unpack_f32x2(mul2(x[i], pack_f32x2(scale, scale)), &lo, &hi);
+            const __half2 v = __floats2half2_rn(lo, hi);
             h[i] = *reinterpret_cast<const uint32_t*>(&v);
         }
     }
@@ -249,70 +277,79 @@ struct Fp4Half {
     }
 };
 // The tile's first n tokens of K or V (rows of `pitch` elements) into the half page at `half`, whose value codes start at v_off.  What
-// belongs to other tokens stays as it is.
+// belongs to other tokens stays as it is.  Keys in a rolled loop, the next token's block under way: unrolled, the code did not fit the instruction
+// caches (20 001 tokens, 8 heads of 128, rotated: 46.7 -> 31.9 us, keys and values).
 template <int D, bool HAD>
 SA_D void fp4_fill(uint8_t* half, size_t v_off, bool values, const uint16_t* rows, size_t pitch, int n, int lane) {
     using F = Fp4Half<D>;
-    uint4 in[F::PARTS][4][2];
+    const bool wide = (reinterpret_cast<uintptr_t>(rows) & 31) == 0;
+    auto load = [&](uint32_t (&x)[8], int t, int blk) {
 #pragma unroll
-    for (int part = 0; part < F::PARTS; ++part) {
-        const F f(lane, part);
+        for (int i = 0; i < 8; ++i) x[i] = 0u;
+        if (t < n) load_32_bytes(rows + (size_t)t * pitch + 16 * blk, wide, x);
+    };
+    if (!values) {
+        uint32_t next[2][8];
+        load(next[0], F(lane, 0).t8, F(lane, 0).blk);
+        load(next[1], F(lane, 0).t8 + 8, F(lane, 0).blk);
+        uint32_t scales = 0, mask = 0;
+#pragma unroll(HAD ? 1 : 4 * F::PARTS)
+        for (int i = 0; i < 4 * F::PARTS; ++i) {
+            const int part = i >> 2, k = i & 3;
+            const F f(lane, part);
+            uint32_t x[8], w[2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint4* p = reinterpret_cast<const uint4*>(rows + (size_t)(8 * k + f.t8) * pitch + 16 * f.blk);
-            in[part][k][0] = in[part][k][1] = make_uint4(0u, 0u, 0u, 0u);
+            for (int e = 0; e < 8; ++e) {
+                x[e] = next[0][e];
+                next[0][e] = next[1][e];
+            }
+            if (i + 2 < 4 * F::PARTS) load(next[1], F(lane, (i + 2) >> 2).t8 + 8 * ((i + 2) & 3), f.blk);
+            if constexpr (HAD) f.rotate(x);
+            scales |= fp4_block(x, w) << (8 * k);
             if (8 * k + f.t8 < n) {
-                in[part][k][0] = __ldg(p);
-                in[part][k][1] = __ldg(p + 1);
+                uint8_t* at = f.key_words(half, 8 * k + f.t8);
+                *reinterpret_cast<uint32_t*>(at) = w[0];
+                *reinterpret_cast<uint32_t*>(at + 512) = w[1];
+                mask |= 0xffu << (8 * k);
+            }
+            if (k == 3) {
+                F::store_masked(f.key_scales(half), scales, mask);
+                scales = mask = 0;
             }
         }
+        return;
     }
-#pragma unroll
+#pragma unroll 1
     for (int part = 0; part < F::PARTS; ++part) {
         const F f(lane, part);
-        uint32_t w[4][2], scale[4];
+        uint32_t in[4][8], w[4][2], scale[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint4 a = in[part][k][0], b = in[part][k][1];
-            uint32_t x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-            if constexpr (HAD)
-                if (!values) f.rotate(x);
-            scale[k] = fp4_block(x, w[k]);
-        }
-        if (!values) {
-            uint32_t mask = 0;
+        for (int k = 0; k < 4; ++k) load(in[k], f.t8 + 8 * k, f.blk);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (8 * k + f.t8 < n) {
-                    uint8_t* at = f.key_words(half, 8 * k + f.t8);
-                    *reinterpret_cast<uint32_t*>(at) = w[k][0];
-                    *reinterpret_cast<uint32_t*>(at + 512) = w[k][1];
-                    mask |= 0xffu << (8 * k);
-                }
-            F::store_masked(f.key_scales(half), scale[0] | scale[1] << 8 | scale[2] << 16 | scale[3] << 24, mask);
+        for (int k = 0; k < 4; ++k) scale[k] = fp4_block(in[k], w[k]);
+        uint8_t* v = half + v_off;
+        uint32_t out[4][2];
+        f.pair_tokens(w, out);
+        if (n == kTileTokens) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) *reinterpret_cast<uint2*>(f.value_words(v, g)) = make_uint2(out[g][0], out[g][1]);
         } else {
-            uint8_t* v = half + v_off;
-            uint32_t out[4][2];
-            f.pair_tokens(w, out);
-            const uint32_t m0 = n < kTileTokens ? f.value_mask(0, n) : 0xffffffffu, m1 = n < kTileTokens ? f.value_mask(1, n) : 0xffffffffu;
+            const uint32_t m0 = f.value_mask(0, n), m1 = f.value_mask(1, n);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                if (n == kTileTokens) *reinterpret_cast<uint2*>(f.value_words(v, g)) = make_uint2(out[g][0], out[g][1]);
-                else {
-                    F::store_masked(f.value_words(v, g), out[g][0], m0);
-                    F::store_masked(f.value_words(v, g) + 4, out[g][1], m1);
-                }
+                F::store_masked(f.value_words(v, g), out[g][0], m0);
+                F::store_masked(f.value_words(v, g) + 4, out[g][1], m1);
             }
-            // scales: [t / 16][t % 2][t / 8 % 2]; the even token's lane stores those of the first 16 tokens, the odd one's the others
-            const bool odd = f.t8 & 1;
-            const uint32_t s0 = scale[0] | scale[1] << 8, s1 = scale[2] | scale[3] << 8;
-            const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? s0 : s1, F::LPV);
-            uint32_t mask = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)                                      // byte i: t % 2 = i / 2, t / 8 % 2 = i % 2
-                if (16 * odd + 8 * (i & 1) + (f.t8 & ~1) + (i >> 1) < n) mask |= 0xffu << (8 * i);
-            F::store_masked(f.value_scales(v) + 4 * odd, odd ? other | s1 << 16 : s0 | other << 16, mask);
         }
+        // scales: [t / 16][t % 2][t / 8 % 2]; the even token's lane stores those of the first 16 tokens, the odd one's the others
+        const bool odd = f.t8 & 1;
+        const uint32_t s0 = scale[0] | scale[1] << 8, s1 = scale[2] | scale[3] << 8;
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? s0 : s1, F::LPV);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)                                          // byte i: t % 2 = i / 2, t / 8 % 2 = i % 2
+            if (16 * odd + 8 * (i & 1) + (f.t8 & ~1) + (i >> 1) < n) mask |= 0xffu << (8 * i);
+        F::store_masked(f.value_scales(v) + 4 * odd, odd ? other | s1 << 16 : s0 | other << 16, mask);
     }
 }
 // The way back: tokens first .. end - 1 of the half page to their rows (rows: that of token 0, from which only these are touched).
@@ -320,55 +357,68 @@ template <int D, bool HAD>
 SA_D void fp4_read(const uint8_t* half_, size_t v_off, bool values, uint16_t* rows, int64_t pitch, int first, int end, int lane) {
     using F = Fp4Half<D>;
     uint8_t* half = const_cast<uint8_t*>(half_);
+    const bool wide = (reinterpret_cast<uintptr_t>(rows) & 31) == 0;
+    auto write = [&](const F& f, int k, uint32_t c0, uint32_t c1, uint32_t b, bool rotated) {
+        const uint32_t s = b << 7 | b << 23;
+        uint32_t x[8], lo[4], hi[4];
+        fp4_to_half2(c0, lo);
+        fp4_to_half2(c1, hi);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = mul_half2(lo[i], s);
+            x[4 + i] = mul_half2(hi[i], s);
+        }
+        if (rotated) f.rotate(x);
+        const int t = 8 * k + f.t8;
+        if (t >= first && t < end) store_32_bytes(rows + t * pitch + 16 * f.blk, wide, x);
+    };
+    if (!values) {
+        uint32_t w[F::PARTS * 4][2], scales[F::PARTS];
+#pragma unroll
+        for (int i = 0; i < 4 * F::PARTS; ++i) {
+            const F f(lane, i >> 2);
+            w[i][0] = *reinterpret_cast<const uint32_t*>(f.key_words(half, 8 * (i & 3) + f.t8));
+            w[i][1] = *reinterpret_cast<const uint32_t*>(f.key_words(half, 8 * (i & 3) + f.t8) + 512);
+        }
+#pragma unroll
+        for (int part = 0; part < F::PARTS; ++part) scales[part] = *reinterpret_cast<const uint32_t*>(F(lane, part).key_scales(half));
+        if constexpr (HAD) {                                                 // rolled: the rotation is long
+#pragma unroll 1
+            for (int i = 0; i < 4 * F::PARTS; ++i) {
+                write(F(lane, i >> 2), i & 3, w[0][0], w[0][1], scales[0] >> (8 * (i & 3)) & 0xffu, true);
+#pragma unroll
+                for (int k = 0; k + 1 < 4 * F::PARTS; ++k) {
+                    w[k][0] = w[k + 1][0];
+                    w[k][1] = w[k + 1][1];
+                }
+                if ((i & 3) == 3) scales[0] = scales[F::PARTS - 1];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4 * F::PARTS; ++i) write(F(lane, i >> 2), i & 3, w[i][0], w[i][1], scales[i >> 2] >> (8 * (i & 3)) & 0xffu, false);
+        }
+        return;
+    }
     uint32_t w[F::PARTS][4][2], scales[F::PARTS][2];
 #pragma unroll
     for (int part = 0; part < F::PARTS; ++part) {
         const F f(lane, part);
-        if (!values) {
-            scales[part][0] = *reinterpret_cast<const uint32_t*>(f.key_scales(half));
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                w[part][k][0] = *reinterpret_cast<const uint32_t*>(f.key_words(half, 8 * k + f.t8));
-                w[part][k][1] = *reinterpret_cast<const uint32_t*>(f.key_words(half, 8 * k + f.t8) + 512);
-            }
-        } else {
-            uint8_t* v = half + v_off;
+        for (int k = 0; k < 2; ++k) scales[part][k] = *reinterpret_cast<const uint16_t*>(f.value_scales(half + v_off) + 4 * k + 2 * (f.t8 & 1));
 #pragma unroll
-            for (int k = 0; k < 2; ++k) scales[part][k] = *reinterpret_cast<const uint16_t*>(f.value_scales(v) + 4 * k + 2 * (f.t8 & 1));
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const uint2 x = *reinterpret_cast<const uint2*>(f.value_words(v, g));
-                w[part][g][0] = x.x;
-                w[part][g][1] = x.y;
-            }
+        for (int g = 0; g < 4; ++g) {
+            const uint2 x = *reinterpret_cast<const uint2*>(f.value_words(half + v_off, g));
+            w[part][g][0] = x.x;
+            w[part][g][1] = x.y;
         }
     }
 #pragma unroll
     for (int part = 0; part < F::PARTS; ++part) {
         const F f(lane, part);
         uint32_t c[4][2];
-        if (values) f.part_tokens(w[part], c);
+        f.part_tokens(w[part], c);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t b = values ? scales[part][k / 2] >> (8 * (k & 1)) & 0xffu : scales[part][0] >> (8 * k) & 0xffu;
-            const uint32_t s = b << 7 | b << 23;
-            uint32_t x[8], lo[4], hi[4];
-            fp4_to_half2(values ? c[k][0] : w[part][k][0], lo);
-            fp4_to_half2(values ? c[k][1] : w[part][k][1], hi);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[i] = mul_half2(lo[i], s);
-                x[4 + i] = mul_half2(hi[i], s);
-            }
-            if constexpr (HAD)
-                if (!values) f.rotate(x);
-            const int t = 8 * k + f.t8;
-            if (t >= first && t < end) {
-                uint4* out = reinterpret_cast<uint4*>(rows + t * pitch + 16 * f.blk);
-                out[0] = make_uint4(x[0], x[1], x[2], x[3]);
-                out[1] = make_uint4(x[4], x[5], x[6], x[7]);
-            }
-        }
+        for (int k = 0; k < 4; ++k) write(f, k, c[k][0], c[k][1], scales[part][k / 2] >> (8 * (k & 1)) & 0xffu, false);
     }
 }
 

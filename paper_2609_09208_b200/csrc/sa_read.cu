@@ -1,6 +1,7 @@
 // sa_read_kv: keys and values of a cache back as binary16 rows.
-#include "sa_common.cuh"
 #include "sa_cache_write.cuh"
+#include "sa_common.cuh"
+#include "sa_score_mma.cuh"
 
 namespace sa {
 
@@ -54,14 +55,29 @@ struct KeyReader {
             const uint32_t h[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = half_bits_to_float((h[i / 2] >> (16 * (i & 1))) & 0xffffu);
-        } else if constexpr (MODE < 8 || MODE == 32) {                            // a byte a channel
+        } else if constexpr (MODE == 32) {                                        // INT8
             if (c % 2 == 0) w = chunk(c / 2);
             const uint32_t h[2] = {c % 2 ? w.z : w.x, c % 2 ? w.w : w.y};
+            const f32x2 s2 = pack_f32x2(s, s), d2 = pack_f32x2(-127.0f, -127.0f), i2 = pack_f32x2(1.0f / 127.0f, 1.0f / 127.0f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t b = (h[i / 4] >> (8 * (i & 3))) & 0xffu;
-                if constexpr (MODE == 32) x[i] = __fdiv_rn((float)(int)(int8_t)b * s, 127.0f);
-                else x[i] = power_of_two(b & 7u, 16u + ((b >> 3) & 15u), b >> 7) * s;
+            for (int i = 0; i < 8; i += 4) {
+                const uint32_t even = int8_to_half2<false>(h[i / 4]), odd = int8_to_half2<true>(h[i / 4]);
+                const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&even)), o = __half22float2(*reinterpret_cast<const __half2*>(&odd));
+                const f32x2 v[2] = {mul2(pack_f32x2(e.x, o.x), s2), mul2(pack_f32x2(e.y, o.y), s2)};       // code times scale: exact
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {                                     // over 127, as good as rounded correctly
+                    const f32x2 q = mul2(v[k], i2);
+                    unpack_f32x2(ffma2(ffma2(q, d2, v[k]), i2, q), &x[i + 2 * k], &x[i + 2 * k + 1]);
+                }
+            }
+        } else if constexpr (MODE < 8) {                                          // a byte a channel: bfloat16 numbers, 2^-120 of the codes'
+            if (c % 2 == 0) w = chunk(c / 2);
+            const uint32_t h[2] = {c % 2 ? w.z : w.x, c % 2 ? w.w : w.y};
+            const f32x2 up = pack_f32x2(0x1p120f, 0x1p120f), s2 = pack_f32x2(s, s);
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const uint32_t p = i & 2 ? byte_codes_to_bf16<2>(h[i / 4], 1u) : byte_codes_to_bf16<0>(h[i / 4], 1u);
+                unpack_f32x2(mul2(mul2(pack_f32x2(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u)), up), s2), &x[i], &x[i + 1]);
             }
         } else {                                                                  // nibbles, and K planes of mantissa bits
             constexpr int K = MODE - 8;
@@ -120,15 +136,20 @@ SA_D void read_values(const uint8_t* half, const CacheArgs& a, int t, uint4* row
 #pragma unroll
         for (int c = 0; c < D / 8; ++c) row[c ^ (t & 7)] = __ldg(reinterpret_cast<const uint4*>(v + ((size_t)c * kTileTokens + t) * 16));
     } else {
-        const float f = pow2i(-(int)(int8_t)half[a.meta_off + t * 4 + 2]);
+        // times 2^-g in two exact steps: the first keeps clear of the subnormal numbers, the second rounds where the value is one
+        const int g = (int)(int8_t)half[a.meta_off + t * 4 + 2], g1 = max(-10, min(g, 12));
+        const uint32_t f1 = half2_bits(pow2i(-g1), pow2i(-g1)), f2 = half2_bits(pow2i(max(g1 - g, -40)), pow2i(max(g1 - g, -40)));
 #pragma unroll 2
         for (int k = 0; k < D / 16; ++k) {
             const uint4 in = __ldg(reinterpret_cast<const uint4*>(v + ((size_t)k * kTileTokens + t) * 16));
             const uint32_t w[4] = {in.x, in.y, in.z, in.w};
             uint32_t h[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                h[i] = half2_bits((float)(int)(int8_t)(w[i / 2] >> (16 * (i & 1))) * f, (float)(int)(int8_t)(w[i / 2] >> (16 * (i & 1) + 8)) * f);
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t even = int8_to_half2<false>(w[i]), odd = int8_to_half2<true>(w[i]);
+                h[2 * i] = mul_half2(mul_half2(__byte_perm(even, odd, 0x5410), f1), f2);
+                h[2 * i + 1] = mul_half2(mul_half2(__byte_perm(even, odd, 0x7632), f1), f2);
+            }
             row[(2 * k) ^ (t & 7)] = make_uint4(h[0], h[1], h[2], h[3]);
             row[(2 * k + 1) ^ (t & 7)] = make_uint4(h[4], h[5], h[6], h[7]);
         }
