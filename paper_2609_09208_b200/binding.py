@@ -188,11 +188,9 @@ def fill_kv(cfg, cache: SaCache, K, V, cu_lens_host):
 
 def read_kv(cfg, cache: SaCache, starts, cu_lens_host, K=None, V=None):
     """Tokens starts[b] .. of every sequence, cu_lens_host[b + 1] - cu_lens_host[b] of them, as binary16 rows of K and V
-    ([rows, n_kv_heads, head_dim], contiguous; either may be None).  starts (None: all 0), cu_lens_host: numpy int64 of batch and batch + 1
-    entries (host memory)."""
-    import numpy as np
-    starts = None if starts is None else np.ascontiguousarray(starts, dtype=np.int64)
-    st = (_nat or native()).read_kv(cfg, cache, starts, np.ascontiguousarray(cu_lens_host, dtype=np.int64), K, V)
+    ([rows, n_kv_heads, head_dim], contiguous; either may be None).  starts (None: all 0), cu_lens_host: contiguous numpy int64 arrays of batch
+    and batch + 1 entries (host memory)."""
+    st = (_nat or native()).read_kv(cfg, cache, starts, cu_lens_host, K, V)
     if st:
         raise SaError(st, "sa_read_kv")
 

@@ -11,7 +11,7 @@
 
 namespace {
 
-PyObject *g_data_ptr, *g_nbytes, *g_get_device, *g_get_stream, *g_shape, *g_stride, *g_dtype, *g_itemsize, *g_device_of;
+PyObject *g_data_ptr, *g_nbytes, *g_get_device, *g_get_stream, *g_shape, *g_stride, *g_is_contiguous, *g_dtype, *g_itemsize, *g_device_of, *g_float16, *g_int32;
 
 struct Args {
     PyObject* const* v;
@@ -73,29 +73,44 @@ struct Args {
         bad = true;
         return false;
     }
-    // Shape and strides (elements) of a tensor of n dimensions, its bytes an element and its device; dtype (unless null): its type.
-    bool describe(PyObject* o, int n, long long* shape, long long* stride, PyObject* dtype, long long* itemsize, long long* device, const char* what) {
-        if (bad) return false;
-        PyObject* sh = PyObject_GetAttr(o, g_shape);
-        PyObject* st = sh ? PyObject_CallMethodNoArgs(o, g_stride) : nullptr;
-        bool ok = st && PyTuple_Check(sh) && PyTuple_Check(st) && PyTuple_GET_SIZE(sh) == n && PyTuple_GET_SIZE(st) == n;
-        for (int i = 0; ok && i < n; ++i) {
-            shape[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(sh, i));
-            stride[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(st, i));
-        }
+    // What a tensor of n dimensions has to be, at a price that a call of a few microseconds can bear: each of these is one attribute or method.
+    bool shape(PyObject* o, int n, long long* out) {
+        PyObject* sh = bad ? nullptr : PyObject_GetAttr(o, g_shape);
+        bool ok = sh && PyTuple_Check(sh) && PyTuple_GET_SIZE(sh) == n;
+        for (int i = 0; ok && i < n; ++i) out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(sh, i));
         Py_XDECREF(sh);
+        return ok;
+    }
+    bool strides(PyObject* o, int n, long long* out) {        // in elements
+        PyObject* st = bad ? nullptr : PyObject_CallMethodNoArgs(o, g_stride);
+        bool ok = st && PyTuple_Check(st) && PyTuple_GET_SIZE(st) == n;
+        for (int i = 0; ok && i < n; ++i) out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(st, i));
         Py_XDECREF(st);
-        PyObject* t = ok ? PyObject_GetAttr(o, g_dtype) : nullptr;
-        ok = t && (!dtype || t == dtype);
-        if (ok) *itemsize = (long long)number_of(PyObject_GetAttr(t, g_itemsize));
+        return ok;
+    }
+    bool contiguous(PyObject* o) {
+        PyObject* c = bad ? nullptr : PyObject_CallMethodNoArgs(o, g_is_contiguous);
+        const bool ok = c == Py_True;
+        Py_XDECREF(c);
+        return ok;
+    }
+    bool on_device(PyObject* o, long long device) {           // (a tensor that is not on a CUDA device says -1)
+        PyObject* d = bad ? nullptr : PyObject_CallMethodNoArgs(o, g_device_of);
+        const bool ok = d && PyLong_AsLongLong(d) == device;
+        Py_XDECREF(d);
+        return ok;
+    }
+    // dtype: exactly that type; null: any of `itemsize` bytes
+    bool typed(PyObject* o, PyObject* dtype, unsigned long long itemsize) {
+        PyObject* t = bad ? nullptr : PyObject_GetAttr(o, g_dtype);
+        bool ok = t && (dtype ? t == dtype : (itemsize == 2 && t == g_float16) || (itemsize == 4 && t == g_int32));
+        if (t && !ok && !dtype) ok = number_of(PyObject_GetAttr(t, g_itemsize)) == itemsize;
         Py_XDECREF(t);
-        if (ok) {
-            PyObject* d = PyObject_CallMethodNoArgs(o, g_device_of);
-            *device = d ? PyLong_AsLongLong(d) : -1;                  // (-1: not on a CUDA device)
-            Py_XDECREF(d);
-        }
-        if (PyErr_Occurred()) bad = true;
-        return !bad && (ok || fail(what));
+        return ok;
+    }
+    template <typename T>
+    T* address(PyObject* o) {
+        return reinterpret_cast<T*>(bad ? 0 : number_of(PyObject_CallMethodNoArgs(o, g_data_ptr)));
     }
     // The current device, which tensors and streams of a call belong to.
     long long current_device() { return bad ? -1 : (long long)number_of(PyObject_CallNoArgs(g_get_device)); }
@@ -230,7 +245,7 @@ PyObject* fill_kv(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return PyLong_FromLong(st);
 }
 
-// A host array of at least `n` 64-bit integers; None (where it may be): null.
+// A contiguous host array of at least `n` 64-bit integers; None (where it may be): null.
 struct HostArray {
     Py_buffer b{};
     bool held = false;
@@ -238,12 +253,13 @@ struct HostArray {
     HostArray(Args& a, Py_ssize_t n, bool may_be_none, const char* what) {
         PyObject* o = a.bad ? nullptr : a.next();
         if (a.bad || (may_be_none && o == Py_None)) return;
-        if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) {
+        if (PyObject_GetBuffer(o, &b, PyBUF_FORMAT | PyBUF_C_CONTIGUOUS) != 0) {
             a.bad = true;
             return;
         }
         held = true;
-        if (b.len / (Py_ssize_t)sizeof(int64_t) < n) a.fail(what);
+        const char* f = b.format ? b.format : "B";
+        if (b.itemsize != 8 || (f[0] != 'l' && f[0] != 'q') || f[1] || b.len / (Py_ssize_t)sizeof(int64_t) < n) a.fail(what);
         else p = static_cast<const int64_t*>(b.buf);
     }
     ~HostArray() {
@@ -257,20 +273,17 @@ PyObject* read_kv(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const sa_config* cfg = a.structure<sa_config>();
     const sa_cache* cache = a.structure<sa_cache>();
     const Py_ssize_t batch = a.bad || cache->batch < 0 ? 0 : cache->batch;
-    HostArray starts(a, batch, true, "starts holds fewer than batch numbers of 8 bytes");
-    HostArray cu(a, batch + 1, false, "cu_lens holds fewer than batch + 1 numbers of 8 bytes");
+    HostArray starts(a, batch, true, "starts holds at least batch 64-bit integers");
+    HostArray cu(a, batch + 1, false, "cu_lens holds at least batch + 1 64-bit integers");
     const long long dev = a.current_device();
     uint16_t* out[2] = {nullptr, nullptr};
     for (int i = 0; i < 2 && !a.bad; ++i) {
         PyObject* o = a.next();
         if (a.bad || o == Py_None) continue;
-        long long shape[3], stride[3], size = 0, device = -1;
-        const long long H = cfg->n_kv_heads, d = cfg->head_dim;
-        if (!a.describe(o, 3, shape, stride, nullptr, &size, &device, "K and V are tensors [rows, n_kv_heads, head_dim]")) break;
-        if (size != 2 || shape[1] != H || shape[2] != d || (shape[0] > 1 && stride[0] != H * d) || (H > 1 && stride[1] != d) || stride[2] != 1 || shape[0] < cu.p[batch])
-            a.fail("K and V are contiguous [rows, n_kv_heads, head_dim] of 2-byte numbers with a row for every token");
-        else if (device != dev) a.fail("K and V lie on the current CUDA device");
-        else out[i] = reinterpret_cast<uint16_t*>(a.number_of(PyObject_CallMethodNoArgs(o, g_data_ptr)));
+        long long sh[3];
+        if (!a.shape(o, 3, sh) || sh[1] != cfg->n_kv_heads || sh[2] != cfg->head_dim || sh[0] < cu.p[batch] || !a.typed(o, nullptr, 2) || !a.contiguous(o) || !a.on_device(o, dev))
+            a.fail("K and V are contiguous [rows, n_kv_heads, head_dim] of 2-byte numbers on the current CUDA device, with a row for every token");
+        out[i] = a.address<uint16_t>(o);
     }
     const sa_stream s = a.stream();
     SA_RETURN(sa_read_kv(cfg, cache, starts.p, cu.p, out[0], out[1], s));
@@ -286,38 +299,33 @@ PyObject* rotate_qkv(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     if (!a.bad && tables >= 0 && tables != dev) a.fail("the tables lie on another device than the current one");
     const void* in[3] = {};
     uint16_t* out[3] = {};
-    long long stride[3] = {}, n = -1, shape[3], st[3], size = 0, device = -1;
-    const char* rows = "Q, K and V are [n, heads, head_dim] of the rotary's dtype on the current CUDA device, a token's heads one after another, n the same for all";
+    long long stride[3] = {}, n = -1, sh[3], step[3];
+    const long long d = a.bad ? 0 : cfg->head_dim;
     for (int i = 0; i < 3 && !a.bad; ++i) {
         PyObject* o = a.next();
-        if (a.bad || o == Py_None || !a.describe(o, 3, shape, st, dtype, &size, &device, rows)) continue;
-        const long long H = i == 0 ? cfg->n_q_heads : cfg->n_kv_heads, d = cfg->head_dim;
-        if (device != dev || shape[1] != H || shape[2] != d || (H > 1 && st[1] != d) || st[2] != 1 || (n >= 0 && shape[0] != n)) a.fail(rows);
-        n = shape[0];
-        stride[i] = n > 1 ? st[0] : H * d;
-        in[i] = reinterpret_cast<const void*>(a.bad ? 0 : a.number_of(PyObject_CallMethodNoArgs(o, g_data_ptr)));
+        if (a.bad || o == Py_None) continue;
+        const long long H = i == 0 ? cfg->n_q_heads : cfg->n_kv_heads;
+        if (!a.shape(o, 3, sh) || sh[1] != H || sh[2] != d || (n >= 0 && sh[0] != n) || !a.strides(o, 3, step) || (H > 1 && step[1] != d) || step[2] != 1 ||
+            !a.typed(o, dtype, 0) || !a.on_device(o, dev))
+            a.fail("Q, K and V are [n, heads, head_dim] of the rotary's dtype on the current CUDA device, a token's heads one after another, n the same for all");
+        n = sh[0];
+        stride[i] = n > 1 ? step[0] : H * d;
+        in[i] = a.address<const void>(o);
     }
     const int32_t* positions = nullptr;
     PyObject* pos = a.bad ? nullptr : a.next();
     if (!a.bad && pos != Py_None) {
-        PyObject* sh = PyObject_GetAttr(pos, g_shape);
-        const int dims = sh && PyTuple_Check(sh) ? (int)PyTuple_GET_SIZE(sh) : 0;
-        Py_XDECREF(sh);
-        const char* what = "positions are contiguous 4-byte integers [n_axes, n] on the current CUDA device";
-        if (dims != 1 && dims != 2) a.fail(what);
-        else if (a.describe(pos, dims, shape, st, nullptr, &size, &device, what)) {
-            const long long axes = dims == 2 ? shape[0] : 1, len = shape[dims - 1];
-            if (size != 4 || device != dev || axes != rot->n_axes || (n >= 0 && len != n) || (len > 1 && st[dims - 1] != 1) || (axes > 1 && len > 0 && st[0] != len)) a.fail(what);
-            positions = reinterpret_cast<const int32_t*>(a.bad ? 0 : a.number_of(PyObject_CallMethodNoArgs(pos, g_data_ptr)));
-        }
+        const bool two = a.shape(pos, 2, sh);
+        if (two ? sh[0] != rot->n_axes || (n >= 0 && sh[1] != n) : rot->n_axes != 1 || !a.shape(pos, 1, sh) || (n >= 0 && sh[0] != n)) a.fail("positions are [n_axes, n]");
+        else if (!a.typed(pos, nullptr, 4) || !a.contiguous(pos) || !a.on_device(pos, dev)) a.fail("positions are contiguous 4-byte integers on the current CUDA device");
+        positions = a.address<const int32_t>(pos);
     }
     for (int i = 0; i < 3 && !a.bad; ++i) {
         PyObject* o = a.next();
-        const char* what = "the outputs are contiguous [n, heads, head_dim] of 2-byte numbers on the current CUDA device, one for each of Q, K and V that is given";
-        if (a.bad || o == Py_None || !a.describe(o, 3, shape, st, nullptr, &size, &device, what)) continue;
-        const long long H = i == 0 ? cfg->n_q_heads : cfg->n_kv_heads, d = cfg->head_dim;
-        if (size != 2 || device != dev || shape[0] != n || shape[1] != H || shape[2] != d || (n > 1 && st[0] != H * d) || (H > 1 && st[1] != d) || st[2] != 1) a.fail(what);
-        out[i] = reinterpret_cast<uint16_t*>(a.bad ? 0 : a.number_of(PyObject_CallMethodNoArgs(o, g_data_ptr)));
+        if (a.bad || o == Py_None) continue;
+        if (!a.shape(o, 3, sh) || sh[0] != n || sh[1] != (i == 0 ? cfg->n_q_heads : cfg->n_kv_heads) || sh[2] != d || !a.typed(o, nullptr, 2) || !a.contiguous(o) || !a.on_device(o, dev))
+            a.fail("the outputs are contiguous [n, heads, head_dim] of 2-byte numbers on the current CUDA device, one for each of Q, K and V that is given");
+        out[i] = a.address<uint16_t>(o);
     }
     // (a tensor without elements has no address, which would read as one that is not there)
     if (!a.bad && n == 0) return PyLong_FromLong(SA_OK);
@@ -350,9 +358,14 @@ PyMODINIT_FUNC PyInit__native(void) {
     g_nbytes = PyUnicode_InternFromString("nbytes");
     g_shape = PyUnicode_InternFromString("shape");
     g_stride = PyUnicode_InternFromString("stride");
+    g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    PyObject* torch = PyImport_ImportModule("torch");
+    g_float16 = torch ? PyObject_GetAttrString(torch, "float16") : nullptr;
+    g_int32 = torch ? PyObject_GetAttrString(torch, "int32") : nullptr;
+    Py_XDECREF(torch);
     g_dtype = PyUnicode_InternFromString("dtype");
     g_itemsize = PyUnicode_InternFromString("itemsize");
     g_device_of = PyUnicode_InternFromString("get_device");
-    if (!g_get_device || !g_get_stream || !g_data_ptr || !g_nbytes || !g_shape || !g_stride || !g_dtype || !g_itemsize || !g_device_of) return nullptr;
+    if (!g_get_device || !g_get_stream || !g_data_ptr || !g_nbytes || !g_shape || !g_stride || !g_is_contiguous || !g_float16 || !g_int32 || !g_dtype || !g_itemsize || !g_device_of) return nullptr;
     return PyModule_Create(&kModule);
 }

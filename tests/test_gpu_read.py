@@ -77,7 +77,8 @@ def test_reads_what_the_codes_stand_for(code, dense, d, Hkv, hadamard):
     tol_V = half_step(V) * (1 + 1e-3)
     for starts, counts in [(None, LENS), ([0, 0, 5, 31, 63, 1, 40, 7], [0, 1, 20, 2, 1, 64, 80, 0]), ([0, 1, 31, 0, 33, 65, 129, 3], [0, 0, 0, 33, 31, 0, 1, 4])]:
         cu = np.concatenate([[2], 2 + np.cumsum(counts)])
-        rows = np.concatenate([case.cu_lens[b] + (starts[b] if starts else 0) + np.arange(n) for b, n in enumerate(counts)]).astype(np.int64)
+        starts = None if starts is None else np.array(starts)
+        rows = np.concatenate([case.cu_lens[b] + (0 if starts is None else starts[b]) + np.arange(n) for b, n in enumerate(counts)]).astype(np.int64)
         out = [torch.full((int(cu[-1]) + 3, Hkv, d), 777.0, dtype=torch.float16, device="cuda") for _ in range(4)]
         sa.read_kv(cfg, c.handle, starts, cu, out[0], out[1])
         sa.read_kv(cfg, c.handle, starts, cu, out[2], None)
@@ -98,9 +99,9 @@ def test_unmapped_pages_read_as_zeros(code):
     c = sa.PagedCache(cfg, [200], "cuda")
     c.fill(up(case.K), up(case.V), case.cu_lens)
     whole, holes = ([torch.full((200, 2, 64), 3.0, dtype=torch.float16, device="cuda") for _ in "kv"] for _ in range(2))
-    sa.read_kv(cfg, c.handle, None, [0, 200], *whole)
+    sa.read_kv(cfg, c.handle, None, np.array([0, 200]), *whole)
     c.page_table[0, 1], c.page_table[0, 3] = -1, 1 << 20
-    sa.read_kv(cfg, c.handle, None, [0, 200], *holes)
+    sa.read_kv(cfg, c.handle, None, np.array([0, 200]), *holes)
     torch.cuda.synchronize()
     for w, h in zip(whole, holes):
         assert torch.equal(h[:64], w[:64]) and torch.equal(h[128:192], w[128:192]) and not h[64:128].any() and not h[192:].any()
@@ -140,10 +141,10 @@ def test_what_is_read_can_be_written_again():
     c = sa.PagedCache(cfg, [300], "cuda")
     c.fill(up(case.K), up(case.V), case.cu_lens)
     out = [torch.full((300, 2, 128), 3.0, dtype=torch.float16, device="cuda") for _ in range(4)]
-    sa.read_kv(cfg, c.handle, None, [0, 300], out[0], out[1])
+    sa.read_kv(cfg, c.handle, None, np.array([0, 300]), out[0], out[1])
     c.pages.fill_(0xff)
     c.fill(out[0], out[1], case.cu_lens)
-    sa.read_kv(cfg, c.handle, None, [0, 300], out[2], out[3])
+    sa.read_kv(cfg, c.handle, None, np.array([0, 300]), out[2], out[3])
     torch.cuda.synchronize()
     assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3])
 
@@ -153,7 +154,7 @@ def test_the_binding_refuses_what_does_not_fit():
     cfg = sa.make_config(64, 4, 4, sa.SA_KV_FP4)
     c = sa.PagedCache(cfg, [100, 100], "cuda")
     good = torch.zeros(200, 4, 64, dtype=torch.float16, device="cuda")
-    call = lambda K, V=None, starts=None, cu=(0, 100, 200): sa.read_kv(cfg, c.handle, starts, list(cu), K, V)
+    call = lambda K, V=None, starts=None, cu=(0, 100, 200): sa.read_kv(cfg, c.handle, None if starts is None else np.array(starts), np.array(cu), K, V)
     call(good)
     for bad in (good[:199], good.float(), good.cpu(), good.view(200, 2, 128), torch.zeros(200, 4, 128, dtype=torch.float16, device="cuda")[..., :64],
                 torch.zeros(400, 4, 64, dtype=torch.float16, device="cuda")[::2], good[0]):
@@ -163,6 +164,9 @@ def test_the_binding_refuses_what_does_not_fit():
             call(None, bad)
     with pytest.raises(ValueError, match="starts"):
         call(good, starts=[0])
+    for cu in (np.array([0, 1, 2], dtype=np.int32), np.array([0.0, 1.0, 2.0]), np.array([0, 9, 1, 9, 2])[::2], np.array([0, 1])):
+        with pytest.raises(ValueError):
+            sa.read_kv(cfg, c.handle, None, cu, good, None)
     for starts, cu, status in ((None, (0, 100, 50), 1), ([-1, 0], (0, 1, 2), 1), ([100, 0], (0, 29, 30), 4), ([129, 0], (0, 0, 1), 4), (None, (0, 129, 130), 4)):
         with pytest.raises(sa.SaError) as err:
             call(good, starts=starts, cu=cu)
