@@ -219,7 +219,7 @@ def test_unmapped_pages_are_skipped():
     assert (np.abs(O.cpu().numpy() - ref) <= fp4.tolerance(against, 64, 500)).all()
 
 
-FORMS = [(64, 32, 4, [0, 1, 31, 63, 64, 500], 0), (64, 8, 1, [2047], 0), (64, 32, 2, [33, 100], 0), (128, 32, 8, [0, 15, 128, 700], 0),
+FORMS = [(64, 32, 4, [0, 1, 31, 63, 64, 500], 0), (64, 5, 1, [40, 200], 0), (128, 28, 4, [900, 0, 64], 0), (64, 12, 2, MIX, 16384), (64, 8, 1, [2047], 0), (64, 32, 2, [33, 100], 0), (128, 32, 8, [0, 15, 128, 700], 0),
          (128, 16, 16, [62, 63], 0), (64, 32, 4, MIX, 16384), (128, 32, 8, MIX, 16384), (64, 4, 4, [(7 * i) % 62 for i in range(130)], 0)]
 
 
@@ -295,6 +295,79 @@ def test_static_scratch_stages_and_repeats_give_the_same_bits():
     with pytest.raises(sa.SaError) as err:
         attend(cfg, c, Q, O[0], dbg_scores=torch.zeros(4 * 32 * 5056, dtype=torch.int32, device="cuda"))
     assert err.value.status == 2
+
+
+@pytest.mark.parametrize("d,Hq,Hkv,lens,room", [(64, 10, 2, [5000, 333], 0), (128, 14, 2, [20000], 0), (64, 28, 4, MIX, 16384), (128, 40, 8, MIX, 16384), (64, 36, 4, MIX, 16384)])
+def test_stages_of_groups_of_any_size(d, Hq, Hkv, lens, room):
+    """The decode kernel and the merge of its partials apart, for query groups of 5, 7 and 9 (three heads a block)."""
+    import torch
+    cfg = config(d, Hq, Hkv)
+    case = synth.make_case("fp4g", lens, Hq, Hkv, d, 0, seed=Hq)
+    c = poisoned(cfg, lens, room=room)
+    c.fill(up(case.K), up(case.V), case.cu_lens)
+    Q, O = up(case.Q), [torch.full((len(lens), Hq, d), float("nan"), device="cuda") for _ in range(2)]
+    attend(cfg, c, Q, O[0])
+    attend(cfg, c, Q, O[1], stages=1)
+    attend(cfg, c, Q, O[1], stages=2)
+    ref, against = fp4.attention(case.Q, fp4.quantised(case.K), fp4.quantised(case.V), case.cu_lens, Hq // Hkv)
+    tol = fp4.tolerance(against, d, max(lens))
+    for o in O:
+        o = o.cpu().numpy()
+        assert np.isfinite(o).all() and (np.abs(o - ref) <= tol).all(), np.max(np.abs(o - ref) / tol)
+
+
+def test_one_workspace_for_calls_of_different_forms_in_turn():
+    """4-bit calls of every form and calls of another code, each after every other on one workspace that starts as 255."""
+    import torch
+    forms = [(64, 32, 4, sa.SA_KV_FP4, MIX, 16384), (64, 32, 4, sa.SA_KV_FP4, [700, 64, 0, 31], 0), (64, 4, 4, sa.SA_KV_FP4, [33] * 130, 0),
+             (128, 32, 8, sa.SA_KV_FP4, [20000], 0), (64, 32, 4, sa.SA_POTM4, MIX, 16384), (128, 32, 8, sa.SA_KV_FP4, MIX, 16384)]
+    calls = []
+    for d, Hq, Hkv, code, lens, room in forms:
+        cfg = sa.make_config(d, Hq, Hkv, code)
+        case = synth.make_case("turn", lens, Hq, Hkv, d, 0, seed=d + len(lens))
+        c = wide_cache(cfg, lens, room or (max(lens) + 64) // 64 * 64, extra=1)
+        c.fill(up(case.K), up(case.V), case.cu_lens)
+        new = [up(x[np.minimum(np.arange(len(lens)), len(x) - 1)]) for x in (case.K, case.V)]
+        calls.append((cfg, c, up(case.Q), new, c.seq_lens.clone()))
+
+    def run(call, workspace):
+        cfg, c, Q, (K, V), lens0 = call
+        O = torch.full(Q.shape, float("nan"), device="cuda")
+        c.seq_lens.copy_(lens0)
+        sa.decode_step(cfg, c.handle, Q, K, V, O, workspace)
+        return O, c.seq_lens.clone()
+
+    want = [run(call, call[1].workspace) for call in calls]
+    one = torch.full((max(len(call[1].workspace) for call in calls),), 255, dtype=torch.uint8, device="cuda")
+    got = [(i, run(calls[i], one)) for a in range(len(calls)) for j in range(len(calls)) for i in (a, j)]
+    torch.cuda.synchronize()
+    for i, (O, lens) in got:
+        assert torch.equal(O, want[i][0]) and torch.equal(lens, calls[i][4] + 1), i
+
+
+def test_a_pool_beyond_32_bits():
+    """Pages behind the first 4 GB of the pool: fill, append, decode, read."""
+    import torch
+    cfg, n_pages, T = config(128, 16, 8), 62000, 200
+    assert n_pages * 8 * sa.get_layout(cfg).page_bytes > 1 << 32
+    case = synth.make_case("fp4big", [T + 1], 16, 8, 128, 0, seed=21)
+    pages = torch.zeros(n_pages * 8 * sa.get_layout(cfg).page_bytes, dtype=torch.uint8, device="cuda")
+    table = torch.tensor([[n_pages - 1, n_pages - 7, n_pages - 2, 58300]], dtype=torch.int32, device="cuda")
+    lens = torch.zeros(1, dtype=torch.int32, device="cuda")
+    handle = sa.make_cache(pages, table, lens, n_pages)
+    workspace = torch.empty(sa.workspace_bytes(cfg, 1, 4), dtype=torch.uint8, device="cuda")
+    sa.fill_kv(cfg, handle, up(case.K[:T]), up(case.V[:T]), np.array([0, T]))
+    lens.fill_(T)
+    O = torch.full((1, 16, 128), float("nan"), device="cuda")
+    sa.decode_step(cfg, handle, up(case.Q), up(case.K[T:]), up(case.V[T:]), O, workspace)
+    K, V = (torch.zeros(T + 1, 8, 128, dtype=torch.float16, device="cuda") for _ in "kv")
+    sa.read_kv(cfg, handle, None, np.array([0, T + 1]), K, V)
+    Kq, Vq = fp4.quantised(case.K), fp4.quantised(case.V)
+    assert np.array_equal(K.cpu().numpy(), Kq) and np.array_equal(V.cpu().numpy(), Vq)
+    ref, against = fp4.attention(case.Q, Kq, Vq, np.array([0, T + 1]), 2)
+    assert (np.abs(O.cpu().numpy() - ref) <= fp4.tolerance(against, 128, T)).all()
+    del pages
+    torch.cuda.empty_cache()
 
 
 def test_two_streams_with_workspaces_of_their_own():

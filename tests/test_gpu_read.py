@@ -51,14 +51,11 @@ def half_step(x):
     return np.maximum(np.abs(x) * 2.0 ** -11, 2.0 ** -25)
 
 
-@pytest.mark.parametrize("hadamard", [False, True])
 @pytest.mark.parametrize("d,Hkv", [(64, 4), (128, 3)])
-@pytest.mark.parametrize("code,dense", CODES)
+@pytest.mark.parametrize("code,dense,hadamard", [(*c, h) for c in CODES for h in (False, True) if c[0] != sa.SA_KV_FP16 or not h])      # (binary16 is never rotated)
 def test_reads_what_the_codes_stand_for(code, dense, d, Hkv, hadamard):
     """Whole sequences and ranges from odd places; rows that are not asked for, and rows behind the last, stay."""
     import torch
-    if hadamard and code == sa.SA_KV_FP16:
-        pytest.skip("the binary16 cache is never rotated")
     cfg = sa.make_config(d, Hkv, Hkv, code, nibble=dense, hadamard=hadamard)
     case = synth.make_case("read", LENS, Hkv, Hkv, d, 0, outliers=True, seed=d + code)
     case.V[::5] *= np.float16(1e-5)
@@ -129,6 +126,43 @@ def test_many_sequences_and_a_captured_call():
         graph.replay()
         torch.cuda.synchronize()
         assert np.array_equal(K.cpu().numpy().astype(np.float64), flip * fp4.quantised(case.K)) and np.array_equal(V.cpu().numpy().astype(np.float64), fp4.quantised(case.V))
+
+
+@pytest.mark.parametrize("hadamard", [False, True])
+def test_rows_that_start_between_32_byte_places(hadamard):
+    """Tensors on 16-byte boundaries only, in and out: the same bytes as from aligned ones."""
+    import torch
+    cfg, n = sa.make_config(64, 3, 3, sa.SA_KV_FP4, hadamard=hadamard), 77
+    case = synth.make_case("reado", [n], 3, 3, 64, 0, seed=9)
+    room = n * 3 * 64
+    aligned = [up(case.K).view(torch.float16), up(case.V).view(torch.float16)]
+    shifted = [torch.empty(room + 8, dtype=torch.float16, device="cuda")[8:].view(n, 3, 64) for _ in range(4)]
+    for s, a in zip(shifted, aligned):
+        s.copy_(a.view(n, 3, 64))
+        assert s.data_ptr() % 32 == 16
+    caches = [sa.PagedCache(cfg, [n], "cuda") for _ in range(2)]
+    caches[0].fill(*aligned, case.cu_lens)
+    caches[1].fill(*shifted[:2], case.cu_lens)
+    out = [torch.zeros(n, 3, 64, dtype=torch.float16, device="cuda") for _ in "kv"]
+    sa.read_kv(cfg, caches[0].handle, None, case.cu_lens, *out)
+    sa.read_kv(cfg, caches[1].handle, None, case.cu_lens, *shifted[2:])
+    torch.cuda.synchronize()
+    assert torch.equal(caches[0].pages, caches[1].pages) and torch.equal(out[0], shifted[2]) and torch.equal(out[1], shifted[3])
+
+
+def test_rows_beyond_32_bits():
+    """A row whose place in the output is beyond 2^32 bytes and 2^31 elements."""
+    import torch
+    cfg, row = sa.make_config(64, 1, 1, sa.SA_KV_FP4), (1 << 25) + 5
+    case = synth.make_case("readb", [90], 1, 1, 64, 0, seed=10)
+    c = sa.PagedCache(cfg, [90], "cuda")
+    c.fill(up(case.K), up(case.V), case.cu_lens)
+    K = torch.zeros(row + 90, 1, 64, dtype=torch.float16, device="cuda")
+    assert row * 64 > 1 << 31
+    sa.read_kv(cfg, c.handle, None, np.array([row, row + 90]), K, None)
+    assert np.array_equal(K[row:].cpu().numpy(), fp4.quantised(case.K)) and not K[:row].any()
+    del K
+    torch.cuda.empty_cache()
 
 
 def test_what_is_read_can_be_written_again():

@@ -50,6 +50,7 @@ CASES = [
     (128, 5, 5, "float16", 32, False, 2, True, False, 1.25, 3), (64, 1, 1, "float32", 8, True, 1, False, False, 0.75, 2),
     (64, 12, 1, "bfloat16", 48, False, 4, True, True, 1.0, 129), (128, 64, 8, "float16", 64, True, 1, False, False, 1.0, 20),
     (64, 8, 2, "float16", 0, False, 1, True, True, 1.0, 31), (128, 40, 8, "float32", 0, True, 1, False, False, 1.0, 5),
+    (64, 8, 2, "bfloat16", 64, False, 2, True, True, 1.0, 601), (128, 4, 1, "float32", 128, True, 1, True, False, 1.0, 1027), (64, 3, 1, "float16", 24, False, 1, False, False, 1.0, 777),
     (128, 2, 1, "bfloat16", 120, False, 3, True, True, 1.0, 17), (64, 33, 11, "float16", 56, False, 1, True, True, 1.0, 9)]
 
 
@@ -133,6 +134,21 @@ def test_in_place_empty_and_extreme_inputs():
     out = torch.zeros(1, 2, d, dtype=torch.float16, device="cuda")
     sa.rotate_qkv(sa.Rotary(cfg, dtype=torch.float32), None, None, V, None, None, None, out)
     assert torch.equal(out, V.half())
+
+
+def test_rows_beyond_32_bits():
+    """Tokens whose places in input and output are beyond 2^31 elements."""
+    import torch
+    n, cfg = (1 << 25) + 3, sa.make_config(64, 1, 1, sa.SA_POTM4)
+    x = torch.zeros(n, 1, 64, dtype=torch.bfloat16, device="cuda")
+    x[-3:] = torch.randn(3, 1, 64, device="cuda")
+    rot = sa.Rotary(cfg, torch.from_numpy(frequencies(64)).cuda(), dtype=torch.bfloat16)
+    pos, out = torch.arange(n, dtype=torch.int32, device="cuda"), torch.full((n, 1, 64), 3.0, dtype=torch.float16, device="cuda")
+    sa.rotate_qkv(rot, x, None, None, pos, out, None, None)
+    y, size = reference(x[-3:].double().cpu().numpy(), 64, False, pos[-3:].cpu().numpy()[None], np.zeros(32, int), frequencies(64), False, 0.0, None, 1.0)
+    assert (np.abs(out[-3:].double().cpu().numpy() - y) <= tolerance(y, size)).all() and not out[:-3].any()
+    del x, out, pos
+    torch.cuda.empty_cache()
 
 
 def test_the_binding_refuses_what_does_not_fit():
