@@ -74,7 +74,7 @@ enum { SA_POT4 = 0, SA_POTM1 = 1, SA_POTM2 = 2, SA_POTM4 = 4, SA_INT8 = 8, SA_KV
  * scale, stored one byte per element in the byte container (132 bytes per key at d = 64, the same
  * as PoT-M4); scores are integer dot products with INT32 sums.  Everything else (query and
  * value quantisers, softmax, A.V, merge, cache layout) is shared with the power-of-two codes. */
-/* SA_KV_FP4: keys AND values in 4 bits, (the paper has no counterpart: its caches hold values in 8).  A vector of head_dim channels is
+/* SA_KV_FP4: keys AND values in 4 bits (the paper has no counterpart: its caches hold values in 8).  A vector of head_dim channels is
  * cut into blocks of 16.  A block's scale is s = max|x| / 6 rounded to the nearest unsigned 8-bit float (5 bits of exponent, 3 of
  * mantissa, ties to even), at most 10240, held as a byte b: s is the binary16 number of the bits b << 7.  A channel's code is x / s rounded to the nearest
  * of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (numbers 0 .. 7 of its lowest three bits; ties to the even number, 6 at most), bit 3 the sign (which a zero may or may not

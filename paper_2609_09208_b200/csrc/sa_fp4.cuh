@@ -20,6 +20,7 @@
 namespace sa {
 
 constexpr uint32_t kFp4ScaleMost = 0xe2u;              // 10240: 6 times that is the largest below 65504
+constexpr uint32_t kFp4ScaleNaN = 0xffu;
 
 // x / s, correctly rounded where it matters (see above): exact for quotients of a few bits, within an ulp otherwise.
 SA_HD float fp4_quotient(float x, float s, float inv) {
@@ -36,13 +37,13 @@ SA_D float fp4_inverse(float s) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
     return s > 0.0f ? r : 0.0f;
 }
-// Scale byte of a block whose largest magnitude has the binary16 bits `amax`.
+// Scale byte of a block whose largest magnitude has the binary16 bits `amax`.  An infinity or NaN marks the whole block: NaN.
 SA_D uint32_t fp4_scale_byte(uint32_t amax) {
     const float t = fp4_quotient(half_bits_to_float(amax), 6.0f, 1.0f / 6.0f);
     const uint32_t u = __float_as_uint(t);
     const uint32_t normal = ((u + 0x7ffffu + ((u >> 20) & 1u)) >> 20) - (112u << 3);
     const uint32_t b = t >= 0x1p-14f ? normal : (uint32_t)__float2int_rn(t * 0x1p17f);
-    return min(b, kFp4ScaleMost);
+    return amax < 0x7c00u ? min(b, kFp4ScaleMost) : kFp4ScaleNaN;
 }
 SA_D float fp4_scale(uint32_t byte) { return half_bits_to_float(byte << 7); }
 // Codes of 8 channels (pairs of binary16), the first in the lowest nibble.  The quotients as fp4_quotient's, two at a time.
@@ -67,7 +68,7 @@ SA_D uint32_t fp4_codes(const uint32_t (&x)[4], float s, float inv) {
 SA_D uint32_t fp4_block(const uint32_t (&x)[8], uint32_t (&w)[2]) {
     uint32_t top = x[0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) asm("max.xorsign.abs.f16x2 %0, %0, %1;" : "+r"(top) : "r"(x[i]));      // two magnitudes at a time, with signs that do not matter
+    for (int i = 1; i < 8; ++i) asm("max.NaN.xorsign.abs.f16x2 %0, %0, %1;" : "+r"(top) : "r"(x[i]));      // two magnitudes at a time, with signs that do not matter
     const uint32_t b = fp4_scale_byte(max(top & 0x7fffu, (top >> 16) & 0x7fffu));
     const float s = fp4_scale(b), inv = fp4_inverse(s);
     const uint32_t lo[4] = {x[0], x[1], x[2], x[3]}, hi[4] = {x[4], x[5], x[6], x[7]};

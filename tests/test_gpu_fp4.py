@@ -345,6 +345,47 @@ def test_one_workspace_for_calls_of_different_forms_in_turn():
         assert torch.equal(O, want[i][0]) and torch.equal(lens, calls[i][4] + 1), i
 
 
+@pytest.mark.parametrize("d,Hq,Hkv,lens,room", [(64, 8, 2, [130, 65, 40], 0), (128, 8, 2, [130, 65, 40], 0), (64, 32, 4, MIX, 16384)])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_infinities_and_nans_show(d, Hq, Hkv, lens, room, bad):
+    """In a key: its head's queries of that sequence; in a value: the 16 channels of its block; nothing else.  By fill and by append."""
+    import torch
+    cfg, B, G = config(d, Hq, Hkv), len(lens), Hq // Hkv
+    case = synth.make_case("fp4n", [n + 1 for n in lens], Hq, Hkv, d, 0, seed=31)
+    K, V = (torch.from_numpy(x.copy()).view(torch.float16).cuda() for x in (case.K, case.V))
+    last = torch.from_numpy(case.cu_lens[1:] - 1).cuda()
+    cut = torch.ones(len(K), dtype=torch.bool, device="cuda")
+    cut[last] = False
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    i, j, l = sorted(np.argsort(lens)[-3:])                   # three sequences
+    k_at, v_at = int(cu[i] + 7), int(cu[j] + lens[j] - 1)     # by fill: the first one's head 1; the second one's head 0
+    Kf, Vf, Kn, Vn = K[cut].clone(), V[cut].clone(), K[last].clone(), V[last].clone()
+    Kf[k_at, 1, 33] = bad
+    Vf[v_at, 0, 20] = bad
+    Vn[l, 1, 5] = bad                                         # by the step: the third one
+    Kn[l, 0, d - 1] = bad
+    c = wide_cache(cfg, [n + 1 for n in lens], room or 256, extra=1)
+    c.fill(Kf, Vf, cu)
+    c.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    O = torch.zeros(B, Hq, d, device="cuda")
+    sa.decode_step(cfg, c.handle, up(case.Q), Kn, Vn, O, c.workspace)
+    want = torch.zeros(B, Hq, d, dtype=torch.bool)
+    want[i, G:2 * G] = True
+    want[j, :G, 16:32] = True
+    want[l, G:2 * G, :16] = True
+    want[l, :G] = True
+    assert torch.equal(O.isnan().cpu(), want) and O[~want.cuda()].isfinite().all()
+    Kr, Vr = (torch.zeros_like(K) for _ in "kv")
+    sa.read_kv(cfg, c.handle, None, case.cu_lens, Kr, Vr)
+    wk, wv = (torch.zeros(K.shape, dtype=torch.bool) for _ in "kv")
+    seq = case.cu_lens
+    wk[seq[i] + 7, 1, 32:48] = True
+    wk[seq[l + 1] - 1, 0, d - 16:] = True
+    wv[seq[j] + lens[j] - 1, 0, 16:32] = True
+    wv[seq[l + 1] - 1, 1, :16] = True
+    assert torch.equal(Kr.isnan().cpu(), wk) and torch.equal(Vr.isnan().cpu(), wv)
+
+
 def test_a_pool_beyond_32_bits():
     """Pages behind the first 4 GB of the pool: fill, append, decode, read."""
     import torch
