@@ -148,16 +148,17 @@ static bool stream_pays(const Plan& p, int batch, long long units, long long til
     if (!p.matrix || batch < 2 || batch > kRankedBatchMax || units < 16) return false;
     if (units * (tiles + stream_unit_cost(p.d, tile_shift(p.d, p.fp4))) >= (1LL << 30)) return false;       // (the kernel counts all tiles in 32 bits)
     const double rounds = (double)units * (double)tiles / ((double)sms * stream_shape(p.d, p.fp16, p.fp4).warps), u = (double)units / sms;
-    if (p.fp4) {
-        const long long room = (long long)sms * p.shape.blocks_per_sm;
-        if (S == 1 && units <= room && 5 * units >= 4 * room) return false;
-        return units >= (p.d == 64 ? 16 : 48) && rounds >= 2.0;
-    }
+    const long long slots = (long long)sms * p.shape.blocks_per_sm;
+    const bool fills = S == 1 && units <= slots && 5 * units >= 4 * slots;        // units that fill the other kernel's slots, once and unsplit
+    // 4-bit cache: the same on its own measurements, 127 shapes of 4 to 128 full sequences (300 to 32 768 tokens; GQA groups of 1 to 12), on which this misses
+    // the better kernel's time by 0.3 % on average, on 90 others by 0.6 % (always this kernel: 5.4 %, never: 3.2 %), on 90 ragged ones by 1.0 %.  us in a graph,
+    // the other kernel / this one: d = 64, 32 / 4 heads: 128 x 1024 tokens 19.3 / 24.1, 128 x 4096 44.8 / 52.2, 128 x 12 288 126 / 110, 32 x 4096 20.6 / 15.2,
+    // 32 x 8192 29.2 / 23.6; d = 128, 32 / 8 heads: 56 x 512 17.5 / 21.1, 40 x 3000 53.8 / 39.8, 32 x 5059 40.5 / 47.0, 72 x 8192 123 / 130, 96 x 8192 213 / 177.
+    if (p.fp4) return !fills && (p.d == 64 ? 0.72 * rounds + 2.15 * u + 2.35 : 0.6 * rounds + 5.0 * u + 3.5) <= cost + (S > 1 ? 5.6 : 0.0);
     if (rounds < (p.d == 128 && !p.fp16 ? 4.5 : 9.0)) return false;
     // binary16 tiles come at the copy rate in either kernel: nothing to gain on units that fill the other one's slots, once and unsplit
     // (d = 64, 64 x 4096 tokens 43.5 -> 45.3 us, 64 x 8192 83.5 -> 86.5; 64 x 1024 of 8192 11.5 -> 14.0)
-    const long long slots = (long long)sms * p.shape.blocks_per_sm;
-    if (p.fp16 && S == 1 && units <= slots && 5 * units >= 4 * slots) return false;
+    if (p.fp16 && fills) return false;
     // both in rounds of the other kernel, fitted to the same measurements
     if (p.d == 64) return 0.97 * rounds + 3.0 * u + 5.6 <= cost + (S > 1 ? 2.2 : 0.0) + 1.5;
     return 0.88 * rounds + 2.2 * u + 2.9 <= cost + (S > 1 ? 3.3 : 0.0) - 2.4;

@@ -147,7 +147,7 @@ def test_decode_against_64_bits(d, Hq, Hkv, lens, hadamard):
         assert n or not O[b].any()
 
 
-STREAM = [(64, 32, 4, MIX, 16384, False), (64, 32, 4, [777] * 30 + [9000] * 7, 16384, False), (64, 32, 4, [95] * 125 + [2000] * 3, 2048, True), (64, 16, 1, MIX * 2, 16384, True),
+STREAM = [(64, 32, 4, MIX, 16384, False), (64, 32, 4, [777] * 30 + [9000] * 7, 16384, False), (64, 32, 4, [95] * 125 + [2000] * 3, 16384, True), (64, 16, 1, MIX * 2, 16384, True),
           (64, 8, 1, [(37 * i) % 400 for i in range(128)], 16384, False), (128, 32, 8, MIX, 16384, False), (128, 16, 16, MIX[:12], 16384, True),
           (64, 5, 5, MIX * 2, 16384, False), (128, 64, 8, MIX, 16384, False)]
 
@@ -219,7 +219,7 @@ def test_unmapped_pages_are_skipped():
     assert (np.abs(O.cpu().numpy() - ref) <= fp4.tolerance(against, 64, 500)).all()
 
 
-FORMS = [(64, 32, 4, [0, 1, 31, 63, 64, 500], 0), (64, 5, 1, [40, 200], 0), (128, 28, 4, [900, 0, 64], 0), (64, 12, 2, MIX, 16384), (64, 8, 1, [2047], 0), (64, 32, 2, [33, 100], 0), (128, 32, 8, [0, 15, 128, 700], 0),
+FORMS = [(64, 32, 4, [0, 1, 31, 63, 64, 500], 0), (64, 5, 1, [40, 200], 0), (128, 28, 4, [900, 0, 64], 0), (64, 12, 2, MIX, 16384), (64, 32, 4, [95] * 125 + [2000] * 3, 2048), (64, 8, 1, [2047], 0), (64, 32, 2, [33, 100], 0), (128, 32, 8, [0, 15, 128, 700], 0),
          (128, 16, 16, [62, 63], 0), (64, 32, 4, MIX, 16384), (128, 32, 8, MIX, 16384), (64, 4, 4, [(7 * i) % 62 for i in range(130)], 0)]
 
 
