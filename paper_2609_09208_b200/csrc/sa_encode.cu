@@ -271,13 +271,14 @@ SA_D void fill_values(uint8_t* half, const CacheArgs& a, int t, const uint4* src
 }
 
 template <int D, int MODE, bool HAD>                          // HAD on its own: the rotation needs twice the registers
-__global__ void __launch_bounds__(128, MODE == 33 ? (D == 128 ? 6 : 8) : 1) fill_kernel(CacheArgs a, const uint16_t* __restrict__ Kin, const uint16_t* __restrict__ Vin,
+__global__ void __launch_bounds__(128, MODE == 33 ? (D == 128 && HAD ? 7 : 8) : 1) fill_kernel(CacheArgs a, const uint16_t* __restrict__ Kin, const uint16_t* __restrict__ Vin,
                                                    const __grid_constant__ FillSeqs seqs) {
     const int lane = threadIdx.x & 31;
     using Unit = std::conditional_t<MODE == 33, uint32_t, int64_t>;           // (a 64-bit division is a long routine; 4 bits: the host sees to it that 32 do)
     const Unit unit = (Unit)blockIdx.x * 4 + (threadIdx.x >> 5);              // (tile, head, keys or values)
-    const int tile = (int)(unit / (Unit)(2 * a.Hkv)), rest = (int)(unit % (Unit)(2 * a.Hkv));
-    const int head = rest >> 1;
+    constexpr int kParts = MODE == 33 ? Fp4Half<D>::PARTS : 1;
+    const Unit each = (Unit)(2 * kParts * a.Hkv);
+    const int tile = (int)(unit / each), rest = (int)(unit % each) / kParts, head = rest >> 1;
     if (tile >= seqs.tiles[seqs.n]) return;
     int i = 0;                                                                // the sequence: the last one that starts at or before the tile
     for (int j0 = 0; j0 < seqs.n; j0 += 32) {
@@ -291,7 +292,7 @@ __global__ void __launch_bounds__(128, MODE == 33 ? (D == 128 ? 6 : 8) : 1) fill
     if (!block) return;
     uint8_t* half = block + (size_t)((t % kPageTokens) >> 5) * (a.page_bytes >> 1);
     if constexpr (MODE == 33) {                                               // 4 bits: a lane has a block of 16 channels (sa_fp4.cuh)
-        fp4_fill<D, HAD>(half, a.v_off, rest & 1, ((rest & 1) ? Vin : Kin) + ((size_t)(seqs.row0[i] + t) * a.Hkv + head) * D, (size_t)a.Hkv * D, min(seqs.len[i] - t, kTileTokens), lane);
+        fp4_fill<D, HAD>(half, a.v_off, rest & 1, (int)(unit % kParts), ((rest & 1) ? Vin : Kin) + ((size_t)(seqs.row0[i] + t) * a.Hkv + head) * D, (size_t)a.Hkv * D, min(seqs.len[i] - t, kTileTokens), lane);
     } else {
         // the tile's rows, a 16-byte chunk per lane: whole 128-byte lines per load
         constexpr int C = D / 8, R = 32 / C;
@@ -521,7 +522,7 @@ sa_status sa_fill_kv(const sa_config* cfg, const sa_cache* cache, const uint16_t
             seqs.len[i] = (int)(cu_lens_host[b0 + i + 1] - cu_lens_host[b0 + i]);
             seqs.tiles[i + 1] = seqs.tiles[i] + (seqs.len[i] + kTileTokens - 1) / kTileTokens;
         }
-        const int64_t units = (int64_t)seqs.tiles[seqs.n] * 2 * a.Hkv;
+        const int64_t units = (int64_t)seqs.tiles[seqs.n] * 2 * a.Hkv * (!p.fp4 ? 1 : p.d == 64 ? Fp4Half<64>::PARTS : Fp4Half<128>::PARTS);
         if (units == 0) continue;
         if ((units + 3) / 4 > (p.fp4 ? 0x3fffffffLL : 0x7fffffffLL)) return SA_ERR_CAPACITY;
         const unsigned grid = (unsigned)((units + 3) / 4);

@@ -277,12 +277,13 @@ struct Fp4Half {
         if (mask) *p = mask == 0xffffffffu ? x : (x & mask) | (*p & ~mask);
     }
 };
-// The tile's first n tokens of K or V (rows of `pitch` elements) into the half page at `half`, whose value codes start at v_off.  What
-// belongs to other tokens stays as it is.  Keys in a rolled loop, the next token's block under way: unrolled, the code did not fit the instruction
+// Part `part` of the tile's first n tokens of K or V (rows of `pitch` elements) into the half page at `half`, whose value codes start at v_off.  What
+// belongs to other tokens stays as it is; the parts share no word.  Keys in a rolled loop, the next token's block under way: unrolled, the code did not fit the instruction
 // caches (20 001 tokens, 8 heads of 128, rotated: 46.7 -> 31.9 us, keys and values).
 template <int D, bool HAD>
-SA_D void fp4_fill(uint8_t* half, size_t v_off, bool values, const uint16_t* rows, size_t pitch, int n, int lane) {
+SA_D void fp4_fill(uint8_t* half, size_t v_off, bool values, int part, const uint16_t* rows, size_t pitch, int n, int lane) {
     using F = Fp4Half<D>;
+    const F f(lane, part);
     const bool wide = (reinterpret_cast<uintptr_t>(rows) & 31) == 0;
     auto load = [&](uint32_t (&x)[8], int t, int blk) {
 #pragma unroll
@@ -291,20 +292,18 @@ SA_D void fp4_fill(uint8_t* half, size_t v_off, bool values, const uint16_t* row
     };
     if (!values) {
         uint32_t next[2][8];
-        load(next[0], F(lane, 0).t8, F(lane, 0).blk);
-        load(next[1], F(lane, 0).t8 + 8, F(lane, 0).blk);
+        load(next[0], f.t8, f.blk);
+        load(next[1], f.t8 + 8, f.blk);
         uint32_t scales = 0, mask = 0;
-#pragma unroll(HAD ? 1 : 4 * F::PARTS)
-        for (int i = 0; i < 4 * F::PARTS; ++i) {
-            const int part = i >> 2, k = i & 3;
-            const F f(lane, part);
+#pragma unroll(HAD ? 1 : 4)
+        for (int k = 0; k < 4; ++k) {
             uint32_t x[8], w[2];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 x[e] = next[0][e];
                 next[0][e] = next[1][e];
             }
-            if (i + 2 < 4 * F::PARTS) load(next[1], F(lane, (i + 2) >> 2).t8 + 8 * ((i + 2) & 3), f.blk);
+            if (k < 2) load(next[1], f.t8 + 8 * (k + 2), f.blk);
             if constexpr (HAD) f.rotate(x);
             scales |= fp4_block(x, w) << (8 * k);
             if (8 * k + f.t8 < n) {
@@ -313,45 +312,38 @@ SA_D void fp4_fill(uint8_t* half, size_t v_off, bool values, const uint16_t* row
                 *reinterpret_cast<uint32_t*>(at + 512) = w[1];
                 mask |= 0xffu << (8 * k);
             }
-            if (k == 3) {
-                F::store_masked(f.key_scales(half), scales, mask);
-                scales = mask = 0;
-            }
         }
+        F::store_masked(f.key_scales(half), scales, mask);
         return;
     }
-#pragma unroll 1
-    for (int part = 0; part < F::PARTS; ++part) {
-        const F f(lane, part);
-        uint32_t in[4][8], w[4][2], scale[4];
+    uint32_t in[4][8], w[4][2], scale[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) load(in[k], f.t8 + 8 * k, f.blk);
+    for (int k = 0; k < 4; ++k) load(in[k], f.t8 + 8 * k, f.blk);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) scale[k] = fp4_block(in[k], w[k]);
-        uint8_t* v = half + v_off;
-        uint32_t out[4][2];
-        f.pair_tokens(w, out);
-        if (n == kTileTokens) {
+    for (int k = 0; k < 4; ++k) scale[k] = fp4_block(in[k], w[k]);
+    uint8_t* v = half + v_off;
+    uint32_t out[4][2];
+    f.pair_tokens(w, out);
+    if (n == kTileTokens) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) *reinterpret_cast<uint2*>(f.value_words(v, g)) = make_uint2(out[g][0], out[g][1]);
-        } else {
-            const uint32_t m0 = f.value_mask(0, n), m1 = f.value_mask(1, n);
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<uint2*>(f.value_words(v, g)) = make_uint2(out[g][0], out[g][1]);
+    } else {
+        const uint32_t m0 = f.value_mask(0, n), m1 = f.value_mask(1, n);
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                F::store_masked(f.value_words(v, g), out[g][0], m0);
-                F::store_masked(f.value_words(v, g) + 4, out[g][1], m1);
-            }
+        for (int g = 0; g < 4; ++g) {
+            F::store_masked(f.value_words(v, g), out[g][0], m0);
+            F::store_masked(f.value_words(v, g) + 4, out[g][1], m1);
         }
-        // scales: [t / 16][t % 2][t / 8 % 2]; the even token's lane stores those of the first 16 tokens, the odd one's the others
-        const bool odd = f.t8 & 1;
-        const uint32_t s0 = scale[0] | scale[1] << 8, s1 = scale[2] | scale[3] << 8;
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? s0 : s1, F::LPV);
-        uint32_t mask = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)                                          // byte i: t % 2 = i / 2, t / 8 % 2 = i % 2
-            if (16 * odd + 8 * (i & 1) + (f.t8 & ~1) + (i >> 1) < n) mask |= 0xffu << (8 * i);
-        F::store_masked(f.value_scales(v) + 4 * odd, odd ? other | s1 << 16 : s0 | other << 16, mask);
     }
+    // scales: [t / 16][t % 2][t / 8 % 2]; the even token's lane stores those of the first 16 tokens, the odd one's the others
+    const bool odd = f.t8 & 1;
+    const uint32_t s0 = scale[0] | scale[1] << 8, s1 = scale[2] | scale[3] << 8;
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? s0 : s1, F::LPV);
+    uint32_t mask = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)                                              // byte i: t % 2 = i / 2, t / 8 % 2 = i % 2
+        if (16 * odd + 8 * (i & 1) + (f.t8 & ~1) + (i >> 1) < n) mask |= 0xffu << (8 * i);
+    F::store_masked(f.value_scales(v) + 4 * odd, odd ? other | s1 << 16 : s0 | other << 16, mask);
 }
 // The way back: tokens first .. end - 1 of the half page to their rows (rows: that of token 0, from which only these are touched).
 template <int D, bool HAD>
