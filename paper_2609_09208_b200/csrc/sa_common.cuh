@@ -265,6 +265,27 @@ SA_D f32x2 add2(f32x2 a, f32x2 b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
+// 32 bytes of global memory, in one piece where the address allows (wide): rows of 16-byte pieces 32 bytes apart fill every sector in two goes.
+// (volatile: stays behind the wait for the kernel in front)
+SA_D void load_32_bytes(const void* p, bool wide, uint32_t (&x)[8]) {
+    if (wide) {
+        asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+            : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7])
+            : "l"(p));
+    } else {
+        const uint4 a = __ldg(static_cast<const uint4*>(p)), b = __ldg(static_cast<const uint4*>(p) + 1);
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    }
+}
+SA_D void store_32_bytes(void* p, bool wide, const uint32_t (&x)[8]) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7])
+                     : "memory");
+    } else {
+        static_cast<uint4*>(p)[0] = make_uint4(x[0], x[1], x[2], x[3]);
+        static_cast<uint4*>(p)[1] = make_uint4(x[4], x[5], x[6], x[7]);
+    }
+}
 SA_D unsigned long long pack_f32x2(float lo, float hi) {
     unsigned long long r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));

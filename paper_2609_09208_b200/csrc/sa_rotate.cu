@@ -5,14 +5,15 @@
 // output written once); single tokens by latency.
 //
 // d / (2 P) lanes share a head vector; a lane holds two pieces of P channels whose pairs lie in the lane: pairing halves, channels
-// u .. u + P - 1 and their partners; pairing neighbours, 2 P channels in a row.  So the rotation needs no exchange, the norm one
-// sum over the lanes.  P = 8, 16-byte loads; 4 where halves are no multiple of 8 channels.  The angles are the same for all heads: each is worked out by one thread
-// of the block, in 64 bits up to the fraction of a turn (position times frequency in 32 bits would be off by 0.01 rad at position
+// u .. u + P - 1 and their partners; pairing neighbours, any two.  So the rotation needs no exchange, the norm one
+// sum over the lanes.  P = 8, 16-byte loads, 32-byte ones of FP32; 4 where halves are no multiple of 8 channels.  The pieces of the lanes follow one another in
+// memory (FP32, neighbours, 5001 tokens of 16 / 16 heads of 128: with two pieces of a lane in a row and 16-byte loads 39.7 us, so 32.6: 5.7 TB/s).  The angles are the same for
+// all heads: each is worked out by one thread of the block, in 64 bits up to the fraction of a turn (position times frequency in 32 bits would be off by 0.01 rad at position
 // 131 072), while the first vectors are on their way, and handed over in shared memory.
 // The threads of a block are dealt to tokens, and a thread stays with its token: the weights of a projection stay in its registers, packed FP32
 // pairs do the arithmetic.  Decode steps: a block of 256 threads per token; prompts: 8 tokens of a block (4 at head_dim 128), so that all
 // lanes have several vectors, the next one under way while one is worked on.  What is left above the copy rate are instructions, 14 for a channel.  us, 32 / 8 heads
-// of 128: 8192 tokens in bfloat16 with norms 51.1 -> 39.4 (5.1 TB/s), in FP32 53.7 (5.6 TB/s); one token of 32 / 4 heads of 64 2.0.  With sines and cosines
+// of 128: 8192 tokens in bfloat16 with norms 51.1 -> 39.4 (5.1 TB/s), in FP32 53.4 (5.7 TB/s); one token of 32 / 4 heads of 64 2.0.  With sines and cosines
 // in registers (fewer threads) 42.6, with their negatives in a third table 41.5.
 #include "sa_cache_write.cuh"
 #include "sa_common.cuh"
@@ -31,6 +32,7 @@ struct RotateArgs {
     const uint8_t* pair_axis;             // [R / 2] or null
     int64_t n;
     int heads[3], R, axes, norm, neighbours;
+    int wide;                             // bit i: rows of in[i] start on 32-byte boundaries
     float eps, scale;
 };
 constexpr int kRotateThreads = 256;
@@ -41,8 +43,9 @@ template <typename T, int P>
 struct Piece {
     static constexpr int kWords = P * (int)sizeof(T) / 4;
     uint32_t w[kWords];
-    SA_D void load(const T* p) {
-        if constexpr (kWords == 2) {
+    SA_D void load(const T* p, bool wide) {                   // wide: p is a multiple of 32 bytes
+        if constexpr (kWords == 8) load_32_bytes(p, wide, w);
+        else if constexpr (kWords == 2) {
             const uint2 v = *reinterpret_cast<const uint2*>(p);
             w[0] = v.x, w[1] = v.y;
         } else
@@ -85,8 +88,8 @@ __global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 4 ? 3 : 4) rotate
     const int64_t token0 = (int64_t)blockIdx.x * TOKENS;
     const int slot = TOKENS == 1 ? 0 : threadIdx.x / THREADS, l = threadIdx.x % L, half = a.R / 2;
     const int64_t token = token0 + slot;
-    const int pa = NEIGHBOURS ? 2 * P * l : P * l < half ? P * l : a.R + P * l - half;                               // first channels of the pieces
-    const int pb = NEIGHBOURS ? 2 * P * l + P : P * l < half ? P * l + half : (a.R + D) / 2 + P * l - half;
+    const int pa = NEIGHBOURS || P * l < half ? P * l : a.R + P * l - half;                                          // first channels of the pieces
+    const int pb = NEIGHBOURS ? D / 2 + P * l : P * l < half ? P * l + half : (a.R + D) / 2 + P * l - half;
     const uint32_t mine = ((1u << L) - 1u) << (threadIdx.x & 31 & ~(L - 1));       // the lanes of this vector
     const int per = token < a.n ? a.heads[0] + a.heads[1] + a.heads[2] : 0;
     Piece<T, P> first, second;
@@ -95,8 +98,9 @@ __global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 4 ? 3 : 4) rotate
     auto load = [&](int v) {                                                       // vector v of the token
         const int kind = kind_of(v);
         const T* in = static_cast<const T*>(a.in[kind]) + token * a.stride[kind] + head_of(v, kind) * D;
-        first.load(in + pa);
-        second.load(in + pb);
+        const bool wide = a.wide >> kind & 1;
+        first.load(in + pa, wide);
+        second.load(in + pb, wide);
     };
     int v = threadIdx.x % THREADS / L;
     pdl_wait();                                                                    // the projections may come from the kernel before
@@ -142,8 +146,8 @@ __global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 4 ? 3 : 4) rotate
                 const f32x2 rr = pack_f32x2(r, r);
                 if (weights_of != kind && a.weight[kind]) {
                     weights_of = kind;
-                    wa.load(static_cast<const T*>(a.weight[kind]) + pa);
-                    wb.load(static_cast<const T*>(a.weight[kind]) + pb);
+                    wa.load(static_cast<const T*>(a.weight[kind]) + pa, false);
+                    wb.load(static_cast<const T*>(a.weight[kind]) + pb, false);
                 }
 #pragma unroll
                 for (int i = 0; i < H; ++i) {
@@ -191,7 +195,7 @@ __global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 4 ? 3 : 4) rotate
 
 template <int D, typename T, int P, bool NEIGHBOURS>
 static void launch_rotate(const RotateArgs& a, cudaStream_t s) {
-        constexpr int kTokens = D == 64 ? 8 : 4;
+    constexpr int kTokens = D == 64 ? 8 : 4;
     const dim3 block(kRotateThreads);
     if (a.n <= 512) (void)launch_pdl(rotate_kernel<D, T, P, 1, NEIGHBOURS>, dim3((unsigned)a.n), block, 0, s, a);
     else (void)launch_pdl(rotate_kernel<D, T, P, kTokens, NEIGHBOURS>, dim3((unsigned)((a.n + kTokens - 1) / kTokens)), block, 0, s, a);
@@ -234,6 +238,7 @@ extern "C" sa_status sa_rotate_qkv(const sa_config* cfg, const sa_rotary* rot, c
         a.in[i] = in[i];
         a.out[i] = out[i];
         a.stride[i] = stride[i];
+        a.wide |= (aligned(in[i], 32) && (n == 1 || stride[i] * size % 32 == 0) ? 1 : 0) << i;
         total += a.heads[i];
     }
     if (total == 0) return SA_ERR_INVALID_ARG;
