@@ -7,7 +7,9 @@ namespace sa {
 
 // One warp takes the keys or the values of one KV head for the 32 tokens of half a page, lane = token, as the fill does: its loads are
 // the 16-byte chunks of the half, 512 contiguous bytes each, and the rows are turned in shared memory, so that whole
-// 128-byte lines are stored.  Bound by memory: the records read and 2 d bytes written for a key or value.
+// 128-byte lines are stored.  Bound by memory: the records read and 2 d bytes written for a key or value.  All of a vector's chunks are asked for at
+// once, with as many registers as 9 blocks on an SM leave (8 at head_dim 128): 8 x 16 384 tokens of PoT-M4, 4 heads of 64, 39.4 -> 33.6 us (6.1 TB/s), of 8 x 8192 of INT8
+// 21.8 -> 18.4, against a register bound of the compiler's choice and chunks by two; 8 heads of 128, 8192 tokens 13.9 -> 12.7; 11 blocks 37.5 and 20.8.
 constexpr int kReadBatch = 64;            // sequences per launch
 struct ReadSeqs {
     int64_t row0[kReadBatch];             // row of the sequence's first token in K / V
@@ -121,7 +123,7 @@ SA_D void read_keys(const uint8_t* half, const CacheArgs& a, int t, uint4* row) 
             row[c ^ (t & 7)] = make_uint4(half2_bits(x[8 * c], x[8 * c + 1]), half2_bits(x[8 * c + 2], x[8 * c + 3]),
                                           half2_bits(x[8 * c + 4], x[8 * c + 5]), half2_bits(x[8 * c + 6], x[8 * c + 7]));
     } else {
-#pragma unroll 8
+#pragma unroll
         for (int c = 0; c < D / 8; ++c) {
             float x[8];
             key.get(c, x);
@@ -139,7 +141,7 @@ SA_D void read_values(const uint8_t* half, const CacheArgs& a, int t, uint4* row
         // times 2^-g in two exact steps: the first keeps clear of the subnormal numbers, the second rounds where the value is one
         const int g = (int)(int8_t)half[a.meta_off + t * 4 + 2], g1 = max(-10, min(g, 12));
         const uint32_t f1 = half2_bits(pow2i(-g1), pow2i(-g1)), f2 = half2_bits(pow2i(max(g1 - g, -40)), pow2i(max(g1 - g, -40)));
-#pragma unroll 2
+#pragma unroll
         for (int k = 0; k < D / 16; ++k) {
             const uint4 in = __ldg(reinterpret_cast<const uint4*>(v + ((size_t)k * kTileTokens + t) * 16));
             const uint32_t w[4] = {in.x, in.y, in.z, in.w};
@@ -157,7 +159,7 @@ SA_D void read_values(const uint8_t* half, const CacheArgs& a, int t, uint4* row
 }
 
 template <int D, int MODE, bool HAD>
-__global__ void __launch_bounds__(128) read_kernel(CacheArgs a, uint16_t* __restrict__ Kout, uint16_t* __restrict__ Vout, const __grid_constant__ ReadSeqs seqs) {
+__global__ void __launch_bounds__(128, HAD ? 0 : D == 64 ? 9 : 8) read_kernel(CacheArgs a, uint16_t* __restrict__ Kout, uint16_t* __restrict__ Vout, const __grid_constant__ ReadSeqs seqs) {
     const int lane = threadIdx.x & 31;
     const int parts = Kout && Vout ? 2 : 1;
     const uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 5), each = (uint32_t)(parts * a.Hkv);      // (tile, head, keys or values)
