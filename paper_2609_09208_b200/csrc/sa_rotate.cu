@@ -7,14 +7,15 @@
 // d / (2 P) lanes share a head vector; a lane holds two pieces of P channels whose pairs lie in the lane: pairing halves, channels
 // u .. u + P - 1 and their partners; pairing neighbours, any two.  So the rotation needs no exchange, the norm one
 // sum over the lanes.  P = 8, 16-byte loads, 32-byte ones of FP32; 4 where halves are no multiple of 8 channels.  The pieces of the lanes follow one another in
-// memory (FP32, neighbours, 5001 tokens of 16 / 16 heads of 128: with two pieces of a lane in a row and 16-byte loads 39.7 us, so 32.6: 5.7 TB/s).  The angles are the same for
+// memory (FP32, neighbours, 5001 tokens of 16 / 16 heads of 128: with two pieces of a lane in a row and 16-byte loads 39.7 us, so 31.9: 5.8 TB/s).  The angles are the same for
 // all heads: each is worked out by one thread of the block, in 64 bits up to the fraction of a turn (position times frequency in 32 bits would be off by 0.01 rad at position
 // 131 072), while the first vectors are on their way, and handed over in shared memory.
 // The threads of a block are dealt to tokens, and a thread stays with its token: the weights of a projection stay in its registers, packed FP32
-// pairs do the arithmetic.  Decode steps: a block of 256 threads per token; prompts: 8 tokens of a block (4 at head_dim 128), so that all
+// pairs do the arithmetic.  Decode steps: a block of 256 threads per token (one of 128: 2.0 -> 2.2 us); prompts: 128 threads, 4 tokens of a block (2 at head_dim 128), so that all
 // lanes have several vectors, the next one under way while one is worked on.  What is left above the copy rate are instructions, 14 for a channel.  us, 32 / 8 heads
-// of 128: 8192 tokens in bfloat16 with norms 51.1 -> 39.4 (5.1 TB/s), in FP32 53.4 (5.7 TB/s); one token of 32 / 4 heads of 64 2.0.  With sines and cosines
-// in registers (fewer threads) 42.6, with their negatives in a third table 41.5.
+// of 128: 8192 tokens in bfloat16 with norms 51.1 -> 38.1 (5.3 TB/s), in FP32 51.6 (5.9 TB/s), 1024 tokens 6.5; one token of 32 / 4 heads of 64 2.0.  Of 8192 tokens: 256 threads with twice the
+// tokens 39.4, 64 threads 37.8 (but 1024 tokens 8.7), two vectors under way 41.3, other register bounds 42 to 46, sines and cosines in registers (fewer threads) 42.6, with their negatives
+// in a third table 41.5.
 #include "sa_cache_write.cuh"
 #include "sa_common.cuh"
 #include <cuda_bf16.h>
@@ -35,7 +36,7 @@ struct RotateArgs {
     int wide;                             // bit i: rows of in[i] start on 32-byte boundaries
     float eps, scale;
 };
-constexpr int kRotateThreads = 256;
+SA_HD constexpr int rotate_threads(int tokens) { return tokens == 1 ? 256 : 128; }
 constexpr int kRotateMost = 64;           // pairs
 
 // P channels as they lie in memory, and as pairs of FP32.
@@ -82,8 +83,8 @@ SA_D void store_halves(uint16_t* p, const f32x2 (&x)[P / 2]) {
 
 // TOKENS: of a block.  NEIGHBOURS: how channels pair.
 template <int D, typename T, int P, int TOKENS, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 4 ? 3 : 4) rotate_kernel(const __grid_constant__ RotateArgs a) {
-    constexpr int L = D / (2 * P), THREADS = kRotateThreads / TOKENS, GROUPS = THREADS / L, H = P / 2;   // lanes of a vector; threads, vectors of a token
+__global__ void __launch_bounds__(rotate_threads(TOKENS), (sizeof(T) == 4 ? 3 : 4) * 256 / rotate_threads(TOKENS)) rotate_kernel(const __grid_constant__ RotateArgs a) {
+    constexpr int L = D / (2 * P), THREADS = rotate_threads(TOKENS) / TOKENS, GROUPS = THREADS / L, H = P / 2;   // lanes of a vector; threads, vectors of a token
     __shared__ __align__(16) float turn[TOKENS][2][kRotateMost];                               // scale * cos, scale * sin of every pair
     const int64_t token0 = (int64_t)blockIdx.x * TOKENS;
     const int slot = TOKENS == 1 ? 0 : threadIdx.x / THREADS, l = threadIdx.x % L, half = a.R / 2;
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 4 ? 3 : 4) rotate
     pdl_wait();                                                                    // the projections may come from the kernel before
     if (v < per) load(v);
     const int tokens = TOKENS == 1 ? 1 : (int)min((int64_t)TOKENS, a.n - token0);
-    for (int i = threadIdx.x; i < half * tokens; i += kRotateThreads) {
+    for (int i = threadIdx.x; i < half * tokens; i += rotate_threads(TOKENS)) {
         const int j = TOKENS == 1 ? i : i % half, k = TOKENS == 1 ? 0 : i / half;
         const int axis = a.pair_axis ? min((int)a.pair_axis[j], a.axes - 1) : 0;
         const double turns = (double)a.positions[axis * a.n + token0 + k] * (double)a.inv_freq[j] * 0.15915494309189535;
@@ -195,10 +196,9 @@ __global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 4 ? 3 : 4) rotate
 
 template <int D, typename T, int P, bool NEIGHBOURS>
 static void launch_rotate(const RotateArgs& a, cudaStream_t s) {
-    constexpr int kTokens = D == 64 ? 8 : 4;
-    const dim3 block(kRotateThreads);
-    if (a.n <= 512) (void)launch_pdl(rotate_kernel<D, T, P, 1, NEIGHBOURS>, dim3((unsigned)a.n), block, 0, s, a);
-    else (void)launch_pdl(rotate_kernel<D, T, P, kTokens, NEIGHBOURS>, dim3((unsigned)((a.n + kTokens - 1) / kTokens)), block, 0, s, a);
+    constexpr int kTokens = D == 64 ? 4 : 2;
+    if (a.n <= 512) (void)launch_pdl(rotate_kernel<D, T, P, 1, NEIGHBOURS>, dim3((unsigned)a.n), dim3(rotate_threads(1)), 0, s, a);
+    else (void)launch_pdl(rotate_kernel<D, T, P, kTokens, NEIGHBOURS>, dim3((unsigned)((a.n + kTokens - 1) / kTokens)), dim3(rotate_threads(kTokens)), 0, s, a);
 }
 template <int D, typename T>
 static void launch_rotate(const RotateArgs& a, cudaStream_t s) {
