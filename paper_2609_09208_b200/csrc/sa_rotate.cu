@@ -197,7 +197,8 @@ __global__ void __launch_bounds__(rotate_threads(TOKENS), (sizeof(T) == 4 ? 3 : 
 template <int D, typename T, int P, bool NEIGHBOURS>
 static void launch_rotate(const RotateArgs& a, cudaStream_t s) {
     constexpr int kTokens = D == 64 ? 4 : 2;
-    if (a.n <= 512) (void)launch_pdl(rotate_kernel<D, T, P, 1, NEIGHBOURS>, dim3((unsigned)a.n), dim3(rotate_threads(1)), 0, s, a);
+    // one wave of blocks with a token each, while they fit: 32 / 8 heads of 128, 256 tokens 3.8 us (4.8 with blocks of several), 513 4.7 (5.5), 700 7.4 (5.9)
+    if (a.n <= (int64_t)sm_count() * (sizeof(T) == 4 ? 3 : 4)) (void)launch_pdl(rotate_kernel<D, T, P, 1, NEIGHBOURS>, dim3((unsigned)a.n), dim3(rotate_threads(1)), 0, s, a);
     else (void)launch_pdl(rotate_kernel<D, T, P, kTokens, NEIGHBOURS>, dim3((unsigned)((a.n + kTokens - 1) / kTokens)), dim3(rotate_threads(kTokens)), 0, s, a);
 }
 template <int D, typename T>
