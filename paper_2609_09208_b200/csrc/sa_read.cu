@@ -9,7 +9,7 @@ namespace sa {
 // the 16-byte chunks of the half, 512 contiguous bytes each, and the rows are turned in shared memory, so that whole
 // 128-byte lines are stored.  Bound by memory: the records read and 2 d bytes written for a key or value.  All of a vector's chunks are asked for at
 // once, with as many registers as 9 blocks on an SM leave (8 at head_dim 128): 8 x 16 384 tokens of PoT-M4, 4 heads of 64, 39.4 -> 33.6 us (6.1 TB/s), of 8 x 8192 of INT8
-// 21.8 -> 18.4, against a register bound of the compiler's choice and chunks by two; 8 heads of 128, 8192 tokens 13.9 -> 12.7; 11 blocks 37.5 and 20.8.
+// 21.8 -> 18.4, against a register bound of the compiler's choice and chunks by two; 8 heads of 128, 8192 tokens 13.9 -> 12.7; 11 blocks 37.5 and 20.8.  (Not of 4 bits at head_dim 128: no faster, and a read of the new tokens behind a step takes 0.6 us longer.)
 constexpr int kReadBatch = 64;            // sequences per launch
 struct ReadSeqs {
     int64_t row0[kReadBatch];             // row of the sequence's first token in K / V
@@ -159,7 +159,7 @@ SA_D void read_values(const uint8_t* half, const CacheArgs& a, int t, uint4* row
 }
 
 template <int D, int MODE, bool HAD>
-__global__ void __launch_bounds__(128, HAD ? 0 : D == 64 ? 9 : 8) read_kernel(CacheArgs a, uint16_t* __restrict__ Kout, uint16_t* __restrict__ Vout, const __grid_constant__ ReadSeqs seqs) {
+__global__ void __launch_bounds__(128, HAD || (MODE == 33 && D == 128) ? 0 : D == 64 ? 9 : 8) read_kernel(CacheArgs a, uint16_t* __restrict__ Kout, uint16_t* __restrict__ Vout, const __grid_constant__ ReadSeqs seqs) {
     const int lane = threadIdx.x & 31;
     const int parts = Kout && Vout ? 2 : 1;
     const uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 5), each = (uint32_t)(parts * a.Hkv);      // (tile, head, keys or values)
