@@ -136,6 +136,27 @@ def test_in_place_empty_and_extreme_inputs():
     assert torch.equal(out, V.half())
 
 
+@pytest.mark.parametrize("neighbours", [False, True])
+@pytest.mark.parametrize("d,n,extra", [(64, 5, 0), (64, 700, 4), (128, 700, 0), (128, 3, 4)])
+def test_rows_that_start_between_32_byte_places(d, n, extra, neighbours):
+    """FP32 projections on 16-byte boundaries only, by their address or by their stride: the same bits as from aligned ones."""
+    import torch
+    cfg, wide = sa.make_config(d, 4, 2, sa.SA_POTM4), 8 * d + extra
+    torch.manual_seed(d + n)
+    x = torch.randn(n, 8 * d, device="cuda")
+    rot = sa.Rotary(cfg, torch.from_numpy(frequencies(d)).cuda(), dtype=torch.float32, pairs="neighbours" if neighbours else "halves", norm=True, eps=1e-6)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    got = []
+    for first in (0, 4):
+        room = torch.empty(n * wide + 8, device="cuda")[first:first + n * wide].view(n, wide)[:, :8 * d] if first else x
+        room.copy_(x)
+        out = [torch.full((n, h, d), 7.0, dtype=torch.float16, device="cuda") for h in (4, 2, 2)]
+        q, k, v = (part.unflatten(-1, (-1, d)) for part in room.split([4 * d, 2 * d, 2 * d], -1))
+        sa.rotate_qkv(rot, q, k, v, pos, *out)
+        got.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_rows_beyond_32_bits():
     """Tokens whose places in input and output are beyond 2^31 elements."""
     import torch
