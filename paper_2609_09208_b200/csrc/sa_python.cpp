@@ -103,7 +103,7 @@ struct Args {
     // dtype: exactly that type; null: any of `itemsize` bytes
     bool typed(PyObject* o, PyObject* dtype, unsigned long long itemsize) {
         PyObject* t = bad ? nullptr : PyObject_GetAttr(o, g_dtype);
-        bool ok = t && (dtype ? t == dtype : (itemsize == 2 && t == g_float16) || (itemsize == 4 && t == g_int32));
+        bool ok = t && (dtype ? t == dtype : itemsize == 2 && t == g_float16);
         if (t && !ok && !dtype) ok = number_of(PyObject_GetAttr(t, g_itemsize)) == itemsize;
         Py_XDECREF(t);
         return ok;
@@ -317,7 +317,7 @@ PyObject* rotate_qkv(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     if (!a.bad && pos != Py_None) {
         const bool two = a.shape(pos, 2, sh);
         if (two ? sh[0] != rot->n_axes || (n >= 0 && sh[1] != n) : rot->n_axes != 1 || !a.shape(pos, 1, sh) || (n >= 0 && sh[0] != n)) a.fail("positions are [n_axes, n]");
-        else if (!a.typed(pos, nullptr, 4) || !a.contiguous(pos) || !a.on_device(pos, dev)) a.fail("positions are contiguous 4-byte integers on the current CUDA device");
+        else if (!a.typed(pos, g_int32, 0) || !a.contiguous(pos) || !a.on_device(pos, dev)) a.fail("positions are contiguous int32 on the current CUDA device");
         positions = a.address<const int32_t>(pos);
     }
     for (int i = 0; i < 3 && !a.bad; ++i) {
