@@ -11,7 +11,7 @@
 
 namespace {
 
-PyObject *g_data_ptr, *g_nbytes, *g_get_device, *g_get_stream, *g_shape, *g_stride, *g_is_contiguous, *g_dtype, *g_itemsize, *g_device_of, *g_float16, *g_int32;
+PyObject *g_data_ptr, *g_nbytes, *g_get_device, *g_get_stream, *g_shape, *g_stride, *g_is_contiguous, *g_dtype, *g_device_of, *g_float16, *g_int16, *g_uint16, *g_int32;
 
 struct Args {
     PyObject* const* v;
@@ -100,11 +100,16 @@ struct Args {
         Py_XDECREF(d);
         return ok;
     }
-    // dtype: exactly that type; null: any of `itemsize` bytes
-    bool typed(PyObject* o, PyObject* dtype, unsigned long long itemsize) {
+    bool typed(PyObject* o, PyObject* dtype) {
         PyObject* t = bad ? nullptr : PyObject_GetAttr(o, g_dtype);
-        bool ok = t && (dtype ? t == dtype : itemsize == 2 && t == g_float16);
-        if (t && !ok && !dtype) ok = number_of(PyObject_GetAttr(t, g_itemsize)) == itemsize;
+        const bool ok = t && t == dtype;
+        Py_XDECREF(t);
+        return ok;
+    }
+    // binary16, or 16-bit integers as a container of its bits (other types of two bytes would read the bits as other numbers)
+    bool binary16(PyObject* o) {
+        PyObject* t = bad ? nullptr : PyObject_GetAttr(o, g_dtype);
+        const bool ok = t && (t == g_float16 || t == g_int16 || t == g_uint16);
         Py_XDECREF(t);
         return ok;
     }
@@ -281,8 +286,8 @@ PyObject* read_kv(PyObject*, PyObject* const* v, Py_ssize_t n) {
         PyObject* o = a.next();
         if (a.bad || o == Py_None) continue;
         long long sh[3];
-        if (!a.shape(o, 3, sh) || sh[1] != cfg->n_kv_heads || sh[2] != cfg->head_dim || sh[0] < cu.p[batch] || !a.typed(o, nullptr, 2) || !a.contiguous(o) || !a.on_device(o, dev))
-            a.fail("K and V are contiguous [rows, n_kv_heads, head_dim] of 2-byte numbers on the current CUDA device, with a row for every token");
+        if (!a.shape(o, 3, sh) || sh[1] != cfg->n_kv_heads || sh[2] != cfg->head_dim || sh[0] < cu.p[batch] || !a.binary16(o) || !a.contiguous(o) || !a.on_device(o, dev))
+            a.fail("K and V are contiguous [rows, n_kv_heads, head_dim] of float16 (or int16, uint16 for its bits) on the current CUDA device, with a row for every token");
         out[i] = a.address<uint16_t>(o);
     }
     const sa_stream s = a.stream();
@@ -306,7 +311,7 @@ PyObject* rotate_qkv(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
         if (a.bad || o == Py_None) continue;
         const long long H = i == 0 ? cfg->n_q_heads : cfg->n_kv_heads;
         if (!a.shape(o, 3, sh) || sh[1] != H || sh[2] != d || (n >= 0 && sh[0] != n) || !a.strides(o, 3, step) || (H > 1 && step[1] != d) || step[2] != 1 ||
-            !a.typed(o, dtype, 0) || !a.on_device(o, dev))
+            !a.typed(o, dtype) || !a.on_device(o, dev))
             a.fail("Q, K and V are [n, heads, head_dim] of the rotary's dtype on the current CUDA device, a token's heads one after another, n the same for all");
         n = sh[0];
         stride[i] = n > 1 ? step[0] : H * d;
@@ -317,14 +322,14 @@ PyObject* rotate_qkv(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     if (!a.bad && pos != Py_None) {
         const bool two = a.shape(pos, 2, sh);
         if (two ? sh[0] != rot->n_axes || (n >= 0 && sh[1] != n) : rot->n_axes != 1 || !a.shape(pos, 1, sh) || (n >= 0 && sh[0] != n)) a.fail("positions are [n_axes, n]");
-        else if (!a.typed(pos, g_int32, 0) || !a.contiguous(pos) || !a.on_device(pos, dev)) a.fail("positions are contiguous int32 on the current CUDA device");
+        else if (!a.typed(pos, g_int32) || !a.contiguous(pos) || !a.on_device(pos, dev)) a.fail("positions are contiguous int32 on the current CUDA device");
         positions = a.address<const int32_t>(pos);
     }
     for (int i = 0; i < 3 && !a.bad; ++i) {
         PyObject* o = a.next();
         if (a.bad || o == Py_None) continue;
-        if (!a.shape(o, 3, sh) || sh[0] != n || sh[1] != (i == 0 ? cfg->n_q_heads : cfg->n_kv_heads) || sh[2] != d || !a.typed(o, nullptr, 2) || !a.contiguous(o) || !a.on_device(o, dev))
-            a.fail("the outputs are contiguous [n, heads, head_dim] of 2-byte numbers on the current CUDA device, one for each of Q, K and V that is given");
+        if (!a.shape(o, 3, sh) || sh[0] != n || sh[1] != (i == 0 ? cfg->n_q_heads : cfg->n_kv_heads) || sh[2] != d || !a.binary16(o) || !a.contiguous(o) || !a.on_device(o, dev))
+            a.fail("the outputs are contiguous [n, heads, head_dim] of float16 (or int16, uint16 for its bits) on the current CUDA device, one for each of Q, K and V that is given");
         out[i] = a.address<uint16_t>(o);
     }
     // (a tensor without elements has no address, which would read as one that is not there)
@@ -361,11 +366,12 @@ PyMODINIT_FUNC PyInit__native(void) {
     g_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     PyObject* torch = PyImport_ImportModule("torch");
     g_float16 = torch ? PyObject_GetAttrString(torch, "float16") : nullptr;
+    g_int16 = torch ? PyObject_GetAttrString(torch, "int16") : nullptr;
+    g_uint16 = torch ? PyObject_GetAttrString(torch, "uint16") : nullptr;
     g_int32 = torch ? PyObject_GetAttrString(torch, "int32") : nullptr;
     Py_XDECREF(torch);
     g_dtype = PyUnicode_InternFromString("dtype");
-    g_itemsize = PyUnicode_InternFromString("itemsize");
     g_device_of = PyUnicode_InternFromString("get_device");
-    if (!g_get_device || !g_get_stream || !g_data_ptr || !g_nbytes || !g_shape || !g_stride || !g_is_contiguous || !g_float16 || !g_int32 || !g_dtype || !g_itemsize || !g_device_of) return nullptr;
+    if (!g_get_device || !g_get_stream || !g_data_ptr || !g_nbytes || !g_shape || !g_stride || !g_is_contiguous || !g_float16 || !g_int16 || !g_uint16 || !g_int32 || !g_dtype || !g_device_of) return nullptr;
     return PyModule_Create(&kModule);
 }

@@ -67,3 +67,11 @@ def test_positions_are_32_bit_integers():
     got = outcomes("{str(t): rotate(positions=t) for t in (torch.int32, torch.float32, torch.uint32, torch.int64, torch.float16)}")
     assert got.pop("torch.int32") == 3
     assert set(got.values()) == {"refused"}, got
+
+
+def test_outputs_are_binary16_or_their_bits():
+    """A bfloat16 tensor of the right size would come back full of binary16 patterns."""
+    got = outcomes("{str(t): (rotate(out=t), read(t)) for t in (torch.float16, torch.int16, torch.uint16, torch.bfloat16, torch.float32, torch.uint8, torch.complex32)}")
+    for bits in ("float16", "int16", "uint16"):
+        assert got.pop("torch." + bits) == (3, 3), bits
+    assert set(got.values()) == {("refused", "refused")}, got
