@@ -201,6 +201,9 @@ __global__ void __launch_bounds__(128, HAD || (MODE == 33 && D == 128) ? 0 : D =
     }
 }
 
+// Half pages that tokens start .. start + n - 1 lie in (their end may be 2^31 - 1: no sums in 32 bits).
+static int64_t half_pages(int64_t start, int64_t n) { return n ? (start + n + kTileTokens - 1) / kTileTokens - start / kTileTokens : 0; }
+
 template <int D, int MODE, bool HAD>
 static void launch_read(const CacheArgs& a, uint16_t* K, uint16_t* V, const ReadSeqs& seqs, unsigned grid, cudaStream_t s) {
     (void)launch_pdl(read_kernel<D, MODE, HAD>, dim3(grid), dim3(128), 0, s, a, K, V, seqs);
@@ -244,7 +247,7 @@ extern "C" sa_status sa_read_kv(const sa_config* cfg, const sa_cache* cache, con
         const int64_t n = cu_lens_host[b + 1] - cu_lens_host[b], start = starts_host ? starts_host[b] : 0;
         if (n < 0 || cu_lens_host[b] < 0 || start < 0) return SA_ERR_INVALID_ARG;
         if (start > most || n > most - start) return SA_ERR_CAPACITY;
-        if (n) tiles += (start + n + kTileTokens - 1) / kTileTokens - start / kTileTokens;
+        tiles += half_pages(start, n);
     }
     const int parts = K && V ? 2 : 1;
     if (tiles * parts * a.Hkv > 0xfffffff0LL || tiles > 0x7fffffffLL) return SA_ERR_CAPACITY;      // (of all launches together: none is made before the last check)
@@ -259,7 +262,7 @@ extern "C" sa_status sa_read_kv(const sa_config* cfg, const sa_cache* cache, con
             seqs.row0[i] = cu_lens_host[b0 + i];
             seqs.start[i] = starts_host ? (int)starts_host[b0 + i] : 0;
             seqs.len[i] = (int)(cu_lens_host[b0 + i + 1] - cu_lens_host[b0 + i]);
-            seqs.tiles[i + 1] = seqs.tiles[i] + (seqs.len[i] ? (seqs.start[i] + seqs.len[i] + kTileTokens - 1) / kTileTokens - seqs.start[i] / kTileTokens : 0);
+            seqs.tiles[i + 1] = seqs.tiles[i] + (int)half_pages(seqs.start[i], seqs.len[i]);
         }
         const int64_t units = (int64_t)seqs.tiles[seqs.n] * parts * a.Hkv;
         if (units == 0) continue;
