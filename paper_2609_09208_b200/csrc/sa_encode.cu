@@ -449,6 +449,7 @@ sa_status sa_quantise_query(const sa_config* cfg, const uint16_t* Q, int batch, 
     Plan p;
     sa_status st = make_plan(cfg, &p);
     if (st != SA_OK) return st;
+    if (p.fp4) return SA_ERR_UNSUPPORTED;                     // (its queries stay binary16)
     if (!Q || !q_hat || !delta || batch < 0) return SA_ERR_INVALID_ARG;
     if (!aligned(Q, 16) || !aligned(q_hat, 16) || !aligned(delta, 4)) return SA_ERR_ALIGNMENT;
     const int64_t n_vec = (int64_t)batch * p.Hq;
@@ -466,6 +467,7 @@ sa_status sa_quantise_values(const sa_config* cfg, const uint16_t* V, int64_t n,
     Plan p;
     sa_status st = make_plan(cfg, &p);
     if (st != SA_OK) return st;
+    if (p.fp4) return SA_ERR_UNSUPPORTED;                     // (its values have 4 bits)
     if (!V || !v_hat || !g || n < 0) return SA_ERR_INVALID_ARG;
     if (!aligned(V, 16) || !aligned(v_hat, 16)) return SA_ERR_ALIGNMENT;
     const int64_t n_vec = n * p.Hkv;
