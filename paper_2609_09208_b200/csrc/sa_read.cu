@@ -239,7 +239,7 @@ extern "C" sa_status sa_read_kv(const sa_config* cfg, const sa_cache* cache, con
     CacheArgs a;
     st = check_cache(p, cache, &a);
     if (st != SA_OK) return st;
-    if (!cu_lens_host || (!K && !V)) return SA_ERR_INVALID_ARG;
+    if (!cu_lens_host) return SA_ERR_INVALID_ARG;
     if (!aligned(K, 16) || !aligned(V, 16)) return SA_ERR_ALIGNMENT;
     int64_t most = (int64_t)a.max_pages * kPageTokens, tiles = 0;
     if (most > 0x7fffffffLL) most = 0x7fffffffLL;                                 // (lengths are 32-bit numbers)
@@ -249,6 +249,8 @@ extern "C" sa_status sa_read_kv(const sa_config* cfg, const sa_cache* cache, con
         if (start > most || n > most - start) return SA_ERR_CAPACITY;
         tiles += half_pages(start, n);
     }
+    if (tiles == 0) return SA_OK;                                                 // (a tensor without elements has no address)
+    if (!K && !V) return SA_ERR_INVALID_ARG;
     const int parts = K && V ? 2 : 1;
     if (tiles * parts * a.Hkv > 0xfffffff0LL || tiles > 0x7fffffffLL) return SA_ERR_CAPACITY;      // (of all launches together: none is made before the last check)
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);

@@ -1,4 +1,5 @@
 """sa_read_kv at the end of the longest caches: positions up to 2^31 - 1."""
+import ctypes as C
 import os
 import subprocess
 import sys
@@ -35,6 +36,28 @@ print(sa.lib().sa_read_kv(C.byref(cfg), C.byref(cache), i64(%d, 0, 0), i64(0, 1,
 """ % (PAGES, END - 1)
     run = subprocess.run([sys.executable, "-c", call], cwd=ROOT, capture_output=True, text=True, env={**os.environ, "CUDA_VISIBLE_DEVICES": ""}, timeout=600)
     assert run.returncode == 0 and run.stdout.split() == ["5"], run.stdout + run.stderr
+
+
+def test_a_read_of_no_tokens_needs_no_outputs():
+    """A tensor without elements has no address: a read of no tokens into two of them is not one without outputs.  What else is wrong with
+    such a call is said all the same."""
+    lib, i64, at, null = sa.lib(), lambda *v: (C.c_int64 * len(v))(*v), C.c_void_p(256), C.c_void_p(0)
+    cfg, cache = sa.make_config(64, 32, 4, sa.SA_KV_FP4), sa.SaCache(256, 256, 256, 2, 4, 8)
+    call = lambda cu, starts, K, V: lib.sa_read_kv(C.byref(cfg), C.byref(cache), starts, cu, K, V, null)
+    for K, V in ((null, null), (at, null), (null, at), (at, at)):
+        assert call(i64(0, 0, 0), None, K, V) == 0 and call(i64(7, 7, 7), i64(256, 3), K, V) == 0
+        assert call(i64(0, 0, 0), i64(257, 0), K, V) == 4 and call(i64(0, 0, 0), i64(-1, 0), K, V) == 1
+    assert call(i64(0, 0, 1), None, null, null) == 1
+
+
+@pytest.mark.gpu
+def test_a_read_of_no_tokens_into_empty_tensors():
+    import torch
+    cfg = sa.make_config(64, 4, 4, sa.SA_POTM4)
+    c = sa.PagedCache(cfg, [10, 0], "cuda")
+    none = torch.empty(0, 4, 64, dtype=torch.float16, device="cuda")
+    sa.read_kv(cfg, c.handle, None, np.array([0, 0, 0]), none, none)
+    sa.read_kv(cfg, c.handle, np.array([10, 0]), np.array([0, 0, 0]), None, none)
 
 
 @pytest.mark.gpu
