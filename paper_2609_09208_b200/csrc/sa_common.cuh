@@ -265,15 +265,21 @@ SA_D f32x2 add2(f32x2 a, f32x2 b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-// 32 bytes of global memory, in one piece where the address allows (wide): rows of 16-byte pieces 32 bytes apart fill every sector in two goes.
-// (volatile: stays behind the wait for the kernel in front)
+// Global memory that a kernel in front of this one may have written: ordinary loads, not those of the non-coherent path, which is for memory
+// that nobody writes while the kernel lives, and a programmatic launch lives beside the kernel in front.  (volatile: behind the wait for that kernel.)
+SA_D uint4 load_16_bytes(const void* p) {
+    uint4 x;
+    asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+    return x;
+}
+// 32 bytes, in one piece where the address allows (wide): rows of 16-byte pieces 32 bytes apart fill every sector in two goes.
 SA_D void load_32_bytes(const void* p, bool wide, uint32_t (&x)[8]) {
     if (wide) {
-        asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
             : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7])
             : "l"(p));
     } else {
-        const uint4 a = __ldg(static_cast<const uint4*>(p)), b = __ldg(static_cast<const uint4*>(p) + 1);
+        const uint4 a = load_16_bytes(p), b = load_16_bytes(static_cast<const uint4*>(p) + 1);
         x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
     }
 }

@@ -321,7 +321,7 @@ struct BumpArgs {
 };
 
 template <int D, int kMergeThreads>
-__global__ void __launch_bounds__(kMergeThreads, 2048 / kMergeThreads) merge_kernel(const float* __restrict__ partials,
+__global__ void __launch_bounds__(kMergeThreads, 2048 / kMergeThreads) merge_kernel(const float* partials,
                                                                                     float* __restrict__ O, int n_splits,
                                                                                     int n_rows, BumpArgs bump) {
     constexpr int kMergeGroups = kMergeThreads / kMergeLanes;     // groups of splits

@@ -72,8 +72,7 @@ __global__ void __launch_bounds__(128) quantise_values_kernel(const uint16_t* __
 
 // sa_append_kv: one block per sequence; warps loop over the KV heads.
 template <int D, int MODE>
-__global__ void __launch_bounds__(128) append_kernel(CacheArgs a, const uint16_t* __restrict__ Knew,
-                                                     const uint16_t* __restrict__ Vnew, int bump) {
+__global__ void __launch_bounds__(128) append_kernel(CacheArgs a, const uint16_t* Knew, const uint16_t* Vnew, int bump) {
     pdl_wait();                 // earlier kernels in the stream may still be reading this cache
     pdl_launch_dependents();
     const int b = blockIdx.x;
@@ -271,7 +270,7 @@ SA_D void fill_values(uint8_t* half, const CacheArgs& a, int t, const uint4* src
 }
 
 template <int D, int MODE, bool HAD>                          // HAD on its own: the rotation needs twice the registers
-__global__ void __launch_bounds__(128, MODE == 33 ? (D == 128 && HAD ? 7 : 8) : 1) fill_kernel(CacheArgs a, const uint16_t* __restrict__ Kin, const uint16_t* __restrict__ Vin,
+__global__ void __launch_bounds__(128, MODE == 33 ? (D == 128 && HAD ? 7 : 8) : 1) fill_kernel(CacheArgs a, const uint16_t* Kin, const uint16_t* Vin,
                                                    const __grid_constant__ FillSeqs seqs) {
     const int lane = threadIdx.x & 31;
     using Unit = std::conditional_t<MODE == 33, uint32_t, int64_t>;           // (a 64-bit division is a long routine; 4 bits: the host sees to it that 32 do)
@@ -304,7 +303,7 @@ __global__ void __launch_bounds__(128, MODE == 33 ? (D == 128 && HAD ? 7 : 8) : 
         uint4 v[C];
 #pragma unroll
         for (int k = 0; k < C; ++k)
-            if (k * R + lane / C < n) v[k] = __ldg(in + (size_t)(k * R + lane / C) * pitch);
+            if (k * R + lane / C < n) v[k] = load_16_bytes(in + (size_t)(k * R + lane / C) * pitch);
 #pragma unroll
         for (int k = 0; k < C; ++k) {
             const int row = k * R + lane / C;

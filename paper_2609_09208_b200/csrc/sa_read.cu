@@ -50,7 +50,7 @@ struct KeyReader {
     SA_D KeyReader(const uint8_t* half_, const CacheArgs& a, int t_) : half(half_), plane_off(a.plane_off), t(t_), s(1.0f) {
         if constexpr (MODE != 16) s = half_bits_to_float(*reinterpret_cast<const uint16_t*>(half + a.meta_off + t * 4));
     }
-    SA_D uint4 chunk(int k) const { return __ldg(reinterpret_cast<const uint4*>(half + ((size_t)k * kTileTokens + t) * 16)); }
+    SA_D uint4 chunk(int k) const { return load_16_bytes(half + ((size_t)k * kTileTokens + t) * 16); }
     SA_D void get(int c, float (&x)[8]) {
         if constexpr (MODE == 16) {
             w = chunk(c);
@@ -136,14 +136,14 @@ SA_D void read_values(const uint8_t* half, const CacheArgs& a, int t, uint4* row
     const uint8_t* v = half + a.v_off;
     if constexpr (MODE == 16) {
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) row[c ^ (t & 7)] = __ldg(reinterpret_cast<const uint4*>(v + ((size_t)c * kTileTokens + t) * 16));
+        for (int c = 0; c < D / 8; ++c) row[c ^ (t & 7)] = load_16_bytes(v + ((size_t)c * kTileTokens + t) * 16);
     } else {
         // times 2^-g in two exact steps: the first keeps clear of the subnormal numbers, the second rounds where the value is one
         const int g = (int)(int8_t)half[a.meta_off + t * 4 + 2], g1 = max(-10, min(g, 12));
         const uint32_t f1 = half2_bits(pow2i(-g1), pow2i(-g1)), f2 = half2_bits(pow2i(max(g1 - g, -40)), pow2i(max(g1 - g, -40)));
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-            const uint4 in = __ldg(reinterpret_cast<const uint4*>(v + ((size_t)k * kTileTokens + t) * 16));
+            const uint4 in = load_16_bytes(v + ((size_t)k * kTileTokens + t) * 16);
             const uint32_t w[4] = {in.x, in.y, in.z, in.w};
             uint32_t h[8];
 #pragma unroll
@@ -159,7 +159,7 @@ SA_D void read_values(const uint8_t* half, const CacheArgs& a, int t, uint4* row
 }
 
 template <int D, int MODE, bool HAD>
-__global__ void __launch_bounds__(128, HAD || (MODE == 33 && D == 128) ? 0 : D == 64 ? 9 : 8) read_kernel(CacheArgs a, uint16_t* __restrict__ Kout, uint16_t* __restrict__ Vout, const __grid_constant__ ReadSeqs seqs) {
+__global__ void __launch_bounds__(128, HAD || (MODE == 33 && D == 128) ? 0 : D == 64 ? 9 : 8) read_kernel(CacheArgs a, uint16_t* Kout, uint16_t* Vout, const __grid_constant__ ReadSeqs seqs) {
     const int lane = threadIdx.x & 31;
     const int parts = Kout && Vout ? 2 : 1;
     const uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 5), each = (uint32_t)(parts * a.Hkv);      // (tile, head, keys or values)
