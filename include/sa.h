@@ -197,7 +197,8 @@ sa_status sa_append_kv(const sa_config* cfg, const sa_cache* cache, const uint16
 
 /* Bulk build of a cache: K, V [sum_b T_b, n_kv_heads, head_dim] binary16, sequence b occupying
  * rows cu_lens_host[b] .. cu_lens_host[b+1] (HOST array of batch + 1 entries).  Writes tokens
- * 0 .. T_b - 1 of every sequence; does not touch seq_lens. */
+ * 0 .. T_b - 1 of every sequence; does not touch seq_lens.  Sequences may share pages for the tokens that
+ * they have in common, each ending anywhere in them. */
 sa_status sa_fill_kv(const sa_config* cfg, const sa_cache* cache, const uint16_t* K,
                      const uint16_t* V, const int64_t* cu_lens_host, sa_stream stream);
 

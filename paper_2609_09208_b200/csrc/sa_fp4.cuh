@@ -251,9 +251,16 @@ struct Fp4Half {
         }
         return m;
     }
+    // The bits of x that `mask` has, by atomics where it has not all: sequences of one call that share a prefix share its pages, and where one ends
+    // within a half that another fills on, both write the shared tokens (with the same bits), and the other's must not get lost between a
+    // load and a store of this word.
     SA_D static void store_masked(uint8_t* at, uint32_t x, uint32_t mask) {
         uint32_t* p = reinterpret_cast<uint32_t*>(at);
-        if (mask) *p = mask == 0xffffffffu ? x : (x & mask) | (*p & ~mask);
+        if (mask == 0xffffffffu) *p = x;
+        else if (mask) {
+            atomicAnd(p, ~mask);
+            atomicOr(p, x & mask);
+        }
     }
 };
 // Part `part` of the tile's first n tokens of K or V (rows of `pitch` elements) into the half page at `half`, whose value codes start at v_off.  What
