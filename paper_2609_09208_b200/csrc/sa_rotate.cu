@@ -111,10 +111,11 @@ __global__ void __launch_bounds__(rotate_threads(TOKENS), (sizeof(T) == 4 ? 3 : 
         const int j = TOKENS == 1 ? i : i % half, k = TOKENS == 1 ? 0 : i / half;
         const int axis = a.pair_axis ? min((int)a.pair_axis[j], a.axes - 1) : 0;
         const double turns = (double)a.positions[axis * a.n + token0 + k] * (double)a.inv_freq[j] * 0.15915494309189535;
-        // within half a turn the fast functions are off by 2^-21.2 at most, a thousandth of what binary16 rounds away
-        const float x = (float)(turns - rint(turns)) * 6.2831853f;
-        turn[k][0][j] = __cosf(x) * a.scale;
-        turn[k][1][j] = __sinf(x) * a.scale;
+        // the fraction's sine and cosine to their last bits: one channel of a pair may be far larger than the other
+        float sn, cs;
+        sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+        turn[k][0][j] = cs * a.scale;
+        turn[k][1][j] = sn * a.scale;
     }
     __syncthreads();
     const bool turns_a = pa < (NEIGHBOURS ? a.R : half), turns_b = NEIGHBOURS ? pb < a.R : turns_a;
