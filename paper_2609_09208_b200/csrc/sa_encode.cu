@@ -270,7 +270,7 @@ SA_D void fill_values(uint8_t* half, const CacheArgs& a, int t, const uint4* src
 }
 
 template <int D, int MODE, bool HAD>                          // HAD on its own: the rotation needs twice the registers
-__global__ void __launch_bounds__(128, MODE == 33 ? (D == 128 && HAD ? 7 : 8) : 1) fill_kernel(CacheArgs a, const uint16_t* Kin, const uint16_t* Vin,
+__global__ void __launch_bounds__(128, MODE == 33 ? (D == 128 && HAD ? 7 : 8) : 0) fill_kernel(CacheArgs a, const uint16_t* Kin, const uint16_t* Vin,
                                                    const __grid_constant__ FillSeqs seqs) {
     const int lane = threadIdx.x & 31;
     using Unit = std::conditional_t<MODE == 33, uint32_t, int64_t>;           // (a 64-bit division is a long routine; 4 bits: the host sees to it that 32 do)
