@@ -209,7 +209,7 @@ sa_status sa_fill_kv(const sa_config* cfg, const sa_cache* cache, const uint16_t
  * Written are the numbers that the codes stand for, rounded once to binary16 (FP32 arithmetic; exact for SA_KV_FP4 and
  * SA_KV_FP16); keys that were rotated on their way in (SA_FLAG_HADAMARD) are rotated back.  The caller keeps the range within
  * what has been written (seq_lens is not read): slots that never were hold anything.  Tokens whose page is not mapped come back as zeros; no other
- * row of K or V is touched. */
+ * row of K or V is touched.  A call of no tokens needs neither K nor V. */
 sa_status sa_read_kv(const sa_config* cfg, const sa_cache* cache, const int64_t* starts_host, const int64_t* cu_lens_host,
                      uint16_t* K, uint16_t* V, sa_stream stream);
 
@@ -241,7 +241,9 @@ typedef struct {
  * lie side by side in one projection's output; addresses and strides are multiples of 16 bytes.  Any of the three may be NULL together with its output.
  * positions: int32 [n_axes][n].  Q_out [n, n_q_heads, head_dim], K_out, V_out [n, n_kv_heads, head_dim] binary16; an output may be
  * its own input where the two have the same layout (SA_F16, contiguous rows).  Of cfg only the head counts and head_dim matter.
- * A result beyond 65504 becomes infinite; a head of zeros with eps = 0 becomes NaN. */
+ * A result beyond 65504 becomes infinite; a head of zeros with eps = 0 becomes NaN.  Squares are summed in FP32: a head with
+ * numbers beyond 1e18 may come out as zeros, and with eps = 0 one of numbers below 1e-18 throughout loses precision (below 1e-23:
+ * counts as one of zeros). */
 sa_status sa_rotate_qkv(const sa_config* cfg, const sa_rotary* rot, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
                         const void* V, int64_t v_stride, const int32_t* positions, int64_t n, uint16_t* Q_out, uint16_t* K_out,
                         uint16_t* V_out, sa_stream stream);
@@ -290,7 +292,7 @@ sa_status sa_decode_attention_fp16(const sa_config* cfg, const sa_cache* cache, 
 /* One decode step of a layer in a single pass (section II-F: the cache stores only quantised data,
  * and the step both extends it and attends over it): equivalent to
  *   sa_append_kv(cfg, cache, K_new, V_new, 1, stream); sa_decode_attention(cfg, cache, Q, O, ...);
- * The warp of the decode kernel that owns the new token's 32-key tile encodes and writes the token
+ * The warp of the decode kernel that owns the new token's tile encodes and writes the token
  * before it stages that tile, so the separate append kernel and its launch disappear from the
  * step; seq_lens[b] is incremented after every block has read it: by the split-K merge kernel, or, where the
  * plan needs no merge kernel (short sequences, whose splits form a thread-block cluster; one split per sequence; large

@@ -188,7 +188,7 @@ def fill_kv(cfg, cache: SaCache, K, V, cu_lens_host):
 
 def read_kv(cfg, cache: SaCache, starts, cu_lens_host, K=None, V=None):
     """Tokens starts[b] .. of every sequence, cu_lens_host[b + 1] - cu_lens_host[b] of them, as binary16 rows of K and V
-    ([rows, n_kv_heads, head_dim], contiguous; either may be None).  starts (None: all 0), cu_lens_host: contiguous numpy int64 arrays of batch
+    ([rows, n_kv_heads, head_dim], contiguous, float16, or int16 / uint16 for its bits; either may be None).  starts (None: all 0), cu_lens_host: contiguous numpy int64 arrays of batch
     and batch + 1 entries (host memory)."""
     st = (_nat or native()).read_kv(cfg, cache, starts, cu_lens_host, K, V)
     if st:
@@ -231,7 +231,7 @@ class Rotary:
 
 def rotate_qkv(rot: Rotary, Q, K, V, positions, Q_out, K_out, V_out):
     """Q [n, n_q_heads, head_dim], K, V [n, n_kv_heads, head_dim] of rot.dtype (a token's heads contiguous; views of one projection's
-    output will do) to contiguous binary16 outputs of the same shapes; any of the three may be None with its output.
+    output will do) to contiguous binary16 outputs of the same shapes (float16, or int16 / uint16 for its bits); any of the three may be None with its output.
     positions: int32 [n_axes, n] (or [n]), None where nothing is rotated."""
     st = (_nat or native()).rotate_qkv(rot.cfg, rot.handle, rot.dtype, rot.device, Q, K, V, positions, Q_out, K_out, V_out)
     if st:

@@ -214,7 +214,7 @@ void split_plan(const Plan& p, int batch, int max_pages, int* n_splits, int* gt,
     // PoT-M4 6.8 against 6.5, but 6.9 against 7.2 launched one by one); two tiles for batches, three where there are enough
     // units for all SMs or rounds are long (4 x 6000 tokens, PoT-M1 planar: 9.7 -> 10.4, 8 x 6000 13.0 -> 11.4).  Fewer than 8
     // units of a batch would leave most SMs idle.  256 blocks, two to an SM, are what the machine takes at a time in clusters of
-    // 8 (9 x 1000 tokens, 288 blocks: 7.3 -> 11.1).
+    // 8 (9 x 1000 tokens, 288 blocks: 7.3 -> 11.1).  (4-bit cache: the line counts its tiles, which have 64 keys at head_dim 64; it was not measured there.)
     const KernelShape whole = p.fp16 ? p.shape : cluster_shape(p.d);
     long long blocks = tiles / 2 < 1 ? 1 : tiles / 2 > kClusterMost ? kClusterMost : tiles / 2;
     if (units * blocks > n_sms && tiles <= kClusterMost / 2 * whole.warps && blocks > kClusterMost / 2) blocks = kClusterMost / 2;

@@ -7,13 +7,14 @@
 // d / (2 P) lanes share a head vector; a lane holds two pieces of P channels whose pairs lie in the lane: pairing halves, channels
 // u .. u + P - 1 and their partners; pairing neighbours, any two.  So the rotation needs no exchange, the norm one
 // sum over the lanes.  P = 8, 16-byte loads, 32-byte ones of FP32; 4 where halves are no multiple of 8 channels.  The pieces of the lanes follow one another in
-// memory (FP32, neighbours, 5001 tokens of 16 / 16 heads of 128: with two pieces of a lane in a row and 16-byte loads 39.7 us, so 31.9: 5.8 TB/s).  The angles are the same for
+// memory (FP32, neighbours, 5001 tokens of 16 / 16 heads of 128: with two pieces of a lane in a row and 16-byte loads 39.7 us, so 31.9: 5.8 TB/s; all times in a graph).  The angles are the same for
 // all heads: each is worked out by one thread of the block, in 64 bits up to the fraction of a turn (position times frequency in 32 bits would be off by 0.01 rad at position
-// 131 072), while the first vectors are on their way, and handed over in shared memory.
+// 131 072), while the first vectors are on their way, and handed over in shared memory; its sine and cosine are those of the full-precision function (the fast ones: the same times,
+but 120 000 tokens of 1 / 1 heads, where an angle serves two vectors only, 76.3 -> 77.2).
 // The threads of a block are dealt to tokens, and a thread stays with its token: the weights of a projection stay in its registers, packed FP32
 // pairs do the arithmetic.  Decode steps: a block of 256 threads per token (one of 128: 2.0 -> 2.2 us); prompts: 128 threads, 4 tokens of a block (2 at head_dim 128), so that all
 // lanes have several vectors, the next one under way while one is worked on.  What is left above the copy rate are instructions, 14 for a channel.  us, 32 / 8 heads
-// of 128: 8192 tokens in bfloat16 with norms 51.1 -> 38.1 (5.3 TB/s), in FP32 51.6 (5.9 TB/s), 1024 tokens 6.5; one token of 32 / 4 heads of 64 2.0.  Of 8192 tokens: 256 threads with twice the
+// of 128: 8192 tokens in bfloat16 with norms 51.1 -> 38.1 (5.3 TB/s), in FP32 51.3 (5.9 TB/s), 1024 tokens 6.5; one token of 32 / 4 heads of 64 2.1.  Of 8192 tokens: 256 threads with twice the
 // tokens 39.4, 64 threads 37.8 (but 1024 tokens 8.7), two vectors under way 41.3, other register bounds 42 to 46, sines and cosines in registers (fewer threads) 42.6, with their negatives
 // in a third table 41.5.
 #include "sa_cache_write.cuh"
