@@ -10,7 +10,7 @@
 // memory (FP32, neighbours, 5001 tokens of 16 / 16 heads of 128: with two pieces of a lane in a row and 16-byte loads 39.7 us, so 31.9: 5.8 TB/s; all times in a graph).  The angles are the same for
 // all heads: each is worked out by one thread of the block, in 64 bits up to the fraction of a turn (position times frequency in 32 bits would be off by 0.01 rad at position
 // 131 072), while the first vectors are on their way, and handed over in shared memory; its sine and cosine are those of the full-precision function (the fast ones: the same times,
-but 120 000 tokens of 1 / 1 heads, where an angle serves two vectors only, 76.3 -> 77.2).
+// but 120 000 tokens of 1 / 1 heads, where an angle serves two vectors only, 76.3 -> 77.2).
 // The threads of a block are dealt to tokens, and a thread stays with its token: the weights of a projection stay in its registers, packed FP32
 // pairs do the arithmetic.  Decode steps: a block of 256 threads per token (one of 128: 2.0 -> 2.2 us); prompts: 128 threads, 4 tokens of a block (2 at head_dim 128), so that all
 // lanes have several vectors, the next one under way while one is worked on.  What is left above the copy rate are instructions, 14 for a channel.  us, 32 / 8 heads
