@@ -248,6 +248,34 @@ sa_status sa_rotate_qkv(const sa_config* cfg, const sa_rotary* rot, const void* 
                         const void* V, int64_t v_stride, const int32_t* positions, int64_t n, uint16_t* Q_out, uint16_t* K_out,
                         uint16_t* V_out, sa_stream stream);
 
+/* sa_rotate_qkv and the cache write in one pass, for any number of new tokens per sequence (the next chunk of a prompt, drafted tokens, one token; sa_append_kv
+ * takes one, sa_fill_kv starts at token 0): queries go to Q_out, keys and values, normed, rotated and rounded to binary16 as sa_rotate_qkv has them, are coded as
+ * sa_append_kv codes them and written behind what the sequence holds.  Sequence b's rows cu_lens_host[b] .. cu_lens_host[b+1] - 1 of Q, K, V, positions and Q_out
+ * become its tokens seq_lens[b] ..; all but Q_out's other rows stay as they are.  n: rows of the inputs, and columns of positions [n_axes][n]; at least cu_lens_host[batch].
+ * Q may be NULL together with Q_out.  If bump_lens is non-zero the lengths grow by the numbers of new tokens.  The pages of the new tokens must be
+ * mapped already: of a sequence for which one is not, nothing is written and the length stays.  Codes and containers of every kind; n_kv_heads * head_dim at most
+ * 12800 (head_dim 64) or 25600 (128).  cu_lens_host: HOST array of batch + 1 entries, read during the call; seq_lens is read on the device (a captured call follows it). */
+sa_status sa_append_qkv(const sa_config* cfg, const sa_cache* cache, const sa_rotary* rot, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+                        const void* V, int64_t v_stride, const int32_t* positions, int64_t n, const int64_t* cu_lens_host, uint16_t* Q_out, int bump_lens,
+                        sa_stream stream);
+
+/* Attention of a chunk of new tokens over the paged cache (the paper decodes one token per sequence; this is for the chunks of a prompt, for drafted
+ * tokens that are checked, and for batches in which some sequences have many new tokens and others one).  The cache holds the new tokens already
+ * (sa_append_qkv, sa_append_kv or sa_fill_kv): sequence b's n_b = cu_lens_host[b+1] - cu_lens_host[b] queries, rows cu_lens_host[b] .. of Q
+ * [rows, n_q_heads, head_dim] binary16, belong to its last n_b tokens, i to token p = seq_lens[b] - n_b + i, and see the tokens j <= p; with window > 0 of
+ * those only j > p - window and j < sinks (a sliding window, and the first tokens of the sequence, which stay visible).  n_b may be 0 or 1, and n_b another for every sequence.
+ *   O [rows, n_q_heads, head_dim], of o_dtype SA_F16 or SA_BF16, = softmax(Q K^T / sqrt(head_dim)) V
+ * over the numbers that the cache's codes stand for, with SA_FLAG_HADAMARD in the rotated space; over the power-of-two codes and SA_INT8 a query is
+ * rounded to 8 bits first, as in sa_decode_attention.  All codes and containers; of the flags SA_FLAG_HADAMARD only.  FP32 statistics and sums; a weight enters as
+ * one binary16 number (which costs no more than the rounding of O).  A query that sees no token (p < 0, or none of its pages is mapped) yields zeros.  Rows of O
+ * outside cu_lens_host[0] .. cu_lens_host[batch] are not touched.  Q and O must not overlap.  What tokens hold that no query of a call sees does not matter; a token with an
+ * infinity or a NaN that some of a sequence's queries see may show in the others.  cu_lens_host: HOST array of batch + 1 entries, read during the call; seq_lens is
+ * read on the device (a captured call follows it).  workspace: sa_chunk_workspace_bytes, 256-byte aligned, any contents, not shared by calls that overlap on the GPU;
+ * ask for it on the device that the call will run on, with the most tokens that a call has.  Deterministic run to run. */
+sa_status sa_chunk_workspace_bytes(const sa_config* cfg, int batch, int64_t n_tokens, size_t* out);
+sa_status sa_chunk_attention(const sa_config* cfg, const sa_cache* cache, const uint16_t* Q, const int64_t* cu_lens_host, int window, int sinks,
+                             void* O, int o_dtype, void* workspace, size_t workspace_bytes, sa_stream stream);
+
 /* Decode attention over the quantised cache — the hot path (section II-B eq. (3), II-C eq. (4),
  * II-D eq. (5), II-E, II-F):
  *   Q is quantised (and rotated, if flagged) inside the kernel; for every cached key the integer

@@ -33,6 +33,7 @@ EXPORTS = [
     "sa_decode_attention_fp16", "sa_decode_attention_stages", "sa_decode_attention_fp16_stages", "sa_debug_unpack", "sa_staging_bytes", "sa_decode_step_host",
     "sa_decode_attention_static", "sa_pipe_microbench", "sa_shiftav_workspace_bytes", "sa_decode_attention_shiftav",
     "sa_decode_step", "sa_debug_decode_lost_copy", "sa_read_kv", "sa_rotate_qkv",
+    "sa_append_qkv", "sa_chunk_workspace_bytes", "sa_chunk_attention",
 ]
 
 
@@ -236,6 +237,30 @@ def rotate_qkv(rot: Rotary, Q, K, V, positions, Q_out, K_out, V_out):
     st = (_nat or native()).rotate_qkv(rot.cfg, rot.handle, rot.dtype, rot.device, Q, K, V, positions, Q_out, K_out, V_out)
     if st:
         raise SaError(st, "sa_rotate_qkv")
+
+
+def append_qkv(rot: Rotary, cache: SaCache, Q, K, V, positions, cu_lens_host, Q_out, bump_lens: bool = True):
+    """rotate_qkv and the cache write in one pass: rows cu_lens_host[b] .. of Q, K, V and positions (as rotate_qkv takes them, the same number of rows in all) become sequence b's
+    next tokens; the queries go to the same rows of Q_out (Q and Q_out may be None together).  cu_lens_host: contiguous numpy int64 array of batch + 1 entries (host memory)."""
+    st = (_nat or native()).append_qkv(rot.cfg, rot.handle, rot.dtype, rot.device, cache, Q, K, V, positions, cu_lens_host, Q_out, 1 if bump_lens else 0)
+    if st:
+        raise SaError(st, "sa_append_qkv")
+
+
+def chunk_workspace_bytes(cfg: SaConfig, batch: int, n_tokens: int) -> int:
+    """Scratch of chunk_attention for calls of at most n_tokens new tokens."""
+    out = C.c_size_t()
+    _check(lib().sa_chunk_workspace_bytes(C.byref(cfg), C.c_int(batch), C.c_int64(n_tokens), C.byref(out)), "sa_chunk_workspace_bytes")
+    return out.value
+
+
+def chunk_attention(cfg, cache: SaCache, Q, O, workspace, cu_lens_host, window: int = 0, sinks: int = 0):
+    """Attention of the last cu_lens_host[b + 1] - cu_lens_host[b] tokens of every sequence, which the cache holds already, each over the tokens up to itself; with a
+    window over its last `window` tokens (itself among them) and the first `sinks` of the sequence.  Q [rows, n_q_heads, head_dim] float16 (or int16 / uint16 for its
+    bits), O of the same shape in float16 or bfloat16, both contiguous; cu_lens_host: contiguous numpy int64 array of batch + 1 entries (host memory)."""
+    st = (_nat or native()).chunk_attention(cfg, cache, Q, O, workspace, cu_lens_host, window, sinks)
+    if st:
+        raise SaError(st, "sa_chunk_attention")
 
 
 def decode_attention(cfg, cache: SaCache, Q, O, workspace, dbg_scores=None, stages: int = 3):

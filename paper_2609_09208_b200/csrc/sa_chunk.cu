@@ -1,0 +1,115 @@
+// sa_chunk_attention: checks, and the launches of the kernels in sa_chunk.cuh.
+#include "sa_chunk.cuh"
+
+namespace sa {
+
+static size_t chunk_workspace(const Plan& p, int64_t rows_most, int blocks) {
+    return kChunkPlanBytes + 2 * (size_t)blocks * sizeof(float) * chunk_slot_floats(p.d, rows_most <= chunk_rows(true));
+}
+static int chunk_blocks_most() { return sm_count() < kChunkBlocksMost ? sm_count() : kChunkBlocksMost; }
+
+static int chunk_format(const Plan& p) {
+    if (p.fp16) return FMT_FP16;
+    if (p.fp4) return FMT_FP4;
+    if (p.int8) return FMT_INT8;
+    if (p.nibble) return p.k == 0 ? FMT_NIBBLE : p.k == 1 ? FMT_PLANAR1 : FMT_PLANAR2;
+    return FMT_BYTE;
+}
+
+// The sequences of one kind (SPLIT: of at most 128 rows; or the others), kChunkBatch a launch.
+static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool split, cudaStream_t s) {
+    const int fmt = chunk_format(p);
+    int64_t most = 0;
+    for (int b = 0; b < a.c.batch; ++b) {
+        const int64_t rows = (cu[b + 1] - cu[b]) * p.G;
+        if ((rows <= chunk_rows(true)) == split && rows > most) most = rows;
+    }
+    if (most == 0) return true;
+    a.copies = !split || most > 64 ? 1 : most > 32 ? 2 : 4;
+    const int per_tile = chunk_rows(split) / a.copies;
+    const int64_t tiles_most = ((int64_t)a.c.max_pages + 1) / 2;
+    for (int b = 0; b < a.c.batch;) {
+        a.s.n = 0;
+        a.s.tiles[0] = 0;
+        int64_t work = 0;
+        for (; b < a.c.batch && a.s.n < kChunkBatch; ++b) {
+            const int64_t n = cu[b + 1] - cu[b], rows = n * p.G;
+            if (n == 0 || (rows <= chunk_rows(true)) != split) continue;
+            const int i = a.s.n, tiles = (int)((rows + per_tile - 1) / per_tile);
+            if (i && a.s.tiles[i] > 0x7ffffff0 - tiles) break;
+            a.s.b[i] = b;
+            a.s.tokens[i] = (int)n;
+            a.s.row0[i] = cu[b];
+            a.s.tiles[i + 1] = a.s.tiles[i] + tiles;
+            a.s.n = i + 1;
+            const int64_t window = a.window ? ((int64_t)a.window + per_tile / p.G + 1) / kChunkTile + 2 + ((int64_t)a.sinks + kChunkTile - 1) / kChunkTile : tiles_most;
+            work += (int64_t)tiles * (kChunkUnitCost + (window < tiles_most ? window : tiles_most));
+        }
+        if (a.s.n == 0) break;
+        int blocks = chunk_blocks_most();
+        if (work * p.Hkv < blocks) blocks = (int)(work * p.Hkv);
+        const bool pot = !p.fp16 && !p.fp4 && !p.int8;
+        if ((pot ? launch_chunk_pot(p.d, fmt, split, a, blocks, s) : launch_chunk_plain(p.d, fmt, split, a, blocks, s)) != cudaSuccess) return false;
+    }
+    return true;
+}
+
+}  // namespace sa
+
+using namespace sa;
+
+extern "C" {
+
+sa_status sa_chunk_workspace_bytes(const sa_config* cfg, int batch, int64_t n_tokens, size_t* out) {
+    if (!out || batch <= 0 || n_tokens < 0) return SA_ERR_INVALID_ARG;
+    Plan p;
+    const sa_status st = make_plan(cfg, &p);
+    if (st != SA_OK) return st;
+    // (the longest chunk may have all tokens)
+    *out = chunk_workspace(p, n_tokens > 0x7fffffff ? 0x7fffffff : n_tokens * p.G, chunk_blocks_most());
+    return SA_OK;
+}
+
+sa_status sa_chunk_attention(const sa_config* cfg, const sa_cache* cache, const uint16_t* Q, const int64_t* cu_lens_host, int window, int sinks, void* O, int o_dtype,
+                             void* workspace, size_t workspace_bytes, sa_stream stream) {
+    Plan p;
+    sa_status st = make_plan(cfg, &p);
+    if (st != SA_OK) return st;
+    if (p.mulshift || p.addalu || p.shiftadd) return SA_ERR_UNSUPPORTED;      // (decode kernels only)
+    ChunkArgs a{};
+    st = check_cache(p, cache, &a.c);
+    if (st != SA_OK) return st;
+    if (!cu_lens_host || window < 0 || sinks < 0) return SA_ERR_INVALID_ARG;
+    if (o_dtype != SA_F16 && o_dtype != SA_BF16) return SA_ERR_UNSUPPORTED;
+    int64_t longest = 0;
+    for (int b = 0; b < a.c.batch; ++b) {
+        const int64_t n = cu_lens_host[b + 1] - cu_lens_host[b];
+        if (n < 0 || cu_lens_host[b] < 0) return SA_ERR_INVALID_ARG;
+        if (n > (int64_t)a.c.max_pages * kPageTokens || n > (0x7fffffff - 256) / p.G) return SA_ERR_CAPACITY;
+        longest = n > longest ? n : longest;
+    }
+    const int64_t n_rows = cu_lens_host[a.c.batch];
+    if (longest == 0) return SA_OK;                                            // (a tensor without elements has no address)
+    if (!Q || !O || !workspace) return SA_ERR_INVALID_ARG;
+    if (!aligned(Q, 16) || !aligned(O, 16) || !aligned(workspace, 256)) return SA_ERR_ALIGNMENT;
+    if (n_rows > (int64_t)(PTRDIFF_MAX / 4) / ((int64_t)p.Hq * p.d)) return SA_ERR_CAPACITY;
+    // a block may read queries of a row behind another's writing of its output
+    const uintptr_t q0 = reinterpret_cast<uintptr_t>(Q), o0 = reinterpret_cast<uintptr_t>(O), bytes = (uintptr_t)n_rows * p.Hq * p.d * 2;
+    if (q0 < o0 + bytes && o0 < q0 + bytes) return SA_ERR_INVALID_ARG;
+    if (workspace_bytes < chunk_workspace(p, longest * p.G, chunk_blocks_most())) return SA_ERR_CAPACITY;
+    a.Q = Q;
+    a.O = O;
+    a.workspace = static_cast<uint8_t*>(workspace);
+    a.Hq = p.Hq;
+    a.G = p.G;
+    a.window = window;
+    a.sinks = sinks;
+    a.bf16 = o_dtype == SA_BF16;
+    const float log2e_over_root = 1.4426950408889634f / (p.d == 64 ? 8.0f : 11.313708498984761f);
+    a.factor = log2e_over_root * (p.fp16 || p.fp4 ? 1.0f : p.int8 ? 1.0f / 127.0f : 256.0f);       // (power-of-two codes: operands of 2^-120 and 2^112)
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    if (!launch_kind(p, a, cu_lens_host, false, s) || !launch_kind(p, a, cu_lens_host, true, s)) return SA_ERR_CUDA;
+    return cudaGetLastError() == cudaSuccess ? SA_OK : SA_ERR_CUDA;
+}
+
+}  // extern "C"

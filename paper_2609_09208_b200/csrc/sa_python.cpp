@@ -11,7 +11,7 @@
 
 namespace {
 
-PyObject *g_data_ptr, *g_nbytes, *g_get_device, *g_get_stream, *g_shape, *g_stride, *g_is_contiguous, *g_dtype, *g_device_of, *g_float16, *g_int16, *g_uint16, *g_int32;
+PyObject *g_data_ptr, *g_nbytes, *g_get_device, *g_get_stream, *g_shape, *g_stride, *g_is_contiguous, *g_dtype, *g_device_of, *g_float16, *g_int16, *g_uint16, *g_int32, *g_bfloat16;
 
 struct Args {
     PyObject* const* v;
@@ -294,6 +294,37 @@ PyObject* read_kv(PyObject*, PyObject* const* v, Py_ssize_t n) {
     SA_RETURN(sa_read_kv(cfg, cache, starts.p, cu.p, out[0], out[1], s));
 }
 
+// What rotate_qkv and append_qkv take of a layer's projections, and the positions.
+struct Projections {
+    const void* in[3] = {};
+    long long stride[3] = {}, n = -1;                          // n: rows; -1: none is given
+    const int32_t* positions = nullptr;
+    void take(Args& a, const sa_config* cfg, PyObject* dtype, long long dev) {
+        long long sh[3], step[3];
+        const long long d = a.bad ? 0 : cfg->head_dim;
+        for (int i = 0; i < 3 && !a.bad; ++i) {
+            PyObject* o = a.next();
+            if (a.bad || o == Py_None) continue;
+            const long long H = i == 0 ? cfg->n_q_heads : cfg->n_kv_heads;
+            if (!a.shape(o, 3, sh) || sh[1] != H || sh[2] != d || (n >= 0 && sh[0] != n) || !a.strides(o, 3, step) || (H > 1 && step[1] != d) || step[2] != 1 ||
+                !a.typed(o, dtype) || !a.on_device(o, dev))
+                a.fail("Q, K and V are [n, heads, head_dim] of the rotary's dtype on the current CUDA device, a token's heads one after another, n the same for all");
+            n = sh[0];
+            stride[i] = n > 1 ? step[0] : H * d;
+            in[i] = a.address<const void>(o);
+        }
+    }
+    void take_positions(Args& a, const sa_rotary* rot, long long dev) {
+        long long sh[3];
+        PyObject* pos = a.bad ? nullptr : a.next();
+        if (a.bad || pos == Py_None) return;
+        const bool two = a.shape(pos, 2, sh);
+        if (two ? sh[0] != rot->n_axes || (n >= 0 && sh[1] != n) : rot->n_axes != 1 || !a.shape(pos, 1, sh) || (n >= 0 && sh[0] != n)) a.fail("positions are [n_axes, n]");
+        else if (!a.typed(pos, g_int32) || !a.contiguous(pos) || !a.on_device(pos, dev)) a.fail("positions are contiguous int32 on the current CUDA device");
+        positions = a.address<const int32_t>(pos);
+    }
+};
+
 // (cfg, rotary, dtype, device of the tables, Q, K, V, positions, Q_out, K_out, V_out)
 PyObject* rotate_qkv(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     Args a{v, n_args};
@@ -302,29 +333,13 @@ PyObject* rotate_qkv(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     PyObject* dtype = a.bad ? nullptr : a.next();
     const long long tables = a.integer(), dev = a.current_device();
     if (!a.bad && tables >= 0 && tables != dev) a.fail("the tables lie on another device than the current one");
-    const void* in[3] = {};
     uint16_t* out[3] = {};
-    long long stride[3] = {}, n = -1, sh[3], step[3];
+    long long sh[3];
     const long long d = a.bad ? 0 : cfg->head_dim;
-    for (int i = 0; i < 3 && !a.bad; ++i) {
-        PyObject* o = a.next();
-        if (a.bad || o == Py_None) continue;
-        const long long H = i == 0 ? cfg->n_q_heads : cfg->n_kv_heads;
-        if (!a.shape(o, 3, sh) || sh[1] != H || sh[2] != d || (n >= 0 && sh[0] != n) || !a.strides(o, 3, step) || (H > 1 && step[1] != d) || step[2] != 1 ||
-            !a.typed(o, dtype) || !a.on_device(o, dev))
-            a.fail("Q, K and V are [n, heads, head_dim] of the rotary's dtype on the current CUDA device, a token's heads one after another, n the same for all");
-        n = sh[0];
-        stride[i] = n > 1 ? step[0] : H * d;
-        in[i] = a.address<const void>(o);
-    }
-    const int32_t* positions = nullptr;
-    PyObject* pos = a.bad ? nullptr : a.next();
-    if (!a.bad && pos != Py_None) {
-        const bool two = a.shape(pos, 2, sh);
-        if (two ? sh[0] != rot->n_axes || (n >= 0 && sh[1] != n) : rot->n_axes != 1 || !a.shape(pos, 1, sh) || (n >= 0 && sh[0] != n)) a.fail("positions are [n_axes, n]");
-        else if (!a.typed(pos, g_int32) || !a.contiguous(pos) || !a.on_device(pos, dev)) a.fail("positions are contiguous int32 on the current CUDA device");
-        positions = a.address<const int32_t>(pos);
-    }
+    Projections x;
+    x.take(a, cfg, dtype, dev);
+    x.take_positions(a, rot, dev);
+    const long long n = x.n;
     for (int i = 0; i < 3 && !a.bad; ++i) {
         PyObject* o = a.next();
         if (a.bad || o == Py_None) continue;
@@ -335,10 +350,65 @@ PyObject* rotate_qkv(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     // (a tensor without elements has no address, which would read as one that is not there)
     if (!a.bad && n == 0) return PyLong_FromLong(SA_OK);
     const sa_stream s = a.stream();
-    SA_RETURN(sa_rotate_qkv(cfg, rot, in[0], stride[0], in[1], stride[1], in[2], stride[2], positions, n < 0 ? 0 : n, out[0], out[1], out[2], s));
+    SA_RETURN(sa_rotate_qkv(cfg, rot, x.in[0], x.stride[0], x.in[1], x.stride[1], x.in[2], x.stride[2], x.positions, n < 0 ? 0 : n, out[0], out[1], out[2], s));
+}
+
+// (cfg, rotary, dtype, device of the tables, cache, Q, K, V, positions, cu_lens, Q_out, bump_lens)
+PyObject* append_qkv(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+    Args a{v, n_args};
+    const sa_config* cfg = a.structure<sa_config>();
+    const sa_rotary* rot = a.structure<sa_rotary>();
+    PyObject* dtype = a.bad ? nullptr : a.next();
+    const long long tables = a.integer(), dev = a.current_device();
+    if (!a.bad && tables >= 0 && tables != dev) a.fail("the tables lie on another device than the current one");
+    const sa_cache* cache = a.structure<sa_cache>();
+    Projections x;
+    x.take(a, cfg, dtype, dev);
+    x.take_positions(a, rot, dev);
+    HostArray cu(a, a.bad || cache->batch < 0 ? 1 : (Py_ssize_t)cache->batch + 1, false, "cu_lens holds at least batch + 1 64-bit integers");
+    PyObject* o = a.bad ? nullptr : a.next();
+    uint16_t* out = nullptr;
+    long long sh[3];
+    if (!a.bad && o != Py_None) {
+        if (!a.shape(o, 3, sh) || sh[0] != x.n || sh[1] != cfg->n_q_heads || sh[2] != cfg->head_dim || !a.binary16(o) || !a.contiguous(o) || !a.on_device(o, dev))
+            a.fail("Q_out is contiguous [n, n_q_heads, head_dim] of float16 (or int16, uint16 for its bits) on the current CUDA device");
+        out = a.address<uint16_t>(o);
+    }
+    const int bump = a.integer();
+    // (a tensor without elements has no address, which would read as one that is not there)
+    if (!a.bad && x.n == 0 && cache->batch >= 0 && cu.p[cache->batch] == 0 && cu.p[0] == 0) return PyLong_FromLong(SA_OK);
+    const sa_stream s = a.stream();
+    SA_RETURN(sa_append_qkv(cfg, cache, rot, x.in[0], x.stride[0], x.in[1], x.stride[1], x.in[2], x.stride[2], x.positions, x.n < 0 ? 0 : x.n, cu.p, out, bump, s));
+}
+
+// (cfg, cache, Q, O, workspace, cu_lens, window, sinks)
+PyObject* chunk_attention(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    Args a{v, n};
+    const sa_config* cfg = a.structure<sa_config>();
+    const sa_cache* cache = a.structure<sa_cache>();
+    PyObject *Q = a.bad ? nullptr : a.next(), *O = a.bad ? nullptr : a.next();
+    size_t bytes;
+    void* ws = a.tensor_and_bytes(&bytes);
+    HostArray cu(a, a.bad || cache->batch < 0 ? 1 : (Py_ssize_t)cache->batch + 1, false, "cu_lens holds at least batch + 1 64-bit integers");
+    const int window = a.integer(), sinks = a.integer();
+    const long long dev = a.current_device(), rows = a.bad || cache->batch < 0 ? 0 : cu.p[cache->batch];
+    int dtype = SA_F16;
+    for (int i = 0; i < 2 && !a.bad; ++i) {
+        PyObject* o = i ? O : Q;
+        long long sh[3];
+        if (i && a.typed(o, g_bfloat16)) dtype = SA_BF16;
+        if (!a.shape(o, 3, sh) || sh[1] != cfg->n_q_heads || sh[2] != cfg->head_dim || sh[0] < rows || (dtype == SA_F16 && !a.binary16(o)) || !a.contiguous(o) || !a.on_device(o, dev))
+            a.fail("Q and O are contiguous [rows, n_q_heads, head_dim] of float16 (or int16, uint16 for its bits; O also bfloat16) on the current CUDA device, with a row for every token");
+    }
+    const uint16_t* q = a.address<const uint16_t>(Q);
+    void* o = a.address<void>(O);
+    const sa_stream s = a.stream();
+    SA_RETURN(sa_chunk_attention(cfg, cache, q, cu.p, window, sinks, o, dtype, ws, bytes, s));
 }
 
 PyMethodDef kMethods[] = {
+    {"append_qkv", (PyCFunction)(void (*)(void))append_qkv, METH_FASTCALL, nullptr},
+    {"chunk_attention", (PyCFunction)(void (*)(void))chunk_attention, METH_FASTCALL, nullptr},
     {"read_kv", (PyCFunction)(void (*)(void))read_kv, METH_FASTCALL, nullptr},
     {"rotate_qkv", (PyCFunction)(void (*)(void))rotate_qkv, METH_FASTCALL, nullptr},
     {"fill_kv", (PyCFunction)(void (*)(void))fill_kv, METH_FASTCALL, nullptr},
@@ -368,10 +438,11 @@ PyMODINIT_FUNC PyInit__native(void) {
     g_float16 = torch ? PyObject_GetAttrString(torch, "float16") : nullptr;
     g_int16 = torch ? PyObject_GetAttrString(torch, "int16") : nullptr;
     g_uint16 = torch ? PyObject_GetAttrString(torch, "uint16") : nullptr;
+    g_bfloat16 = torch ? PyObject_GetAttrString(torch, "bfloat16") : nullptr;
     g_int32 = torch ? PyObject_GetAttrString(torch, "int32") : nullptr;
     Py_XDECREF(torch);
     g_dtype = PyUnicode_InternFromString("dtype");
     g_device_of = PyUnicode_InternFromString("get_device");
-    if (!g_get_device || !g_get_stream || !g_data_ptr || !g_nbytes || !g_shape || !g_stride || !g_is_contiguous || !g_float16 || !g_int16 || !g_uint16 || !g_int32 || !g_dtype || !g_device_of) return nullptr;
+    if (!g_get_device || !g_get_stream || !g_data_ptr || !g_nbytes || !g_shape || !g_stride || !g_is_contiguous || !g_float16 || !g_int16 || !g_uint16 || !g_int32 || !g_bfloat16 || !g_dtype || !g_device_of) return nullptr;
     return PyModule_Create(&kModule);
 }
