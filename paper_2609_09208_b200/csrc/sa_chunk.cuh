@@ -22,6 +22,7 @@
 // equal stretches, one a block.  A unit that a cut goes through leaves partial sums in the workspace, two places a block, for chunk_merge_kernel.
 #pragma once
 #include <cuda_bf16.h>
+#include <type_traits>
 
 #include "sa_cache_write.cuh"
 #include "sa_common.cuh"
@@ -33,7 +34,20 @@
 namespace sa {
 
 constexpr int kChunkBatch = 128;          // sequences per launch
-constexpr int kChunkThreads = 448;        // 2 x 4 warps of softmax, 4 of operands, products, loader
+// Warps of a block: softmax of two streams, 8 each (SPLIT: 4), 4 of operands (SPLIT: 4 of keys and 4 of values), then products, loader and two idle ones.
+SA_HD constexpr int chunk_softmax_warps(bool split) { return split ? 8 : 16; }
+SA_HD constexpr int chunk_operand_warps(bool split) { return split ? 8 : 4; }
+SA_HD constexpr int chunk_threads(bool split) { return 32 * (chunk_softmax_warps(split) + chunk_operand_warps(split) + 4); }
+// Registers of a thread: what the block is launched with, and what the groups of four warps then have of it.
+struct ChunkRegisters {
+    int launch, softmax, operand, other;
+};
+SA_HD constexpr ChunkRegisters chunk_registers(bool split) { return split ? ChunkRegisters{96, 136, 80, 48} : ChunkRegisters{80, 88, 80, 48}; }
+SA_HD constexpr bool chunk_registers_fit(bool split) {
+    const ChunkRegisters r = chunk_registers(split);
+    return 32 * (chunk_softmax_warps(split) * r.softmax + chunk_operand_warps(split) * r.operand + 4 * r.other) <= chunk_threads(split) * r.launch && chunk_threads(split) * r.launch <= 65536;
+}
+static_assert(chunk_registers_fit(false) && chunk_registers_fit(true), "the groups' registers are those of the launch");
 constexpr int kChunkTile = 128;           // keys
 constexpr int kChunkUnitCost = 4;         // what a unit costs beside its tiles, in tiles
 constexpr int kChunkPlanBytes = 16384;    // of the workspace, ahead of the partial sums: a ChunkCut a block
@@ -99,32 +113,25 @@ SA_D ChunkUnit chunk_unit(const ChunkArgs& a, const int* lens, int flat, int per
     return u;
 }
 
-// The pieces of a block, in order; every warp walks through them by itself.
+// A piece of a block's work as its warps read it, in shared memory.
 struct ChunkPiece {
-    ChunkUnit u;
-    int head, flat, begin, end;           // tiles begin .. end - 1 of the unit's
-    SA_D bool whole() const { return begin == 0 && end == u.count; }
-};
-struct ChunkWalk {
-    int head, flat, skip;                 // the unit, and how far into it (its fixed cost included) the stretch starts
-    long long left;                       // of the stretch
-    SA_D bool next(const ChunkArgs& a, const int* lens, int per_tile, ChunkPiece& p) {
-        while (left > 0) {
-            p.u = chunk_unit(a, lens, flat, per_tile);
-            p.head = head;
-            p.flat = flat;
-            const int cost = kChunkUnitCost + p.u.count, from = skip;
-            const int to = left < cost - from ? from + (int)left : cost;
-            left -= to - from;
-            skip = 0;
-            if (++flat == a.s.tiles[a.s.n]) flat = 0, ++head;
-            p.begin = max(from - kChunkUnitCost, 0);
-            p.end = max(to - kChunkUnitCost, 0);
-            if (p.end > p.begin || (p.u.count == 0 && from == 0)) return true;
-        }
-        return false;
+    int n;                                // key tiles; -1: no more pieces
+    int head, b;
+    int rows, token_row, token;           // row r is row token_row + r of the heads of the group, counted from token `token` (of the sequence) on
+    int64_t q_token;                      // that token's row in Q and O
+    int lo, hi;                           // keys lo .. hi - 1, and below sinks
+    int sink_tiles, window_tile, begin;   // of the unit; the piece's first tile
+    int place;                            // 0: the whole unit; 1, 2: its sums go to the block's first, second place
+    int first[2], last[2];                // of the streams: positions of the first and last row's token
+    SA_D int tile(int i) const { return begin + i < sink_tiles ? begin + i : window_tile + begin + i - sink_tiles; }
+    // Row r: its token's position, its row (of heads) in Q and O.
+    SA_D int position(const ChunkArgs& a, int r) const { return token + (token_row + r) / a.G; }
+    SA_D int64_t row(const ChunkArgs& a, int r) const {
+        const int at = token_row + r, t = at / a.G;
+        return (q_token + t) * a.Hq + head * a.G + (at - t * a.G);
     }
 };
+constexpr int kChunkPieces = 8;           // of them in the ring, as the loader may be several ahead
 
 // Shared memory of a block.
 template <int D, int FMT>
@@ -134,7 +141,7 @@ struct ChunkShape {
     static constexpr int kRaw = 4 * kHalf;                            // records of a tile
     static constexpr int kOperand = D / 64 * 16384;                   // 128 rows
     static constexpr int kBuffers = D == 64 ? 2 : 1;                  // of operands
-    static constexpr int kFixed = (2 + 2 * kBuffers) * kOperand + 8192;
+    static constexpr int kFixed = (2 + 2 * kBuffers) * kOperand + 10240;
     static constexpr int kFit = (227 * 1024 - 1024 - kFixed) / kRaw;
     static constexpr int kStages = kFit > 4 ? 4 : kFit;
     static constexpr int kBytes = 1024 + kFixed + kStages * kRaw;     // (1024: to align)
@@ -143,29 +150,63 @@ struct ChunkShape {
     static constexpr bool kScaled = FMT != FMT_FP16 && FMT != FMT_FP4;                                  // keys have a scale of their own
     static constexpr bool kBf16 = kScaled && FMT != FMT_INT8;                                           // type of keys and queries
     static_assert(kStages >= 1, "a tile's records have to fit");
+    // Columns of tensor memory: scores of the streams, 128 each; sums; at head_dim 64 the weights have a place of their own, so that the next tile's scores are
+    // under way while the softmax works on the last one's; at 128 they take the scores'.
+    static constexpr bool kApart = D == 64;
+    SA_HD static constexpr uint32_t weights(int stream) { return kApart ? 384 + 64 * stream : 128 * stream; }
+    SA_HD static constexpr uint32_t sums(int stream) { return 256 + D * stream; }
 };
 struct ChunkShared {                      // behind the rings
     float scale[4][kChunkTile];           // of the keys of four tiles
-    float m[256], l[256];
-    uint32_t pages[4];                    // which of a tile's pages there are
+    float m[256], l[256];                 // SPLIT: of all threads' rows
+    float meet[2][512];                   // else: what the two halves of a row tell each other
+    int2 info[4];                         // of four tiles: first key; bits 0, 1: pages there are, 2, 3: streams whose rows see all of the tile
+    ChunkPiece pieces[kChunkPieces];
+    unsigned long long piece_full[kChunkPieces], piece_empty[kChunkPieces];
     uint32_t raw_info[4];
-    unsigned long long raw_full[4], raw_empty[4], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2], o_full[2], done;
+    unsigned long long raw_full[4], raw_empty[4], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], s_free[2], p_full[2], o_full[2], done;
     int lens[kChunkBatch];
     uint32_t tmem;
     int start_head, start_flat, start_skip;
-    long long sums[16];
+    long long sums[24];
 };
-static_assert(sizeof(ChunkShared) <= 8192, "room behind the rings");
+static_assert(sizeof(ChunkShared) <= 10240, "room behind the rings");
 
-// A wait that ends: where the limit is reached, nothing is waited for any more and the outputs become NaN.
+// A wait that ends: where the limit is reached, nothing is waited for any more and the outputs become NaN.  A poll may sleep up to 2 us, so that waiting warps leave
+// their issue slots to the others (without it a tenth of all instructions were polls), and the limit is a third of a second.
 struct ChunkWait {
     bool lost = false;
-    SA_D void one(const unsigned long long& bar, uint32_t parity) {
-        if (!lost) lost = !mbar_wait_bounded(smem_addr(&bar), parity);
+    SA_D static bool poll(uint32_t bar, uint32_t parity) {
+        uint32_t ok;
+        asm volatile("{.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
+        return ok != 0;
     }
-    SA_D void operator()(const unsigned long long& bar, uint32_t parity) {      // a whole warp
-        one(bar, parity);
+    SA_D void operator()(const unsigned long long& bar, uint32_t parity) {      // by a whole warp
+        const uint32_t at = smem_addr(&bar);
+        if (!lost && !poll(at, parity)) {
+            lost = true;
+#pragma unroll 1
+            for (uint32_t i = 0; i < kWaitLimit && lost; ++i) lost = !poll(at, parity);
+        }
         __syncwarp();
+    }
+};
+
+// The pieces, one after another: next() gives the one at hand (null: no more), leave() hands its place back.  By a whole warp.  (Its waits are its own: warps that have given
+// up on a tile go on from piece to piece, so that all rows of the block come out as NaN.)
+struct ChunkReader {
+    ChunkShared& sh;
+    ChunkWait wait{};
+    uint32_t i = 0;
+    SA_D const ChunkPiece* next() {
+        wait(sh.piece_full[i % kChunkPieces], i / kChunkPieces & 1);
+        const ChunkPiece* p = &sh.pieces[i % kChunkPieces];
+        return wait.lost || p->n < 0 ? nullptr : p;
+    }
+    SA_D void leave() {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(smem_addr(&sh.piece_empty[i % kChunkPieces]));
+        ++i;
     }
 };
 
@@ -189,144 +230,172 @@ SA_D uint32_t plane_pair(uint32_t p, int i) {
     return ((q | q << 15) & 0x00010001u) << AT;
 }
 
-// The key of one token (t of a half) as a row of the operand.
-template <int D, int FMT>
-SA_D void chunk_key(const uint8_t* half, int t, uint32_t operand, int row) {
-    const uint4* chunk = reinterpret_cast<const uint4*>(half) + t;                      // + 32 k: chunk k
-    if constexpr (FMT == FMT_FP16) {
+// INT8 values 2 I, 2 I + 1 of a word as binary16 numbers 1152 larger: the biased byte in the low mantissa bits of 1024.
+template <int I>
+SA_D uint32_t int8_biased(uint32_t w) { return __byte_perm(w ^ 0x80808080u, 0x64646464u, I ? 0x4342u : 0x4140u); }
+SA_D uint32_t add_half2_1152(uint32_t h) {
+    asm("add.rn.f16x2 %0, %0, %1;" : "+r"(h) : "r"(0xe480e480u));
+    return h;
+}
+SA_D uint32_t fma_half2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t d;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
+SA_D uint32_t twice_half(float x) { return (uint32_t)__half_as_ushort(__float2half_rn(x)) * 0x10001u; }
+// The codes of one token's key (KEY) or value (t of a half): read at once, then put into a row of the operand (zeros: not seen).
+template <int D, int FMT, bool KEY>
+struct ChunkCodes {
+    using S = ChunkShape<D, FMT>;
+    static constexpr bool kPairs = FMT == FMT_FP4 && !KEY;             // 4-bit values: a byte is two tokens' nibbles
+    static constexpr int kPlanes = !KEY ? 0 : FMT == FMT_PLANAR1 ? 1 : FMT == FMT_PLANAR2 ? 2 : 0;
+    static constexpr bool kNibbles = KEY && (FMT == FMT_NIBBLE || FMT == FMT_PLANAR1 || FMT == FMT_PLANAR2);
+    static constexpr int kChunks = FMT == FMT_FP16 ? D / 8 : FMT == FMT_FP4 || kNibbles ? D / 32 : D / 16;
+    static constexpr int kAhead = FMT == FMT_FP16 ? 4 : kChunks;       // chunks that are read ahead of the wait for the operand's place
+    uint4 w[kPairs ? 1 : kAhead];
+    uint32_t plane[kPlanes ? kPlanes * D / 32 : 1];
+
+    SA_D static const uint4* chunk(const uint8_t* half, int t) { return reinterpret_cast<const uint4*>(half + (KEY ? 0 : S::kV)) + t; }      // + 32 k: chunk k
+    SA_D ChunkCodes(const uint8_t* half, int t) {
+        if constexpr (!kPairs) {
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-            const uint4 w = chunk[32 * c];
-            put_operand(operand, row, c, w.x, w.y, w.z, w.w);
+            for (int k = 0; k < kAhead; ++k) w[k] = chunk(half, t)[32 * k];
         }
-    } else if constexpr (FMT == FMT_FP4) {
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            const uint4 v = chunk[32 * k];
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        for (int bit = 0; bit < kPlanes; ++bit)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t b = half[16 * D + k / 2 * 128 + i * 32 + t % 8 * 4 + t / 8], s = b << 7 | b << 23;
-                uint32_t h[4];
-                fp4_to_half2(w[i], h);
-                put_operand(operand, row, 8 * (k / 2) + 2 * i + k % 2, mul_half2(h[0], s), mul_half2(h[1], s), mul_half2(h[2], s), mul_half2(h[3], s));
+            for (int k = 0; k < D / 32; ++k) plane[bit * (D / 32) + k] = *reinterpret_cast<const uint32_t*>(half + 16 * D + (bit * kTileTokens + t) * (D / 8) + 4 * k);
+    }
+    SA_D void put(const uint8_t* half, int t, uint32_t operand, int row, bool seen) {
+        auto to = [&](int c, uint32_t a, uint32_t b, uint32_t x, uint32_t y) { put_operand(operand, row, c, a, b, x, y); };
+        if constexpr (FMT == FMT_FP16) {
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+                const uint4 v = w[c % kAhead];
+                if (c + kAhead < D / 8) w[c % kAhead] = chunk(half, t)[32 * (c + kAhead)];
+                to(c, v.x, v.y, v.z, v.w);
             }
-        }
-    } else if constexpr (FMT == FMT_BYTE || FMT == FMT_INT8) {
+        } else if constexpr (kPairs) {
+            const uint8_t* at = half + S::kV + t % 8 / 2 * 16 + t / 16 * 4 + t / 8 % 2 * 2;
+            const uint8_t* scales = half + S::kV + 16 * D + t % 8 / 2 * 16 + t / 16 * 4 + t % 2 * 2 + t / 8 % 2;
+            const int shift = 4 * (t & 1);
+            uint32_t x[2][8], b[2];                                                     // of this block of 16 channels and the next: x[e]: channels e, e + 8
+            auto read = [&](int blk) {
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            const uint4 v = chunk[32 * k];
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            uint32_t h[8];
+                for (int e = 0; e < 8; ++e) x[blk % 2][e] = *reinterpret_cast<const uint16_t*>(at + blk / 2 * 512 + e * 64 + blk % 2 * 8);
+                b[blk % 2] = scales[blk / 2 * 64 + blk % 2 * 8];
+            };
+            read(0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (FMT == FMT_BYTE) {
-                    h[2 * i] = byte_codes_to_bf16<0>(w[i], 1u);
-                    h[2 * i + 1] = byte_codes_to_bf16<2>(w[i], 1u);
-                } else {
-                    const uint32_t even = int8_to_half2<false>(w[i]), odd = int8_to_half2<true>(w[i]);
-                    h[2 * i] = __byte_perm(even, odd, 0x5410);
-                    h[2 * i + 1] = __byte_perm(even, odd, 0x7632);
+            for (int blk = 0; blk < D / 16; ++blk) {
+                if (blk + 1 < D / 16) read(blk + 1);
+                uint32_t n[8], h[4];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) n[e] = x[blk % 2][e] >> shift & 0x0f0fu;
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) n[e] |= n[e + 1] << 4;
+                const uint32_t lo = n[0] | n[2] << 16, hi = n[4] | n[6] << 16, s = b[blk % 2] << 7 | b[blk % 2] << 23;
+                const uint32_t word[2] = {__byte_perm(lo, hi, 0x6420), __byte_perm(lo, hi, 0x7531)};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    fp4_to_half2(word[i], h);
+                    to(2 * blk + i, mul_half2(h[0], s), mul_half2(h[1], s), mul_half2(h[2], s), mul_half2(h[3], s));
                 }
             }
-            put_operand(operand, row, 2 * k, h[0], h[1], h[2], h[3]);
-            put_operand(operand, row, 2 * k + 1, h[4], h[5], h[6], h[7]);
-        }
-    } else {
-        constexpr int K = FMT == FMT_PLANAR1 ? 1 : FMT == FMT_PLANAR2 ? 2 : 0;
+        } else if constexpr (FMT == FMT_FP4) {
+            uint32_t b[D / 16];
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) {
-            const uint4 v = chunk[32 * k];
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            uint32_t plane[K ? K : 1] = {};
+            for (int i = 0; i < D / 16; ++i) b[i] = half[16 * D + i / 4 * 128 + i % 4 * 32 + t % 8 * 4 + t / 8];
 #pragma unroll
-            for (int bit = 0; bit < K; ++bit) plane[bit] = *reinterpret_cast<const uint32_t*>(half + 16 * D + (bit * kTileTokens + t) * (D / 8) + 4 * k);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t h[4];
+            for (int k = 0; k < D / 32; ++k) {
+                const uint32_t code[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    h[i] = nibbles_to_bf16(w[c], i);
-                    if constexpr (K == 1) h[i] |= plane_pair<6>(plane[0] >> (8 * c), i);
-                    if constexpr (K == 2) h[i] |= plane_pair<5>(plane[0] >> (8 * c), i) | plane_pair<6>(plane[1] >> (8 * c), i);
+                    const uint32_t s = b[k / 2 * 4 + i] << 7 | b[k / 2 * 4 + i] << 23;
+                    uint32_t h[4];
+                    fp4_to_half2(code[i], h);
+                    to(8 * (k / 2) + 2 * i + k % 2, mul_half2(h[0], s), mul_half2(h[1], s), mul_half2(h[2], s), mul_half2(h[3], s));
                 }
-                put_operand(operand, row, 4 * k + c, h[0], h[1], h[2], h[3]);
             }
+        } else if constexpr (KEY && !kNibbles) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const uint32_t code[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                uint32_t h[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (FMT == FMT_BYTE) {
+                        h[2 * i] = byte_codes_to_bf16<0>(code[i], 1u);
+                        h[2 * i + 1] = byte_codes_to_bf16<2>(code[i], 1u);
+                    } else {
+                        h[2 * i] = add_half2_1152(int8_biased<0>(code[i]));
+                        h[2 * i + 1] = add_half2_1152(int8_biased<1>(code[i]));
+                    }
+                }
+                to(2 * k, h[0], h[1], h[2], h[3]);
+                to(2 * k + 1, h[4], h[5], h[6], h[7]);
+            }
+        } else if constexpr (KEY) {
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                const uint32_t code[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t h[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        h[i] = nibbles_to_bf16(code[c], i);
+                        if constexpr (kPlanes == 1) h[i] |= plane_pair<6>(plane[k] >> (8 * c), i);
+                        if constexpr (kPlanes == 2) h[i] |= plane_pair<5>(plane[k] >> (8 * c), i) | plane_pair<6>(plane[D / 32 + k] >> (8 * c), i);
+                    }
+                    to(4 * k + c, h[0], h[1], h[2], h[3]);
+                }
+            }
+        } else {
+            // times 2^-g in two exact steps: the first (with the bias of the bytes taken off) keeps clear of the subnormal and of the largest numbers; the product is a number that
+            // binary16 has, as the value that was rounded was one, but for 65536, which becomes the largest
+            const int g = (int)(int8_t)half[S::kMeta + t * 4 + 2], g1 = max(-5, min(g, 12));
+            const uint32_t f1 = twice_half(pow2i(-g1)), off = twice_half(-1152.0f * pow2i(-g1)), f2 = twice_half(pow2i(max(g1 - g, -40)));
+            const bool twice = __any_sync(0xffffffffu, g != g1);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const uint32_t code[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+                uint32_t h[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    h[2 * i] = fma_half2(int8_biased<0>(code[i]), f1, off);
+                    h[2 * i + 1] = fma_half2(int8_biased<1>(code[i]), f1, off);
+                }
+                if (twice) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        h[i] = mul_half2(h[i], f2);
+                        asm("{.reg .b32 m; mov.b32 m, 0x7bff7bff; min.f16x2 %0, %0, m; neg.f16x2 m, m; max.f16x2 %0, %0, m;}" : "+r"(h[i]));
+                    }
+                }
+                to(2 * k, h[0], h[1], h[2], h[3]);
+                to(2 * k + 1, h[4], h[5], h[6], h[7]);
+            }
+        }
+        if (!seen) {
+#pragma unroll 1
+            for (int c = 0; c < D / 8; ++c) to(c, 0u, 0u, 0u, 0u);
         }
     }
-}
-// Its value.
-template <int D, int FMT>
-SA_D void chunk_value(const uint8_t* half, int t, uint32_t operand, int row) {
-    using S = ChunkShape<D, FMT>;
-    const uint8_t* v = half + S::kV;
-    if constexpr (FMT == FMT_FP16) {
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-            const uint4 w = reinterpret_cast<const uint4*>(v)[32 * c + t];
-            put_operand(operand, row, c, w.x, w.y, w.z, w.w);
-        }
-    } else if constexpr (FMT == FMT_FP4) {
-        const uint8_t* at = v + t % 8 / 2 * 16 + t / 16 * 4 + t / 8 % 2 * 2;
-        const uint8_t* scales = v + 16 * D + t % 8 / 2 * 16 + t / 16 * 4 + t % 2 * 2 + t / 8 % 2;
-        const int shift = 4 * (t & 1);
-#pragma unroll
-        for (int blk = 0; blk < D / 16; ++blk) {
-            uint32_t x[8], w[2], h[4];                                                  // x[e]: channels e, e + 8 of the block
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = (uint32_t)*reinterpret_cast<const uint16_t*>(at + blk / 2 * 512 + e * 64 + blk % 2 * 8) >> shift & 0x0f0fu;
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) x[e] |= x[e + 1] << 4;
-            const uint32_t lo = x[0] | x[2] << 16, hi = x[4] | x[6] << 16;
-            w[0] = __byte_perm(lo, hi, 0x6420);
-            w[1] = __byte_perm(lo, hi, 0x7531);
-            const uint32_t b = scales[blk / 2 * 64 + blk % 2 * 8], s = b << 7 | b << 23;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fp4_to_half2(w[i], h);
-                put_operand(operand, row, 2 * blk + i, mul_half2(h[0], s), mul_half2(h[1], s), mul_half2(h[2], s), mul_half2(h[3], s));
-            }
-        }
-    } else {
-        // times 2^-g in two exact steps: the first keeps clear of the subnormal numbers; the product is a number that binary16 has, as the value that was
-        // rounded was one, but for 65536, which becomes the largest
-        const int g = (int)(int8_t)half[S::kMeta + t * 4 + 2], g1 = max(-9, min(g, 12));
-        const __half f1h = __float2half_rn(pow2i(-g1)), f2h = __float2half_rn(pow2i(max(g1 - g, -40)));
-        const uint32_t f1 = (uint32_t)__half_as_ushort(f1h) * 0x10001u, f2 = (uint32_t)__half_as_ushort(f2h) * 0x10001u;
-        const bool twice = __any_sync(0xffffffffu, g != g1);
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            const uint4 in = reinterpret_cast<const uint4*>(v)[32 * k + t];
-            const uint32_t w[4] = {in.x, in.y, in.z, in.w};
-            uint32_t h[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t even = int8_to_half2<false>(w[i]), odd = int8_to_half2<true>(w[i]);
-                h[2 * i] = mul_half2(__byte_perm(even, odd, 0x5410), f1);
-                h[2 * i + 1] = mul_half2(__byte_perm(even, odd, 0x7632), f1);
-            }
-            if (twice)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    h[i] = mul_half2(h[i], f2);
-                    asm("{.reg .b32 m; mov.b32 m, 0x7bff7bff; min.f16x2 %0, %0, m; neg.f16x2 m, m; max.f16x2 %0, %0, m;}" : "+r"(h[i]));
-                }
-            put_operand(operand, row, 2 * k, h[0], h[1], h[2], h[3]);
-            put_operand(operand, row, 2 * k + 1, h[4], h[5], h[6], h[7]);
-        }
-    }
-}
+};
 
-// The 32 queries of a warp as rows of the operand, D / 16 lanes a row; returns the factor of the lane's own row.  row_of(r): row r's binary16 numbers, or null.
-template <int D, int FMT, typename RowOf>
-SA_D float chunk_queries(const ChunkArgs& a, uint32_t operand, int lane, int first_row, RowOf row_of) {
+// 32 queries (HALVES = 2: the first or, with half = 1, the last 16 of them) as rows of the operand, D / 16 lanes a row; returns the factor of the lane's own row, if it is one of
+// them.  row_of(r): row r's binary16 numbers, or null.
+template <int D, int FMT, int HALVES, typename RowOf>
+SA_D float chunk_queries(const ChunkArgs& a, uint32_t operand, int lane, int first_row, int half, RowOf row_of) {
     using S = ChunkShape<D, FMT>;
-    constexpr int LPV = D / 16, RPW = 32 / LPV, STEPS = 32 / RPW;
+    constexpr int LPV = D / 16, RPW = 32 / LPV, STEPS = 32 / RPW / HALVES;
+    const int row0 = half * STEPS * RPW;
     const Fp4Half<D> f(lane, 0);
     uint32_t x[STEPS][8];
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
-        const uint16_t* p = row_of(i * RPW + lane / LPV);
+        const uint16_t* p = row_of(row0 + i * RPW + lane / LPV);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[i][e] = 0u;
         if (p) load_32_bytes(p + 16 * f.blk, (reinterpret_cast<uintptr_t>(a.Q) & 31) == 0, x[i]);
@@ -356,9 +425,9 @@ SA_D float chunk_queries(const ChunkArgs& a, uint32_t operand, int lane, int fir
                 }
             }
             const float d = __shfl_sync(0xffffffffu, top ? delta : 1.0f, (lane % RPW) * LPV);      // (a query of zeros: any factor but zero)
-            if (lane / RPW == i) mine = d * a.factor;
+            if (lane / RPW == half * STEPS + i) mine = d * a.factor;
         }
-        const int row = first_row + i * RPW + lane / LPV;
+        const int row = first_row + row0 + i * RPW + lane / LPV;
         put_operand(operand, row, 2 * f.blk, x[i][0], x[i][1], x[i][2], x[i][3]);
         put_operand(operand, row, 2 * f.blk + 1, x[i][4], x[i][5], x[i][6], x[i][7]);
     }
@@ -378,6 +447,164 @@ SA_D uint32_t chunk_out(float a, float b, int bf16) {
 SA_D uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 SA_D void chunk_sync(int barrier, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory"); }
 
+template <int N>
+SA_D void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+SA_D void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// A row's softmax: reference and sum of weights (in its units), factor from a product's units to the log2 domain.
+struct ChunkRow {
+    float m, l, factor;
+};
+// Which columns of a tile (whose first key is t0) a row sees.  whole: all.
+struct ChunkMask {
+    int t0, pages;
+    bool whole;
+    int position, window, sinks;
+};
+SA_D float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// 32 columns of a row's scores, in registers x: times the keys' scales.
+template <int D, int FMT>
+SA_D void chunk_scores(const uint32_t (&x)[32], f32x2 (&y)[16], const float* scale, int c) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) y[e] = pack_f32x2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
+    if constexpr (ChunkShape<D, FMT>::kScaled) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+            const float4 s4 = *reinterpret_cast<const float4*>(scale + 32 * c + 2 * e);
+            y[e] = mul2(y[e], pack_f32x2(s4.x, s4.y));
+            y[e + 1] = mul2(y[e + 1], pack_f32x2(s4.z, s4.w));
+        }
+    }
+}
+// Scores of hidden keys become -inf where they lie, in tensor memory: few tiles need it, and in registers the others would pay for the meeting of the branches
+// with a move of every score.
+template <int C>
+SA_D void chunk_hide(const ChunkMask& mask, uint32_t s_col, int chunk0) {
+    const int hi = mask.position - mask.t0, sink = mask.sinks - mask.t0;
+    const int lo = mask.window && mask.position >= 0 ? (int)max((long long)hi - mask.window + 1, -0x40000000ll) : -0x40000000;
+#pragma unroll 1
+    for (int c = chunk0; c < chunk0 + C; ++c) {
+        uint32_t x[32];
+        tmem_load(s_col + 32 * c, x);
+        tmem_loaded();
+        const int at = 32 * c;
+        const uint32_t seen = (mask.pages >> (c >> 1) & 1u) ? bits_below(hi - at + 1) & (~bits_below(lo - at) | bits_below(sink - at)) : 0u;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = seen >> e & 1u ? x[e] : 0xff800000u;
+        tmem_store(s_col + 32 * c, x);
+    }
+    tmem_stored();
+}
+SA_D void chunk_largest(const f32x2 (&y)[16], float (&top)[4]) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        float v, w;
+        unpack_f32x2(y[e], &v, &w);
+        top[e & 3] = max3(top[e & 3], v, w);
+    }
+}
+// The reference follows the largest score; returns what the sums so far are worth in its units.
+SA_D float chunk_reference(ChunkRow& row, float top, bool& grown) {
+    const float z = top * row.factor;
+    grown = z > row.m + 8.0f;
+    const float shrink = grown ? ex2_approx(row.m - z) : 1.0f;
+    if (grown) row.m = z;
+    row.l *= shrink;
+    return shrink;
+}
+// Weights of 32 columns, and their sum to l (of the numbers ahead of their rounding: with the sum of the rounded ones outputs are no nearer, and a fifth more instructions).
+SA_D void chunk_weights(const ChunkRow& row, const f32x2 (&y)[16], uint32_t (&w)[16], f32x2 (&l)[2]) {
+    const f32x2 f2 = pack_f32x2(row.factor, row.factor), m2 = pack_f32x2(7.0f - row.m, 7.0f - row.m);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        float u0, u1;
+        unpack_f32x2(ffma2(y[e], f2, m2), &u0, &u1);
+        u0 = ex2_approx(u0);
+        u1 = ex2_approx(u1);
+        w[e] = half2_of(u0, u1);
+        l[e & 1] = add2(l[e & 1], pack_f32x2(u0, u1));
+    }
+}
+template <int D>
+SA_D void chunk_shrink(uint32_t o_col, float shrink) {
+#pragma unroll 1
+    for (int c = 0; c < D; c += 16) {
+        uint32_t o[16];
+        tmem_load(o_col + c, o);
+        tmem_loaded();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * shrink);
+        tmem_store(o_col + c, o);
+    }
+}
+SA_D void chunk_scores_read(bool apart, uint32_t free_scores) {
+    if (!apart) return;
+    tcgen05_before_sync();
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) mbar_arrive(free_scores);
+}
+// One tile of a row: columns 32 chunk0 .. of the scores (32 C of them) to weights.  free_scores: mbarrier, where the scores' place is apart from the weights';
+// ahead(): waits until weights and sums may be written; all(x): the largest x of the row's threads; sums: there are some, OUT channels of them from o_col for this thread to
+// rescale.  TWICE: the scores are read once for the largest and again for the weights, by a thread without the registers for all of them.
+template <int D, int FMT, int C, bool TWICE, int OUT, typename Ahead, typename All>
+SA_D void chunk_softmax(ChunkRow& row, const ChunkMask& mask, const float* scale, uint32_t s_col, uint32_t p_col, int chunk0, uint32_t free_scores, Ahead ahead, All all, bool sums, uint32_t o_col) {
+    using S = ChunkShape<D, FMT>;
+    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    f32x2 l[2] = {pack_f32x2(0.0f, 0.0f), pack_f32x2(0.0f, 0.0f)};
+    bool grown;
+    if (!mask.whole) chunk_hide<C>(mask, s_col, chunk0);
+    if constexpr (TWICE) {
+        uint32_t x[32], w[16];
+        f32x2 y[16];
+#pragma unroll 1
+        for (int c = chunk0; c < chunk0 + C; ++c) {
+            tmem_load(s_col + 32 * c, x);
+            tmem_loaded();
+            chunk_scores<D, FMT>(x, y, scale, c);
+            chunk_largest(y, top);
+        }
+        const float shrink = chunk_reference(row, all(fmaxf(max3(top[0], top[1], top[2]), top[3])), grown);
+        ahead();
+        if (sums && __any_sync(0xffffffffu, grown)) chunk_shrink<OUT>(o_col, shrink);
+#pragma unroll 1
+        for (int c = chunk0; c < chunk0 + C; ++c) {                    // (weights in the scores' place: 16 c .. is behind what has been read)
+            tmem_load(s_col + 32 * c, x);
+            tmem_loaded();
+            chunk_scores<D, FMT>(x, y, scale, c);
+            chunk_weights(row, y, w, l);
+            tmem_store(p_col + 16 * c, w);
+        }
+        chunk_scores_read(S::kApart, free_scores);
+    } else {
+        uint32_t x[C][32], w[C][16];
+        f32x2 y[C][16];
+#pragma unroll
+        for (int c = 0; c < C; ++c) tmem_load(s_col + 32 * (chunk0 + c), x[c]);
+        tmem_loaded();
+        chunk_scores_read(S::kApart, free_scores);
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            chunk_scores<D, FMT>(x[c], y[c], scale, chunk0 + c);
+            chunk_largest(y[c], top);
+        }
+        const float shrink = chunk_reference(row, all(fmaxf(max3(top[0], top[1], top[2]), top[3])), grown);
+#pragma unroll
+        for (int c = 0; c < C; ++c) chunk_weights(row, y[c], w[c], l);
+        ahead();
+        if (sums && __any_sync(0xffffffffu, grown)) chunk_shrink<OUT>(o_col, shrink);
+#pragma unroll
+        for (int c = 0; c < C; ++c) tmem_store(p_col + 16 * (chunk0 + c), w[c]);
+    }
+    float l0, l1;
+    unpack_f32x2(add2(l[0], l[1]), &l0, &l1);
+    row.l += l0 + l1;
+}
+
 // Row r of a unit: its number in Q and O.
 SA_D int64_t chunk_row(const ChunkArgs& a, const ChunkUnit& u, int head, int r) {
     const int at = u.row0 + r, token = at / a.G;
@@ -385,9 +612,11 @@ SA_D int64_t chunk_row(const ChunkArgs& a, const ChunkUnit& u, int head, int r) 
 }
 
 template <int D, int FMT, bool SPLIT>
-__global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_constant__ ChunkArgs a) {
+__global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __grid_constant__ ChunkArgs a) {
     using S = ChunkShape<D, FMT>;
-    constexpr int kPerTile = chunk_rows(SPLIT), NB = S::kBuffers;
+    constexpr int kPerTile = chunk_rows(SPLIT), NB = S::kBuffers, kThreads = chunk_threads(SPLIT);
+    constexpr int kOperands = chunk_softmax_warps(SPLIT), kProducts = kOperands + chunk_operand_warps(SPLIT), kHalves = SPLIT ? 1 : 2;      // first warps; parts of a row's columns
+    constexpr ChunkRegisters kRegisters = chunk_registers(SPLIT);
     extern __shared__ uint8_t dynamic[];
     const uint32_t base = (smem_addr(dynamic) + 1023u) & ~1023u;
     uint8_t* const rings = dynamic + (base - smem_addr(dynamic));
@@ -400,17 +629,22 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
     if (tid == 0) {
         for (int i = 0; i < 4; ++i) {
             mbar_init(smem_addr(&sh.raw_full[i]), 1);
-            mbar_init(smem_addr(&sh.raw_empty[i]), 4);
+            mbar_init(smem_addr(&sh.raw_empty[i]), SPLIT ? 8 : 4);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_addr(&sh.k_full[i]), 4);
             mbar_init(smem_addr(&sh.v_full[i]), 4);
             mbar_init(smem_addr(&sh.k_empty[i]), 1);
             mbar_init(smem_addr(&sh.v_empty[i]), 1);
-            mbar_init(smem_addr(&sh.q_full[i]), 4);
+            mbar_init(smem_addr(&sh.q_full[i]), 4 * kHalves);
             mbar_init(smem_addr(&sh.s_full[i]), 2);                    // (the products' arrival, and the issuing thread's own, which hands on what it has seen)
-            mbar_init(smem_addr(&sh.p_full[i]), 4);
+            mbar_init(smem_addr(&sh.s_free[i]), 4 * kHalves);
+            mbar_init(smem_addr(&sh.p_full[i]), 4 * kHalves);
             mbar_init(smem_addr(&sh.o_full[i]), 1);
+        }
+        for (int i = 0; i < kChunkPieces; ++i) {
+            mbar_init(smem_addr(&sh.piece_full[i]), 1);
+            mbar_init(smem_addr(&sh.piece_empty[i]), chunk_softmax_warps(SPLIT) + chunk_operand_warps(SPLIT) + 2);
         }
         mbar_init(smem_addr(&sh.done), 1);
         fence_mbar_init();
@@ -422,7 +656,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
     const int n_flat = a.s.tiles[a.s.n];
     if (tid < a.s.n) sh.lens[tid] = max(a.c.seq_lens[a.s.b[tid]], 0);
     __syncthreads();
-    const int each = (n_flat + kChunkThreads - 1) / kChunkThreads, mine0 = min(tid * each, n_flat), mine1 = min(mine0 + each, n_flat);
+    const int each = (n_flat + kThreads - 1) / kThreads, mine0 = min(tid * each, n_flat), mine1 = min(mine0 + each, n_flat);
     long long cost = 0;
     for (int i = mine0; i < mine1; ++i) cost += kChunkUnitCost + chunk_unit(a, sh.lens, i, per_tile).count;
     long long ahead = cost;
@@ -435,7 +669,7 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
     __syncthreads();
     long long sum = 0;
     ahead -= cost;
-    for (int w = 0; w < kChunkThreads / 32; ++w) {
+    for (int w = 0; w < kThreads / 32; ++w) {
         if (w < warp) ahead += sh.sums[w];
         sum += sh.sums[w];
     }
@@ -462,171 +696,106 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
             sh.start_skip = (int)rest;
         }
     }
-    if (warp == 12) tmem_alloc(smem_addr(&sh.tmem));
+    if (warp == kProducts) tmem_alloc(smem_addr(&sh.tmem));
     tcgen05_before_sync();
     __syncthreads();
     tcgen05_after_sync();
-    const uint32_t tmem = sh.tmem;
-    ChunkWalk walk{sh.start_head, sh.start_flat, sh.start_skip, x1 - x0};
-    ChunkPiece p;
     ChunkWait wait;
+    ChunkReader reader{sh};
 
-    if (warp < 8) {
-        // ---- softmax: a row a thread
-        const int stream = warp >> 2, quarter = warp & 3, own = quarter * 32 + lane;
-        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), s_col = lanes + stream * 128, o_col = lanes + 256 + stream * D;
+    if (warp < kOperands) {
+        // ---- softmax: a row a thread (SPLIT), or half a row
+        const int stream = warp / (4 * kHalves), part = warp / 4 % kHalves, quarter = warp & 3, own = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_col = lanes + stream * 128, p_col = lanes + S::weights(stream), o_col = lanes + S::sums(stream);
         const uint32_t q_operand = q_at + stream * S::kOperand;
         const int copies = SPLIT ? a.copies : 1, rows_own = 128 / copies;
         const int row = SPLIT ? own % rows_own : stream * 128 + own;   // of the unit
-        const int chunks = 4 / copies, chunk0 = SPLIT ? own / rows_own * chunks : 0;      // columns of 32 that this thread has
-        uint32_t tiles_done = 0, pieces_done = 0, keys_done = 0;
-        bool cut_here = false;
-        while (walk.next(a, sh.lens, per_tile, p)) {
-            const ChunkUnit& u = p.u;
-            const bool there = row < u.rows;
-            const int position = there ? u.first + (u.row0 + row) / a.G - u.row0 / a.G : -1;
-            const int n = p.end - p.begin, mine = SPLIT ? (n + 1 - stream) / 2 : n;       // tiles of this stream
-            float m = -1e30f, l = 0.0f, f = a.factor;
+        const int chunks = 4 / (copies * kHalves), chunk0 = SPLIT ? own / rows_own * chunks : 2 * part;      // columns of 32 that this thread has
+        registers_up<kRegisters.softmax>();
+        uint32_t tiles_done = 0, keys_done = 0;
+        // The halves of a row meet at a barrier of their two warps, with a number of each (in turn in two places: one barrier a meeting will do).
+        int meetings = 0;
+        auto meet = [&](float x) {
+            float* at = sh.meet[meetings++ & 1];
+            at[tid] = x;
+            chunk_sync(2 + 4 * stream + quarter, 64);
+            return at[tid ^ 128];
+        };
+        while (const ChunkPiece* p = reader.next()) {
+            const int n = p->n, mine = SPLIT ? (n + 1 - stream) / 2 : n;                  // tiles of this stream
+            const int position = row < p->rows ? p->position(a, row) : -1;
+            ChunkRow r{-1e30f, 0.0f, a.factor};
             if (n > 0) {
                 const int first_row = SPLIT ? quarter * 32 : stream * 128 + quarter * 32;
-                f = chunk_queries<D, FMT>(a, q_operand, lane, quarter * 32, [&](int r) -> const uint16_t* {
-                    const int at = SPLIT ? (first_row + r) % rows_own : first_row + r;
-                    return at < u.rows ? a.Q + chunk_row(a, u, p.head, at) * D : nullptr;
-                });
+                auto query = [&](int k) -> const uint16_t* {
+                    const int at = SPLIT ? (first_row + k) % rows_own : first_row + k;
+                    return at < p->rows ? a.Q + p->row(a, at) * D : nullptr;
+                };
+                // (a half has the factors of its 16 rows in the lanes that the other half's 16 leave)
+                r.factor = chunk_queries<D, FMT, kHalves>(a, q_operand, lane, quarter * 32, part, query);
+                if constexpr (!SPLIT) {
+                    const float others = meet(r.factor);
+                    if (lane / 16 != part) r.factor = others;
+                }
                 fence_proxy_async();
                 tcgen05_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[stream]));
             }
-            // positions of the stream's first and last row: a tile that all of them see whole needs no masks
-            const int row_lo = SPLIT ? 0 : min(stream * 128, u.rows - 1), row_hi = SPLIT ? u.rows - 1 : min(stream * 128 + 127, u.rows - 1);
-            const int position_lo = u.first + (u.row0 + row_lo) / a.G - u.row0 / a.G, position_hi = u.first + (u.row0 + row_hi) / a.G - u.row0 / a.G;
             for (int i = 0; i < mine; ++i) {
-                const int j = SPLIT ? 2 * i + stream : i, t0 = u.tile(p.begin + j) * kChunkTile, slot = (keys_done + j) & 3;
+                const int slot = (keys_done + (SPLIT ? 2 * i + stream : i)) & 3;
                 wait(sh.s_full[stream], tiles_done & 1);
-                ++tiles_done;
                 tcgen05_after_sync();
-                const uint32_t pages = sh.pages[slot];
-                const float* scale = sh.scale[slot];
-                const bool plain = pages == 3u && position_lo - t0 >= kChunkTile - 1 && (a.window == 0 || position_hi - t0 < a.window || t0 + kChunkTile <= a.sinks);
-                const int hi = position - t0, lo = a.window && position >= 0 ? (int)max((long long)hi - a.window + 1, -0x40000000ll) : -0x40000000, sink = a.sinks - t0;
-                auto scores = [&](int c, f32x2 (&y)[16]) {             // columns 32 c .. of the row, times the keys' scales; -inf where they are hidden
-                    uint32_t x[32];
-                    tmem_load(s_col + 32 * c, x);
-                    tmem_loaded();
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) y[e] = pack_f32x2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1]));
-                    if constexpr (S::kScaled) {
-#pragma unroll
-                        for (int e = 0; e < 16; e += 2) {
-                            const float4 s4 = *reinterpret_cast<const float4*>(scale + 32 * c + 2 * e);
-                            y[e] = mul2(y[e], pack_f32x2(s4.x, s4.y));
-                            y[e + 1] = mul2(y[e + 1], pack_f32x2(s4.z, s4.w));
-                        }
-                    }
-                    if (!plain) {
-                        const uint32_t seen = (pages >> (c >> 1) & 1u) ? bits_below(hi - 32 * c + 1) & (~bits_below(lo - 32 * c) | bits_below(sink - 32 * c)) : 0u;
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            float v, w;
-                            unpack_f32x2(y[e], &v, &w);
-                            y[e] = pack_f32x2(seen >> (2 * e) & 1u ? v : -INFINITY, seen >> (2 * e + 1) & 1u ? w : -INFINITY);
-                        }
-                    }
+                const int2 info = sh.info[slot];
+                const ChunkMask mask{info.x, info.y, (info.y >> (2 + stream) & 1) != 0, position, a.window, a.sinks};
+                auto ahead = [&] {
+                    // the weights' place and the sums are free once the products of the tile before are done
+                    wait(sh.o_full[stream], (tiles_done & 1) ^ 1);
+                    tcgen05_after_sync();
                 };
-                float top = -INFINITY;
-#pragma unroll(SPLIT ? 1 : 4)
-                for (int c = chunk0; c < chunk0 + chunks; ++c) {
-                    f32x2 y[16];
-                    scores(c, y);
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float v, w;
-                        unpack_f32x2(y[e], &v, &w);
-                        top = fmaxf(top, fmaxf(v, w));
-                    }
-                }
-                const float z = top * f;
-                const bool grown = z > m + 8.0f;
-                if (__any_sync(0xffffffffu, grown)) {
-                    const float r = grown ? ex2_approx(m - z) : 1.0f;
-                    if (grown) m = z;
-                    l *= r;
-                    if (i > 0) {                                       // (the products of the tile before are done: the scores come behind them)
+                auto same = [](float x) { return x; };
+                const uint32_t read = smem_addr(&sh.s_free[stream]);
+                if constexpr (!SPLIT) {
+                    chunk_softmax<D, FMT, 2, false, D / 2>(r, mask, sh.scale[slot], s_col, p_col, chunk0, read, ahead, [&](float x) { return fmaxf(x, meet(x)); }, i > 0, o_col + part * (D / 2));
+                } else {
+                    if (copies == 1) chunk_softmax<D, FMT, 4, true, D>(r, mask, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
+                    else if (copies == 2) chunk_softmax<D, FMT, 2, false, D>(r, mask, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
+                    else chunk_softmax<D, FMT, 1, false, D>(r, mask, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
+                    uint32_t zero[16] = {};                            // the weights of the other copies' keys
 #pragma unroll 1
-                        for (int c = 0; c < D; c += 32) {
-                            uint32_t x[32];
-                            tmem_load(o_col + c, x);
-                            tmem_loaded();
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * r);
-                            tmem_store(o_col + c, x);
-                        }
-                    }
+                    for (int c = 0; c < 4; ++c)
+                        if (c < chunk0 || c >= chunk0 + chunks) tmem_store(p_col + 16 * c, zero);
                 }
-                const f32x2 f2 = pack_f32x2(f, f), m2 = pack_f32x2(7.0f - m, 7.0f - m);
-                f32x2 l2 = pack_f32x2(0.0f, 0.0f);
-#pragma unroll(SPLIT ? 1 : 4)
-                for (int c = chunk0; c < chunk0 + chunks; ++c) {
-                    f32x2 y[16];
-                    scores(c, y);
-                    uint32_t w[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float u0, u1;
-                        unpack_f32x2(ffma2(y[e], f2, m2), &u0, &u1);
-                        u0 = ex2_approx(u0);
-                        u1 = ex2_approx(u1);
-                        l2 = add2(l2, pack_f32x2(u0, u1));
-                        w[e] = half2_of(u0, u1);
-                    }
-                    tmem_store(s_col + 16 * c, w);
-                }
-                if constexpr (SPLIT) {
-                    if (copies > 1) {
-                        uint32_t zero[16] = {};
-#pragma unroll 1
-                        for (int c = 0; c < 4; ++c)
-                            if (c < chunk0 || c >= chunk0 + chunks) tmem_store(s_col + 16 * c, zero);
-                    }
-                }
-                float l0, l1;
-                unpack_f32x2(l2, &l0, &l1);
-                l += l0 + l1;
+                ++tiles_done;
                 tmem_stored();
                 tcgen05_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_addr(&sh.p_full[stream]));
             }
             keys_done += n;
-            if (n > 0) {
-                wait(sh.o_full[stream], pieces_done & 1);
-                ++pieces_done;
+            if (mine > 0) {
+                wait(sh.o_full[stream], (tiles_done & 1) ^ 1);
                 tcgen05_after_sync();
             }
-            // ---- the piece's sums
-            const bool whole = p.whole();
-            float* slot = nullptr;
-            if (!whole) {
-                slot = reinterpret_cast<float*>(a.workspace + kChunkPlanBytes) + (size_t)(2 * blockIdx.x + (p.begin == 0 ? 1 : 0)) * chunk_slot_floats(D, SPLIT);
-                if (p.begin == 0) {
-                    cut_here = true;
-                    if (tid == 0) {
-                        // the block that has the unit's last tile: the last one that starts at or before it
-                        const long long x = x1 + p.u.count - p.end - 1;
-                        cuts[blockIdx.x] = ChunkCut{p.head, p.flat, (int)(((x + 1) * blocks - 1) / total), 1};
-                    }
-                }
-            }
+            const float m = r.m;
+            float l = r.l;
             if constexpr (!SPLIT) {
-                const float inv = wait.lost ? __int_as_float(0x7fc00000) : l > 0.0f ? __fdiv_rn(1.0f, l) : 0.0f;
-                if (slot && there) {
+                if (wait.lost) l = __int_as_float(0x7fc00000);
+                l += meet(l);
+            }
+            // ---- the piece's sums
+            float* slot = nullptr;
+            if (p->place) slot = reinterpret_cast<float*>(a.workspace + kChunkPlanBytes) + (size_t)(2 * blockIdx.x + p->place - 1) * chunk_slot_floats(D, SPLIT);
+            const bool there = row < p->rows;
+            if constexpr (!SPLIT) {
+                const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == 0.0f ? 0.0f : l;
+                if (slot && there && part == 0) {
                     slot[kPerTile * D + row] = m;
-                    slot[kPerTile * (D + 1) + row] = wait.lost ? inv : l;
+                    slot[kPerTile * (D + 1) + row] = l;
                 }
-                uint16_t* out = there ? static_cast<uint16_t*>(a.O) + chunk_row(a, u, p.head, row) * D : nullptr;
+                uint16_t* out = there ? static_cast<uint16_t*>(a.O) + p->row(a, row) * D : nullptr;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
+                for (int c = part * (D / 2); c < (part + 1) * (D / 2); c += 32) {
                     uint32_t x[32] = {};
                     if (mine > 0) {
                         tmem_load(o_col + c, x);
@@ -662,14 +831,14 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                     float item_most = -1e30f;
                     for (int k = item_row; k < 256; k += rows_own) item_most = fmaxf(item_most, sh.m[k]);
                     for (int k = item_row; k < 256; k += rows_own) all += sh.l[k] * ex2_approx(sh.m[k] - item_most);
-                    if (slot && channel0 == 0 && item_row < u.rows) {
+                    if (slot && channel0 == 0 && item_row < p->rows) {
                         slot[kPerTile * D + item_row] = item_most;
                         slot[kPerTile * (D + 1) + item_row] = all;
                     }
                 }
                 const float inv = all > 0.0f ? __fdiv_rn(1.0f, all) : all == 0.0f ? 0.0f : all;
-                const bool item_there = item_row < u.rows;
-                uint16_t* out = item_there ? static_cast<uint16_t*>(a.O) + chunk_row(a, u, p.head, item_row) * D : nullptr;
+                const bool item_there = item_row < p->rows;
+                uint16_t* out = item_there ? static_cast<uint16_t*>(a.O) + p->row(a, item_row) * D : nullptr;
 #pragma unroll 1
                 for (int c = 0; c < D; c += 16) {
                     uint32_t x[16] = {};
@@ -698,82 +867,102 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                 }
             }
             tcgen05_before_sync();
+            reader.leave();
         }
-        if (tid == 0 && !cut_here) cuts[blockIdx.x].there = 0;
-    } else if (warp < 12) {
+    } else if (warp < kProducts) {
         // ---- operands: a key a thread
-        const int part = warp - 8, row = part * 32 + lane;             // half page of the tile
+        registers_down<kRegisters.operand>();
+        const int part = warp & 3, row = part * 32 + lane;             // half page of the tile
+        const bool keys = !SPLIT || warp < kOperands + 4, values = !SPLIT || warp >= kOperands + 4;
         uint32_t keys_done = 0;
-        while (walk.next(a, sh.lens, per_tile, p))
-            for (int j = p.begin; j < p.end; ++j, ++keys_done) {
+        while (const ChunkPiece* p = reader.next()) {
+            for (int j = 0; j < p->n; ++j, ++keys_done) {
                 const int stage = keys_done % S::kStages, buffer = keys_done % NB, slot = keys_done & 3;
                 const uint32_t turn = keys_done / NB & 1;
-                const int key = p.u.tile(j) * kChunkTile + row;
+                const int t0 = p->tile(j) * kChunkTile, key = t0 + row;
                 wait(sh.raw_full[stage], keys_done / S::kStages & 1);
                 const uint8_t* half = raw + stage * S::kRaw + part * S::kHalf;
-                const uint32_t pages = sh.raw_info[stage];
+                const int pages = (int)sh.raw_info[stage];
                 // what no row sees is zero: it may hold anything, and a weight of zero times that is not zero
-                const bool seen = (pages >> (part >> 1) & 1u) && key < p.u.hi && (key >= p.u.lo || key < a.sinks);
-                wait(sh.k_empty[buffer], turn ^ 1);
-                const uint32_t k_operand = k_at + buffer * S::kOperand, v_operand = v_at + buffer * S::kOperand;
-                if (seen) chunk_key<D, FMT>(half, lane, k_operand, row);
-                else
-#pragma unroll
-                    for (int c = 0; c < D / 8; ++c) put_operand(k_operand, row, c, 0u, 0u, 0u, 0u);
-                if constexpr (S::kScaled) sh.scale[slot][row] = seen ? half_bits_to_float(*reinterpret_cast<const uint16_t*>(half + S::kMeta + lane * 4)) : 0.0f;
-                if (row == 0) sh.pages[slot] = pages;
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_addr(&sh.k_full[buffer]));
-                wait(sh.v_empty[buffer], turn ^ 1);
-                chunk_value<D, FMT>(half, lane, v_operand, row);
-                if (!seen)
-#pragma unroll
-                    for (int c = 0; c < D / 8; ++c) put_operand(v_operand, row, c, 0u, 0u, 0u, 0u);
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(smem_addr(&sh.v_full[buffer]));
-                    mbar_arrive(smem_addr(&sh.raw_empty[stage]));
+                const bool seen = (pages >> (part >> 1) & 1) && key < p->hi && (key >= p->lo || key < a.sinks);
+                if (keys) {
+                    const uint32_t operand = k_at + buffer * S::kOperand;
+                    ChunkCodes<D, FMT, true> codes(half, lane);
+                    wait(sh.k_empty[buffer], turn ^ 1);
+                    codes.put(half, lane, operand, row, seen);
+                    if constexpr (S::kScaled) {
+                        // (of a key of zeros, whose scores are zeros, and of one that nobody sees: any number but zero, which -inf is multiplied by)
+                        const uint32_t bits = seen ? *reinterpret_cast<const uint16_t*>(half + S::kMeta + lane * 4) : 0u;
+                        sh.scale[slot][row] = bits ? half_bits_to_float(bits) : 1.0f;
+                    }
+                    if (row == 0) {
+                        auto whole = [&](int stream) { return pages == 3 && p->first[stream] - t0 >= kChunkTile - 1 && (a.window == 0 || p->last[stream] - t0 < a.window || t0 + kChunkTile <= a.sinks); };
+                        sh.info[slot] = make_int2(t0, pages | (whole(0) ? 4 : 0) | (whole(1) ? 8 : 0));
+                    }
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_addr(&sh.k_full[buffer]));
                 }
+                if (values) {
+                    const uint32_t operand = v_at + buffer * S::kOperand;
+                    ChunkCodes<D, FMT, false> codes(half, lane);
+                    wait(sh.v_empty[buffer], turn ^ 1);
+                    codes.put(half, lane, operand, row, seen);
+                    fence_proxy_async();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_addr(&sh.v_full[buffer]));
+                }
+                if (lane == 0) mbar_arrive(smem_addr(&sh.raw_empty[stage]));
             }
-    } else if (warp == 12) {
+            reader.leave();
+        }
+    } else if (warp == kProducts) {
         // ---- products
-        if (lane == 0) {
+        registers_down<kRegisters.other>();
+        {
+            const bool elected = elect_lane();
             constexpr uint32_t kScores = mma_form(kChunkTile, S::kBf16, false), kValues = mma_form(D, false, true);
-            uint32_t keys_done = 0, pieces = 0, weights[2] = {};
+            uint32_t keys_done = 0, pieces = 0, done[2] = {}, read[2] = {};          // of the streams: tiles whose values are issued, whose scores have been read
             auto scores = [&](int stream, uint32_t key_tile) {
                 const uint32_t q = q_at + stream * S::kOperand, k = k_at + key_tile % NB * S::kOperand;
-                if (wait.lost) return;
+                const bool go = elected && !wait.lost;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
                     const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
-                    tcgen05_mma_ss(tmem + stream * 128, smem_operand(q + off), smem_operand(k + off), kScores, i > 0);
+                    tcgen05_mma_ss(stream * 128, smem_operand(q + off), smem_operand(k + off), kScores, i > 0, go);
                 }
-                mbar_arrive(smem_addr(&sh.s_full[stream]));
-                tcgen05_commit(smem_addr(&sh.s_full[stream]));
+                if (go) mbar_arrive(smem_addr(&sh.s_full[stream]));
+                tcgen05_commit(smem_addr(&sh.s_full[stream]), go);
+            };
+            auto commit = [&](const unsigned long long& bar) {
+                tcgen05_commit(smem_addr(&bar), elected && !wait.lost);
             };
             auto values = [&](int stream, uint32_t key_tile, bool first) {
                 const uint32_t v = v_at + key_tile % NB * S::kOperand;
-                wait.one(sh.p_full[stream], weights[stream]++ & 1);
+                wait(sh.p_full[stream], done[stream]++ & 1);
                 tcgen05_after_sync();
-                if (wait.lost) return;
+                const bool go = elected && !wait.lost;
 #pragma unroll
                 for (int i = 0; i < kChunkTile / 16; ++i)
-                    tcgen05_mma_ts(tmem + 256 + stream * D, tmem + stream * 128 + 8 * i, smem_operand(v + i * 2048, 16384), kValues, !first || i > 0);
-            };
-            auto commit = [&](const unsigned long long& bar) {
-                if (!wait.lost) tcgen05_commit(smem_addr(&bar));
+                    tcgen05_mma_ts(S::sums(stream), S::weights(stream) + 8 * i, smem_operand(v + i * 2048, 16384), kValues, !first || i > 0, go);
+                commit(sh.o_full[stream]);
             };
             auto key_ready = [&](uint32_t key_tile) {
-                wait.one(sh.k_full[key_tile % NB], key_tile / NB & 1);
+                wait(sh.k_full[key_tile % NB], key_tile / NB & 1);
                 tcgen05_after_sync();
             };
-            while (walk.next(a, sh.lens, per_tile, p)) {
-                const int n = p.end - p.begin;
+            auto scores_read = [&](int stream) {                       // (with the weights in their place that is known by the weights' being there)
+                if constexpr (S::kApart) {
+                    wait(sh.s_free[stream], read[stream]++ & 1);
+                    tcgen05_after_sync();
+                }
+            };
+            while (const ChunkPiece* p = reader.next()) {
+                const int n = p->n;
+                reader.leave();
                 if (n == 0) continue;
-                wait.one(sh.q_full[0], pieces & 1);
-                wait.one(sh.q_full[1], pieces & 1);
+                wait(sh.q_full[0], pieces & 1);
+                wait(sh.q_full[1], pieces & 1);
                 ++pieces;
                 tcgen05_after_sync();
                 const uint32_t g = keys_done;
@@ -789,50 +978,69 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                     }
                 for (int j = 0; j < n; ++j) {
                     const uint32_t now = g + j;
-                    wait.one(sh.v_full[now % NB], now / NB & 1);
-                    tcgen05_after_sync();
-                    if constexpr (!SPLIT) {
+                    if constexpr (SPLIT) {
+                        const int stream = j & 1;
+                        wait(sh.v_full[now % NB], now / NB & 1);
+                        tcgen05_after_sync();
+                        values(stream, now, j < 2);
+                        commit(sh.v_empty[now % NB]);
+                        scores_read(stream);
+                        if (j + 2 < n) {
+                            key_ready(now + 2);
+                            scores(stream, now + 2);
+                            commit(sh.k_empty[(now + 2) % NB]);
+                        }
+                    } else if constexpr (S::kApart) {
+                        scores_read(0);
+                        if (j + 1 < n) {
+                            key_ready(now + 1);
+                            scores(0, now + 1);
+                        }
+                        scores_read(1);
+                        if (j + 1 < n) {
+                            scores(1, now + 1);
+                            commit(sh.k_empty[(now + 1) % NB]);
+                        }
+                        wait(sh.v_full[now % NB], now / NB & 1);
+                        tcgen05_after_sync();
+                        values(0, now, j == 0);
+                        values(1, now, j == 0);
+                        commit(sh.v_empty[now % NB]);
+                    } else {
+                        wait(sh.v_full[now % NB], now / NB & 1);
+                        tcgen05_after_sync();
                         values(0, now, j == 0);
                         if (j + 1 < n) {
                             key_ready(now + 1);
                             scores(0, now + 1);
-                        } else commit(sh.o_full[0]);
+                        }
                         values(1, now, j == 0);
                         commit(sh.v_empty[now % NB]);
                         if (j + 1 < n) {
                             scores(1, now + 1);
                             commit(sh.k_empty[(now + 1) % NB]);
-                        } else commit(sh.o_full[1]);
-                    } else {
-                        const int stream = j & 1;
-                        values(stream, now, j < 2);
-                        commit(sh.v_empty[now % NB]);
-                        if (j + 2 < n) {
-                            key_ready(now + 2);
-                            scores(stream, now + 2);
-                            commit(sh.k_empty[(now + 2) % NB]);
-                        } else commit(sh.o_full[stream]);
+                        }
                     }
                 }
-                if (SPLIT && n == 1) commit(sh.o_full[1]);
                 keys_done += n;
             }
             commit(sh.done);
-            wait.one(sh.done, 0);
+            wait(sh.done, 0);
         }
-        __syncwarp();
-    } else {
+    } else if (warp == kProducts + 1) {
         // ---- loader
+        registers_down<kRegisters.other>();
         fence_proxy_async_global();                                    // (the records were written by ordinary stores)
         uint32_t keys_done = 0;
-        while (walk.next(a, sh.lens, per_tile, p)) {
-            const int b = a.s.b[p.u.seq];
-            for (int j0 = p.begin; j0 < p.end; j0 += 16) {             // the pages of 16 tiles, one a lane
-                const int j = j0 + lane / 2, page = p.u.tile(min(j, p.end - 1)) * 2 + lane % 2;
+        while (const ChunkPiece* p = reader.next()) {
+            const int n = p->n, hi = p->hi, head = p->head;
+            const int32_t* table = a.c.page_table + (size_t)p->b * a.c.max_pages;
+            for (int j0 = 0; j0 < n; j0 += 16) {                       // the pages of 16 tiles, one a lane
+                const int j = j0 + lane / 2, page = p->tile(min(j, n - 1)) * 2 + lane % 2;
                 int at = -1;                                           // (none)
-                if (j < p.end && page < a.c.max_pages && page * kPageTokens < p.u.hi) at = a.c.page_table[(size_t)b * a.c.max_pages + page];
+                if (j < n && page < a.c.max_pages && page * kPageTokens < hi) at = table[page];
                 if (at >= a.c.n_pages) at = -1;
-                for (int i = 0; i < 16 && j0 + i < p.end; ++i, ++keys_done) {
+                for (int i = 0; i < 16 && j0 + i < n; ++i, ++keys_done) {
                     const int at0 = __shfl_sync(0xffffffffu, at, 2 * i), at1 = __shfl_sync(0xffffffffu, at, 2 * i + 1);
                     const int stage = keys_done % S::kStages;
                     wait(sh.raw_empty[stage], keys_done / S::kStages & 1 ^ 1);
@@ -840,12 +1048,13 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
                         const uint32_t bar = smem_addr(&sh.raw_full[stage]), to = smem_addr(raw + stage * S::kRaw);
                         sh.raw_info[stage] = (at0 >= 0 ? 1u : 0u) | (at1 >= 0 ? 2u : 0u);
                         mbar_arrive_expect_tx(bar, ((at0 >= 0) + (at1 >= 0)) * 2u * S::kHalf);
-                        if (at0 >= 0) bulk_g2s(to, a.c.pages + ((size_t)at0 * a.c.Hkv + p.head) * (2 * S::kHalf), 2 * S::kHalf, bar);
-                        if (at1 >= 0) bulk_g2s(to + 2 * S::kHalf, a.c.pages + ((size_t)at1 * a.c.Hkv + p.head) * (2 * S::kHalf), 2 * S::kHalf, bar);
+                        if (at0 >= 0) bulk_g2s(to, a.c.pages + ((size_t)at0 * a.c.Hkv + head) * (2 * S::kHalf), 2 * S::kHalf, bar);
+                        if (at1 >= 0) bulk_g2s(to + 2 * S::kHalf, a.c.pages + ((size_t)at1 * a.c.Hkv + head) * (2 * S::kHalf), 2 * S::kHalf, bar);
                     }
                     __syncwarp();
                 }
             }
+            reader.leave();
         }
         // copies in flight land before the block ends, also where the operands' warps have given up
         const uint32_t last = keys_done < (uint32_t)S::kStages ? keys_done : (uint32_t)S::kStages;
@@ -853,11 +1062,73 @@ __global__ void __launch_bounds__(kChunkThreads, 1) chunk_kernel(const __grid_co
             const uint32_t k = keys_done - 1 - i;
             wait(sh.raw_full[k % S::kStages], k / S::kStages & 1);
         }
+    } else if (warp == kProducts + 2) {
+        // ---- the block's stretch, piece by piece
+        registers_down<kRegisters.other>();
+        int head = sh.start_head, flat = sh.start_flat, skip = sh.start_skip;      // the unit, and how far into it (its fixed cost included) the stretch starts
+        long long left = x1 - x0;
+        uint32_t made = 0;
+        bool cut = false;
+        auto place = [&]() -> ChunkPiece& {
+            wait(sh.piece_empty[made % kChunkPieces], made / kChunkPieces & 1 ^ 1);
+            return sh.pieces[made % kChunkPieces];
+        };
+        auto ready = [&] {
+            __syncwarp();
+            if (lane == 0 && !wait.lost) mbar_arrive(smem_addr(&sh.piece_full[made % kChunkPieces]));
+            ++made;
+        };
+        while (left > 0) {
+            const ChunkUnit u = chunk_unit(a, sh.lens, flat, per_tile);
+            const int cost = kChunkUnitCost + u.count, to = left < cost - skip ? skip + (int)left : cost;
+            const int begin = max(skip - kChunkUnitCost, 0), end = max(to - kChunkUnitCost, 0);
+            if (end > begin || (u.count == 0 && skip == 0)) {
+                ChunkPiece& p = place();
+                if (lane == 0) {
+                    const int token = u.row0 / a.G;
+                    p.n = end - begin;
+                    p.head = head;
+                    p.b = a.s.b[u.seq];
+                    p.rows = u.rows;
+                    p.token_row = u.row0 - token * a.G;
+                    p.token = u.first;
+                    p.q_token = a.s.row0[u.seq] + token;
+                    p.lo = u.lo;
+                    p.hi = u.hi;
+                    p.sink_tiles = u.sink_tiles;
+                    p.window_tile = u.window_tile;
+                    p.begin = begin;
+                    p.place = begin == 0 && end == u.count ? 0 : begin == 0 ? 2 : 1;
+                    for (int i = 0; i < 2; ++i) {
+                        p.first[i] = p.position(a, SPLIT ? 0 : min(i * 128, u.rows - 1));
+                        p.last[i] = p.position(a, SPLIT ? u.rows - 1 : min(i * 128 + 127, u.rows - 1));
+                    }
+                    if (p.place == 2) {
+                        // the block that has the unit's last tile: the last one whose stretch starts at or before it
+                        const long long x = x1 + u.count - end - 1;
+                        cuts[blockIdx.x] = ChunkCut{head, flat, (int)(((x + 1) * blocks - 1) / total), 1};
+                        cut = true;
+                    }
+                }
+                ready();
+            }
+            left -= to - skip;
+            skip = 0;
+            if (++flat == n_flat) flat = 0, ++head;
+        }
+        ChunkPiece& p = place();
+        if (lane == 0) {
+            p.n = -1;
+            if (!cut) cuts[blockIdx.x].there = 0;
+        }
+        ready();
+    } else {
+        registers_down<kRegisters.other>();
     }
     tcgen05_before_sync();
     __syncthreads();
     tcgen05_after_sync();
-    if (warp == 12) tmem_free(tmem);
+    if (warp == kProducts) tmem_free();
 }
 
 // Units that the deal has cut: block x takes the one that starts in block x of the kernel above.
@@ -900,7 +1171,7 @@ template <int D, int FMT, bool SPLIT>
 cudaError_t launch_chunk(const ChunkArgs& a, int blocks, cudaStream_t s) {
     static OncePerDevice once;
     if (!allow_shared(chunk_kernel<D, FMT, SPLIT>, ChunkShape<D, FMT>::kBytes, once)) return cudaGetLastError();
-    const cudaError_t e = launch_pdl(chunk_kernel<D, FMT, SPLIT>, dim3(blocks), dim3(kChunkThreads), (size_t)ChunkShape<D, FMT>::kBytes, s, a);
+    const cudaError_t e = launch_pdl(chunk_kernel<D, FMT, SPLIT>, dim3(blocks), dim3(chunk_threads(SPLIT)), (size_t)ChunkShape<D, FMT>::kBytes, s, a);
     if (e != cudaSuccess) return e;
     return launch_pdl(chunk_merge_kernel<D, SPLIT>, dim3(blocks, SPLIT ? 4 : 16), dim3(256), 0, s, a);
 }

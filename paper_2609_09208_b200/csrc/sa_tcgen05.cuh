@@ -11,18 +11,26 @@ namespace sa {
 
 constexpr uint32_t kTmemColumns = 512;
 
-// By one warp; `at`: shared address of the word that receives the address of the first column.
+// By one warp; `at`: shared address of the word that receives the address of the first column: 0, as all columns are asked for.
 SA_D void tmem_alloc(uint32_t at) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(at), "r"(kTmemColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
 }
-SA_D void tmem_free(uint32_t tmem) { asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns) : "memory"); }
+SA_D void tmem_free() { asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(0u), "r"(kTmemColumns) : "memory"); }
+
+// One lane of the warp; the others' instructions below are issued with `go` false.  So the warp stays together, and operands that are the same for all lanes stay
+// in its uniform registers, from where these instructions take them (in a branch of one lane every operand was moved there, 70 cycles a product).
+SA_D bool elect_lane() {
+    uint32_t x;
+    asm volatile("{.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;}" : "=r"(x));
+    return x != 0;
+}
 
 SA_D void tcgen05_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 SA_D void tcgen05_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // One arrival at the mbarrier once all products that this thread has issued are done.
-SA_D void tcgen05_commit(uint32_t mbar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(mbar) : "memory");
+SA_D void tcgen05_commit(uint32_t mbar, bool go) {
+    asm volatile("{.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];}" ::"r"(mbar), "r"((uint32_t)go) : "memory");
 }
 
 // Shared-memory operand at `at` (see above).  Blocks of 8 rows are 1024 bytes apart; across: blocks of 64 numbers across the contraction.
@@ -34,12 +42,16 @@ SA_HD constexpr uint32_t mma_form(int n, bool bf16, bool b_across) {
     return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (b_across ? 1u : 0u) << 16 | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
 }
 // 16 numbers of the contraction; add: to the sums that are there.
-SA_D void tcgen05_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t form, bool add) {
-    asm volatile("{.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d), "l"(a), "l"(b), "r"(form), "r"((uint32_t)add) : "memory");
+SA_D void tcgen05_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t form, bool add, bool go) {
+    asm volatile("{.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d), "l"(a), "l"(b), "r"(form),
+                 "r"((uint32_t)add), "r"((uint32_t)go)
+                 : "memory");
 }
 // ... with the first operand in tensor memory, two numbers a column.
-SA_D void tcgen05_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t form, bool add) {
-    asm volatile("{.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;}" ::"r"(d), "r"(a), "l"(b), "r"(form), "r"((uint32_t)add) : "memory");
+SA_D void tcgen05_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t form, bool add, bool go) {
+    asm volatile("{.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;}" ::"r"(d), "r"(a), "l"(b), "r"(form),
+                 "r"((uint32_t)add), "r"((uint32_t)go)
+                 : "memory");
 }
 
 // 32 (16) columns of this warp's 32 rows, a row a thread.  The registers are there after tmem_loaded().
