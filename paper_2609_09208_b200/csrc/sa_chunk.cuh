@@ -42,7 +42,7 @@ SA_HD constexpr int chunk_threads(bool split) { return 32 * (chunk_softmax_warps
 struct ChunkRegisters {
     int launch, softmax, operand, other;
 };
-SA_HD constexpr ChunkRegisters chunk_registers(bool split) { return split ? ChunkRegisters{96, 136, 80, 48} : ChunkRegisters{80, 88, 80, 48}; }
+SA_HD constexpr ChunkRegisters chunk_registers(bool split) { return split ? ChunkRegisters{96, 136, 80, 48} : ChunkRegisters{80, 96, 56, 40}; }
 SA_HD constexpr bool chunk_registers_fit(bool split) {
     const ChunkRegisters r = chunk_registers(split);
     return 32 * (chunk_softmax_warps(split) * r.softmax + chunk_operand_warps(split) * r.operand + 4 * r.other) <= chunk_threads(split) * r.launch && chunk_threads(split) * r.launch <= 65536;
@@ -141,7 +141,7 @@ struct ChunkShape {
     static constexpr int kRaw = 4 * kHalf;                            // records of a tile
     static constexpr int kOperand = D / 64 * 16384;                   // 128 rows
     static constexpr int kBuffers = D == 64 ? 2 : 1;                  // of operands
-    static constexpr int kFixed = (2 + 2 * kBuffers) * kOperand + 10240;
+    static constexpr int kFixed = (2 + 2 * kBuffers) * kOperand + 12288;
     static constexpr int kFit = (227 * 1024 - 1024 - kFixed) / kRaw;
     static constexpr int kStages = kFit > 4 ? 4 : kFit;
     static constexpr int kBytes = 1024 + kFixed + kStages * kRaw;     // (1024: to align)
@@ -159,7 +159,7 @@ struct ChunkShape {
 struct ChunkShared {                      // behind the rings
     float scale[4][kChunkTile];           // of the keys of four tiles
     float m[256], l[256];                 // SPLIT: of all threads' rows
-    float meet[2][512];                   // else: what the two halves of a row tell each other
+    float meet[3][512];                   // else: what the two halves of a row tell each other: largest scores of a tile and of the next, and what a piece begins and ends with
     int2 info[4];                         // of four tiles: first key; bits 0, 1: pages there are, 2, 3: streams whose rows see all of the tile
     ChunkPiece pieces[kChunkPieces];
     unsigned long long piece_full[kChunkPieces], piece_empty[kChunkPieces];
@@ -170,7 +170,7 @@ struct ChunkShared {                      // behind the rings
     int start_head, start_flat, start_skip;
     long long sums[24];
 };
-static_assert(sizeof(ChunkShared) <= 10240, "room behind the rings");
+static_assert(sizeof(ChunkShared) <= 12288, "room behind the rings");
 
 // A wait that ends: where the limit is reached, nothing is waited for any more and the outputs become NaN.  A poll may sleep up to 2 us, so that waiting warps leave
 // their issue slots to the others (without it a tenth of all instructions were polls), and the limit is a third of a second.
@@ -181,9 +181,14 @@ struct ChunkWait {
         asm volatile("{.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
         return ok != 0;
     }
+    SA_D static bool over(uint32_t bar, uint32_t parity) {                      // (the phase is over already: a look that cannot sleep is the faster one)
+        uint32_t ok;
+        asm volatile("{.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        return ok != 0;
+    }
     SA_D void operator()(const unsigned long long& bar, uint32_t parity) {      // by a whole warp
         const uint32_t at = smem_addr(&bar);
-        if (!lost && !poll(at, parity)) {
+        if (!over(at, parity) && !lost) {
             lost = true;
 #pragma unroll 1
             for (uint32_t i = 0; i < kWaitLimit && lost; ++i) lost = !poll(at, parity);
@@ -456,11 +461,9 @@ SA_D void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" 
 struct ChunkRow {
     float m, l, factor;
 };
-// Which columns of a tile (whose first key is t0) a row sees.  whole: all.
+// Which columns of a tile (whose first key is t0) a row sees.
 struct ChunkMask {
-    int t0, pages;
-    bool whole;
-    int position, window, sinks;
+    int t0, pages, position, window, sinks;
 };
 SA_D float max3(float a, float b, float c) {
     float d;
@@ -483,12 +486,11 @@ SA_D void chunk_scores(const uint32_t (&x)[32], f32x2 (&y)[16], const float* sca
 }
 // Scores of hidden keys become -inf where they lie, in tensor memory: few tiles need it, and in registers the others would pay for the meeting of the branches
 // with a move of every score.
-template <int C>
-SA_D void chunk_hide(const ChunkMask& mask, uint32_t s_col, int chunk0) {
+SA_D void chunk_hide(const ChunkMask& mask, uint32_t s_col, int chunk0, int chunks) {
     const int hi = mask.position - mask.t0, sink = mask.sinks - mask.t0;
     const int lo = mask.window && mask.position >= 0 ? (int)max((long long)hi - mask.window + 1, -0x40000000ll) : -0x40000000;
 #pragma unroll 1
-    for (int c = chunk0; c < chunk0 + C; ++c) {
+    for (int c = chunk0; c < chunk0 + chunks; ++c) {
         uint32_t x[32];
         tmem_load(s_col + 32 * c, x);
         tmem_loaded();
@@ -552,12 +554,11 @@ SA_D void chunk_scores_read(bool apart, uint32_t free_scores) {
 // ahead(): waits until weights and sums may be written; all(x): the largest x of the row's threads; sums: there are some, OUT channels of them from o_col for this thread to
 // rescale.  TWICE: the scores are read once for the largest and again for the weights, by a thread without the registers for all of them.
 template <int D, int FMT, int C, bool TWICE, int OUT, typename Ahead, typename All>
-SA_D void chunk_softmax(ChunkRow& row, const ChunkMask& mask, const float* scale, uint32_t s_col, uint32_t p_col, int chunk0, uint32_t free_scores, Ahead ahead, All all, bool sums, uint32_t o_col) {
+SA_D void chunk_softmax(ChunkRow& row, const float* scale, uint32_t s_col, uint32_t p_col, int chunk0, uint32_t free_scores, Ahead ahead, All all, bool sums, uint32_t o_col) {
     using S = ChunkShape<D, FMT>;
     float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     f32x2 l[2] = {pack_f32x2(0.0f, 0.0f), pack_f32x2(0.0f, 0.0f)};
     bool grown;
-    if (!mask.whole) chunk_hide<C>(mask, s_col, chunk0);
     if constexpr (TWICE) {
         uint32_t x[32], w[16];
         f32x2 y[16];
@@ -713,17 +714,15 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         const int chunks = 4 / (copies * kHalves), chunk0 = SPLIT ? own / rows_own * chunks : 2 * part;      // columns of 32 that this thread has
         registers_up<kRegisters.softmax>();
         uint32_t tiles_done = 0, keys_done = 0;
-        // The halves of a row meet at a barrier of their two warps, with a number of each (in turn in two places: one barrier a meeting will do).
-        int meetings = 0;
-        auto meet = [&](float x) {
-            float* at = sh.meet[meetings++ & 1];
+        // The halves of a row meet at a barrier of their two warps, with a number of each (one barrier a meeting will do, as the next one has another place).
+        auto meet = [&](float x, uint32_t place) {
+            float* at = sh.meet[place];
             at[tid] = x;
             chunk_sync(2 + 4 * stream + quarter, 64);
             return at[tid ^ 128];
         };
         while (const ChunkPiece* p = reader.next()) {
             const int n = p->n, mine = SPLIT ? (n + 1 - stream) / 2 : n;                  // tiles of this stream
-            const int position = row < p->rows ? p->position(a, row) : -1;
             ChunkRow r{-1e30f, 0.0f, a.factor};
             if (n > 0) {
                 const int first_row = SPLIT ? quarter * 32 : stream * 128 + quarter * 32;
@@ -734,7 +733,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 // (a half has the factors of its 16 rows in the lanes that the other half's 16 leave)
                 r.factor = chunk_queries<D, FMT, kHalves>(a, q_operand, lane, quarter * 32, part, query);
                 if constexpr (!SPLIT) {
-                    const float others = meet(r.factor);
+                    const float others = meet(r.factor, 2);
                     if (lane / 16 != part) r.factor = others;
                 }
                 fence_proxy_async();
@@ -743,11 +742,14 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[stream]));
             }
             for (int i = 0; i < mine; ++i) {
-                const int slot = (keys_done + (SPLIT ? 2 * i + stream : i)) & 3;
+                const int slot = (SPLIT ? keys_done + 2 * i + stream : tiles_done) & 3;
                 wait(sh.s_full[stream], tiles_done & 1);
                 tcgen05_after_sync();
                 const int2 info = sh.info[slot];
-                const ChunkMask mask{info.x, info.y, (info.y >> (2 + stream) & 1) != 0, position, a.window, a.sinks};
+                if (!(info.y >> (2 + stream) & 1)) {
+                    const ChunkMask mask{info.x, info.y, row < p->rows ? p->position(a, row) : -1, a.window, a.sinks};
+                    chunk_hide(mask, s_col, chunk0, chunks);
+                }
                 auto ahead = [&] {
                     // the weights' place and the sums are free once the products of the tile before are done
                     wait(sh.o_full[stream], (tiles_done & 1) ^ 1);
@@ -756,11 +758,11 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 auto same = [](float x) { return x; };
                 const uint32_t read = smem_addr(&sh.s_free[stream]);
                 if constexpr (!SPLIT) {
-                    chunk_softmax<D, FMT, 2, false, D / 2>(r, mask, sh.scale[slot], s_col, p_col, chunk0, read, ahead, [&](float x) { return fmaxf(x, meet(x)); }, i > 0, o_col + part * (D / 2));
+                    chunk_softmax<D, FMT, 2, false, D / 2>(r, sh.scale[slot], s_col, p_col, chunk0, read, ahead, [&](float x) { return fmaxf(x, meet(x, tiles_done & 1)); }, i > 0, o_col + part * (D / 2));
                 } else {
-                    if (copies == 1) chunk_softmax<D, FMT, 4, true, D>(r, mask, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
-                    else if (copies == 2) chunk_softmax<D, FMT, 2, false, D>(r, mask, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
-                    else chunk_softmax<D, FMT, 1, false, D>(r, mask, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
+                    if (copies == 1) chunk_softmax<D, FMT, 4, true, D>(r, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
+                    else if (copies == 2) chunk_softmax<D, FMT, 2, false, D>(r, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
+                    else chunk_softmax<D, FMT, 1, false, D>(r, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
                     uint32_t zero[16] = {};                            // the weights of the other copies' keys
 #pragma unroll 1
                     for (int c = 0; c < 4; ++c)
@@ -781,7 +783,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
             float l = r.l;
             if constexpr (!SPLIT) {
                 if (wait.lost) l = __int_as_float(0x7fc00000);
-                l += meet(l);
+                l += meet(l, 2);
             }
             // ---- the piece's sums
             float* slot = nullptr;
@@ -921,15 +923,16 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         registers_down<kRegisters.other>();
         {
             const bool elected = elect_lane();
+            const uint32_t q_first = smem_operand(q_at), k_first = smem_operand(k_at), v_first = smem_operand(v_at, 16384);
             constexpr uint32_t kScores = mma_form(kChunkTile, S::kBf16, false), kValues = mma_form(D, false, true);
             uint32_t keys_done = 0, pieces = 0, done[2] = {}, read[2] = {};          // of the streams: tiles whose values are issued, whose scores have been read
             auto scores = [&](int stream, uint32_t key_tile) {
-                const uint32_t q = q_at + stream * S::kOperand, k = k_at + key_tile % NB * S::kOperand;
+                const uint32_t q = q_first + stream * (S::kOperand >> 4), k = k_first + key_tile % NB * (S::kOperand >> 4);
                 const bool go = elected && !wait.lost;
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
-                    const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
-                    tcgen05_mma_ss(stream * 128, smem_operand(q + off), smem_operand(k + off), kScores, i > 0, go);
+                    const uint32_t off = ((i >> 2) * 16384 + (i & 3) * 32) >> 4;
+                    tcgen05_mma_ss(stream * 128, q + off, k + off, kScores, i > 0, go);
                 }
                 if (go) mbar_arrive(smem_addr(&sh.s_full[stream]));
                 tcgen05_commit(smem_addr(&sh.s_full[stream]), go);
@@ -938,13 +941,13 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 tcgen05_commit(smem_addr(&bar), elected && !wait.lost);
             };
             auto values = [&](int stream, uint32_t key_tile, bool first) {
-                const uint32_t v = v_at + key_tile % NB * S::kOperand;
+                const uint32_t v = v_first + key_tile % NB * (S::kOperand >> 4);
                 wait(sh.p_full[stream], done[stream]++ & 1);
                 tcgen05_after_sync();
                 const bool go = elected && !wait.lost;
 #pragma unroll
                 for (int i = 0; i < kChunkTile / 16; ++i)
-                    tcgen05_mma_ts(S::sums(stream), S::weights(stream) + 8 * i, smem_operand(v + i * 2048, 16384), kValues, !first || i > 0, go);
+                    tcgen05_mma_ts(S::sums(stream), S::weights(stream) + 8 * i, v + i * 128, kValues, !first || i > 0, go);
                 commit(sh.o_full[stream]);
             };
             auto key_ready = [&](uint32_t key_tile) {

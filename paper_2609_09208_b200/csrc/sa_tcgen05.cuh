@@ -33,24 +33,24 @@ SA_D void tcgen05_commit(uint32_t mbar, bool go) {
     asm volatile("{.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];}" ::"r"(mbar), "r"((uint32_t)go) : "memory");
 }
 
-// Shared-memory operand at `at` (see above).  Blocks of 8 rows are 1024 bytes apart; across: blocks of 64 numbers across the contraction.
-SA_D uint64_t smem_operand(uint32_t at, uint32_t across = 1024) {
-    return (uint64_t)((at >> 4) & 0x3fffu) | (uint64_t)(across >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+// Shared-memory operand at `at` (see above), the lower word of its descriptor: blocks of 64 numbers across the contraction `across` bytes apart.  Its upper word says that blocks of
+// 8 rows are 1024 bytes apart.  An operand `n` bytes further on is n / 16 more.
+SA_D uint32_t smem_operand(uint32_t at, uint32_t across = 1024) { return (at >> 4) | (across >> 4) << 16; }
+constexpr uint32_t kOperandUpper = (1024u >> 4) | 1u << 14 | 2u << 29;
 // 128 x N products of 16-bit numbers (BF16: bfloat16, else binary16), FP32 sums; the second operand's rows run across the contraction.
 SA_HD constexpr uint32_t mma_form(int n, bool bf16, bool b_across) {
     return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (b_across ? 1u : 0u) << 16 | (uint32_t)(n >> 3) << 17 | (128u >> 4) << 24;
 }
 // 16 numbers of the contraction; add: to the sums that are there.
-SA_D void tcgen05_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t form, bool add, bool go) {
-    asm volatile("{.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d), "l"(a), "l"(b), "r"(form),
-                 "r"((uint32_t)add), "r"((uint32_t)go)
+SA_D void tcgen05_mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t form, bool add, bool go) {
+    asm volatile("{.reg .pred p, q;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\tmov.b64 a, {%1, %6};\n\tmov.b64 b, {%2, %6};\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;}" ::"r"(d), "r"(a), "r"(b), "r"(form), "r"((uint32_t)add), "r"((uint32_t)go), "r"(kOperandUpper)
                  : "memory");
 }
 // ... with the first operand in tensor memory, two numbers a column.
-SA_D void tcgen05_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t form, bool add, bool go) {
-    asm volatile("{.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;}" ::"r"(d), "r"(a), "l"(b), "r"(form),
-                 "r"((uint32_t)add), "r"((uint32_t)go)
+SA_D void tcgen05_mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t form, bool add, bool go) {
+    asm volatile("{.reg .pred p, q;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\tmov.b64 b, {%2, %6};\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;}" ::"r"(d), "r"(a), "r"(b), "r"(form), "r"((uint32_t)add), "r"((uint32_t)go), "r"(kOperandUpper)
                  : "memory");
 }
 
