@@ -49,7 +49,8 @@ static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool spl
         int blocks = chunk_blocks_most();
         if (work * p.Hkv < blocks) blocks = (int)(work * p.Hkv);
         const bool pot = !p.fp16 && !p.fp4 && !p.int8;
-        if ((pot ? launch_chunk_pot(p.d, fmt, split, a, blocks, s) : launch_chunk_plain(p.d, fmt, split, a, blocks, s)) != cudaSuccess) return false;
+        const int rows_most = (int)(most < per_tile ? most : per_tile);
+        if ((pot ? launch_chunk_pot(p.d, fmt, split, a, blocks, rows_most, s) : launch_chunk_plain(p.d, fmt, split, a, blocks, rows_most, s)) != cudaSuccess) return false;
     }
     return true;
 }
@@ -102,6 +103,7 @@ sa_status sa_chunk_attention(const sa_config* cfg, const sa_cache* cache, const 
     a.workspace = static_cast<uint8_t*>(workspace);
     a.Hq = p.Hq;
     a.G = p.G;
+    a.by_group = ChunkDivisor(p.G);
     a.window = window;
     a.sinks = sinks;
     a.bf16 = o_dtype == SA_BF16;

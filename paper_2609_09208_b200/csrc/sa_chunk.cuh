@@ -62,12 +62,24 @@ struct ChunkSeqs {
     int64_t row0[kChunkBatch];
     int tiles[kChunkBatch + 1];           // row tiles ahead of it
 };
+// x / d for 0 <= x < 2^31 by a product (Granlund and Montgomery): mul = floor(2^(31 + s) / d) + 1 with 2^s >= d is off by at most d / d 2^-s, too little to matter.
+struct ChunkDivisor {
+    uint32_t mul;
+    int shift;
+    ChunkDivisor() = default;
+    explicit ChunkDivisor(int d) : mul(0), shift(31) {
+        while ((1ll << (shift - 31)) < d) ++shift;
+        mul = (uint32_t)((1ull << shift) / (uint64_t)d + 1);
+    }
+    SA_HD int operator()(int x) const { return (int)((uint64_t)(uint32_t)x * mul >> shift); }
+};
 struct ChunkArgs {
     CacheArgs c;
+    ChunkDivisor by_group;                // rows (token, query head of the group) to tokens
     const uint16_t* Q;
     void* O;
     uint8_t* workspace;
-    int Hq, G, window, sinks;
+    int Hq, G, window, sinks;             // G: query heads of a group
     int copies;                           // SPLIT: 1, 2 or 4 copies of the rows in a tile
     int bf16;                             // type of O
     float factor;                         // log2(e) / sqrt(d) and the unit of the operands
@@ -98,8 +110,8 @@ SA_D ChunkUnit chunk_unit(const ChunkArgs& a, const int* lens, int flat, int per
     u.row0 = (flat - a.s.tiles[lo]) * per_tile;
     u.rows = min(per_tile, a.s.tokens[lo] * a.G - u.row0);
     const int before = lens[lo] - a.s.tokens[lo];
-    u.first = before + u.row0 / a.G;
-    u.last = before + (u.row0 + u.rows - 1) / a.G;
+    u.first = before + a.by_group(u.row0);
+    u.last = before + a.by_group(u.row0 + u.rows - 1);
     const int most = a.c.max_pages > 0x7fffffff / kPageTokens ? 0x7fffffff : a.c.max_pages * kPageTokens;
     u.hi = min(u.last, most - 1) + 1;
     u.lo = a.window && u.first >= a.window ? u.first - a.window + 1 : 0;
@@ -125,9 +137,9 @@ struct ChunkPiece {
     int first[2], last[2];                // of the streams: positions of the first and last row's token
     SA_D int tile(int i) const { return begin + i < sink_tiles ? begin + i : window_tile + begin + i - sink_tiles; }
     // Row r: its token's position, its row (of heads) in Q and O.
-    SA_D int position(const ChunkArgs& a, int r) const { return token + (token_row + r) / a.G; }
+    SA_D int position(const ChunkArgs& a, int r) const { return token + a.by_group(token_row + r); }
     SA_D int64_t row(const ChunkArgs& a, int r) const {
-        const int at = token_row + r, t = at / a.G;
+        const int at = token_row + r, t = a.by_group(at);
         return (q_token + t) * a.Hq + head * a.G + (at - t * a.G);
     }
 };
@@ -392,24 +404,26 @@ struct ChunkCodes {
 // 32 queries (HALVES = 2: the first or, with half = 1, the last 16 of them) as rows of the operand, D / 16 lanes a row; returns the factor of the lane's own row, if it is one of
 // them.  row_of(r): row r's binary16 numbers, or null.
 template <int D, int FMT, int HALVES, typename RowOf>
-SA_D float chunk_queries(const ChunkArgs& a, uint32_t operand, int lane, int first_row, int half, RowOf row_of) {
+SA_D float chunk_queries(const ChunkArgs& a, uint32_t operand, int lane, int first_row, int half, RowOf row_of) {       // (rows behind the last one are zeros: whole steps of them cost little)
     using S = ChunkShape<D, FMT>;
     constexpr int LPV = D / 16, RPW = 32 / LPV, STEPS = 32 / RPW / HALVES;
     const int row0 = half * STEPS * RPW;
     const Fp4Half<D> f(lane, 0);
     uint32_t x[STEPS][8];
+    bool any[STEPS];
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
         const uint16_t* p = row_of(row0 + i * RPW + lane / LPV);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[i][e] = 0u;
         if (p) load_32_bytes(p + 16 * f.blk, (reinterpret_cast<uintptr_t>(a.Q) & 31) == 0, x[i]);
+        any[i] = __any_sync(0xffffffffu, p != nullptr);
     }
     float mine = a.factor;
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
-        if (a.c.hadamard) f.rotate(x[i]);
-        if constexpr (S::kScaled) {                                                     // as quantise_query_vec: 127 steps of the largest magnitude
+        if (a.c.hadamard && any[i]) f.rotate(x[i]);
+        if (S::kScaled && any[i]) {                                                     // as quantise_query_vec: 127 steps of the largest magnitude
             uint32_t top = x[i][0] & 0x7fff7fffu;
 #pragma unroll
             for (int e = 1; e < 8; ++e) top = __vmaxu2(top, x[i][e] & 0x7fff7fffu);
@@ -608,7 +622,7 @@ SA_D void chunk_softmax(ChunkRow& row, const float* scale, uint32_t s_col, uint3
 
 // Row r of a unit: its number in Q and O.
 SA_D int64_t chunk_row(const ChunkArgs& a, const ChunkUnit& u, int head, int r) {
-    const int at = u.row0 + r, token = at / a.G;
+    const int at = u.row0 + r, token = a.by_group(at);
     return (a.s.row0[u.seq] + token) * a.Hq + head * a.G + (at - token * a.G);
 }
 
@@ -674,16 +688,18 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         if (w < warp) ahead += sh.sums[w];
         sum += sh.sums[w];
     }
-    const long long total = sum * a.c.Hkv, blocks = min((long long)gridDim.x, total);
+    // equal stretches but for the last; 32-bit divisions where the numbers allow (64-bit ones are long routines)
+    const uint64_t total = (uint64_t)sum * a.c.Hkv;
+    const bool narrow = total >> 32 == 0;
+    const uint64_t per = narrow ? ((uint32_t)total - 1) / gridDim.x + 1 : (total - 1) / gridDim.x + 1, x0 = per * blockIdx.x, x1 = min(x0 + per, total);
     ChunkCut* cuts = reinterpret_cast<ChunkCut*>(a.workspace);
-    if (blockIdx.x >= blocks) {
+    if (x0 >= total) {
         if (tid == 0) cuts[blockIdx.x].there = 0;
         return;
     }
-    const long long x0 = total * blockIdx.x / blocks, x1 = total * (blockIdx.x + 1) / blocks;
     {
-        const int head = (int)(x0 / sum);
-        long long rest = x0 - head * sum - ahead;
+        const int head = (int)(narrow ? (uint32_t)x0 / (uint32_t)sum : x0 / (uint64_t)sum);
+        long long rest = (long long)x0 - head * sum - ahead;
         if (rest >= 0 && rest < cost) {                                // the unit at which the stretch starts is one of this thread's
             int i = mine0;
             for (;;) {
@@ -710,7 +726,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_col = lanes + stream * 128, p_col = lanes + S::weights(stream), o_col = lanes + S::sums(stream);
         const uint32_t q_operand = q_at + stream * S::kOperand;
         const int copies = SPLIT ? a.copies : 1, rows_own = 128 / copies;
-        const int row = SPLIT ? own % rows_own : stream * 128 + own;   // of the unit
+        const int row = SPLIT ? own & (rows_own - 1) : stream * 128 + own;       // of the piece
         const int chunks = 4 / (copies * kHalves), chunk0 = SPLIT ? own / rows_own * chunks : 2 * part;      // columns of 32 that this thread has
         registers_up<kRegisters.softmax>();
         uint32_t tiles_done = 0, keys_done = 0;
@@ -727,7 +743,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
             if (n > 0) {
                 const int first_row = SPLIT ? quarter * 32 : stream * 128 + quarter * 32;
                 auto query = [&](int k) -> const uint16_t* {
-                    const int at = SPLIT ? (first_row + k) % rows_own : first_row + k;
+                    const int at = SPLIT ? (first_row + k) & (rows_own - 1) : first_row + k;
                     return at < p->rows ? a.Q + p->row(a, at) * D : nullptr;
                 };
                 // (a half has the factors of its 16 rows in the lanes that the other half's 16 leave)
@@ -763,10 +779,12 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                     if (copies == 1) chunk_softmax<D, FMT, 4, true, D>(r, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
                     else if (copies == 2) chunk_softmax<D, FMT, 2, false, D>(r, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
                     else chunk_softmax<D, FMT, 1, false, D>(r, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
-                    uint32_t zero[16] = {};                            // the weights of the other copies' keys
+                    if (!S::kApart || tiles_done == 0) {               // the weights of the other copies' keys; in a place of their own they stay zeros
+                        uint32_t zero[16] = {};
 #pragma unroll 1
-                    for (int c = 0; c < 4; ++c)
-                        if (c < chunk0 || c >= chunk0 + chunks) tmem_store(p_col + 16 * c, zero);
+                        for (int c = 0; c < 4; ++c)
+                            if (c < chunk0 || c >= chunk0 + chunks) tmem_store(p_col + 16 * c, zero);
+                    }
                 }
                 ++tiles_done;
                 tmem_stored();
@@ -818,52 +836,58 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                     __syncwarp();
                 }
             } else {
-                // 2 x copies parts of every row meet, 16 channels at a time, in the queries' place
+                // The 2 x copies parts of every row meet in the queries' place: all channels at a time where the rows are few, else 16 of them.
                 sh.m[tid] = m;
                 sh.l[tid] = wait.lost ? __int_as_float(0x7fc00000) : l;
-                chunk_sync(1, 256);
                 __syncwarp();
-                float most = -1e30f, all = 0.0f;
-                for (int k = row; k < 256; k += rows_own) most = fmaxf(most, sh.m[k]);
-                const float r = ex2_approx(m - most);
+                chunk_sync(1, 256);
+                const int rows = p->rows, parts = 2 * copies;
                 float* exchange = reinterpret_cast<float*>(rings);
-                constexpr int kPitch = 20;
-                const int item_row = tid / (256 / rows_own), per_item = rows_own / 16, channel0 = tid % (256 / rows_own) * per_item;      // 2, 4 or 8 channels of a row
-                {
-                    float item_most = -1e30f;
-                    for (int k = item_row; k < 256; k += rows_own) item_most = fmaxf(item_most, sh.m[k]);
-                    for (int k = item_row; k < 256; k += rows_own) all += sh.l[k] * ex2_approx(sh.m[k] - item_most);
-                    if (slot && channel0 == 0 && item_row < p->rows) {
-                        slot[kPerTile * D + item_row] = item_most;
-                        slot[kPerTile * (D + 1) + item_row] = all;
-                    }
-                }
-                const float inv = all > 0.0f ? __fdiv_rn(1.0f, all) : all == 0.0f ? 0.0f : all;
-                const bool item_there = item_row < p->rows;
-                uint16_t* out = item_there ? static_cast<uint16_t*>(a.O) + p->row(a, item_row) * D : nullptr;
+                float most = -1e30f;
+                for (int k = 0; k < parts; ++k) most = fmaxf(most, sh.m[k * rows_own + row]);
+                const float r = ex2_approx(m - most);
+                const bool wide = parts * rows * (D + 4) * 4 <= 2 * S::kOperand;
+                const int width = wide ? D : 16, pitch = width + 4, quads = width / 4, own_part = tid / rows_own;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                    uint32_t x[16] = {};
-                    if (mine > 0) {
-                        tmem_load(o_col + c, x);
-                        tmem_loaded();
-                    }
-#pragma unroll
-                    for (int e = 0; e < 16; e += 4)
-                        *reinterpret_cast<float4*>(exchange + tid * kPitch + e) =
-                            make_float4(__uint_as_float(x[e]) * r, __uint_as_float(x[e + 1]) * r, __uint_as_float(x[e + 2]) * r, __uint_as_float(x[e + 3]) * r);
-                    chunk_sync(1, 256);
-                    if (item_there)
-                        for (int e = 0; e < per_item; e += 2) {
-                            float2 v = make_float2(0.0f, 0.0f);
-                            for (int k = item_row; k < 256; k += rows_own) {
-                                const float2 w = *reinterpret_cast<const float2*>(exchange + k * kPitch + channel0 + e);
-                                v.x += w.x;
-                                v.y += w.y;
-                            }
-                            if (slot) *reinterpret_cast<float2*>(slot + (size_t)item_row * D + c + channel0 + e) = v;
-                            else *reinterpret_cast<uint32_t*>(out + c + channel0 + e) = chunk_out(v.x * inv, v.y * inv, a.bf16);
+                for (int c0 = 0; c0 < D; c0 += width) {
+#pragma unroll 1
+                    for (int c = 0; c < width; c += 16) {
+                        uint32_t x[16] = {};
+                        if (mine > 0) {
+                            tmem_load(o_col + c0 + c, x);
+                            tmem_loaded();
                         }
+                        if (there) {
+                            float4* to = reinterpret_cast<float4*>(exchange + (own_part * rows + row) * pitch + c);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                to[e] = make_float4(__uint_as_float(x[4 * e]) * r, __uint_as_float(x[4 * e + 1]) * r, __uint_as_float(x[4 * e + 2]) * r, __uint_as_float(x[4 * e + 3]) * r);
+                        }
+                        __syncwarp();
+                    }
+                    chunk_sync(1, 256);
+                    for (int i = tid; i < rows * quads; i += 256) {
+                        const int at = i / quads, c = i % quads * 4;
+                        float top = -1e30f, all = 0.0f;
+                        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        for (int k = 0; k < parts; ++k) top = fmaxf(top, sh.m[k * rows_own + at]);
+#pragma unroll 2
+                        for (int k = 0; k < parts; ++k) {
+                            const float4 w = *reinterpret_cast<const float4*>(exchange + (k * rows + at) * pitch + c);
+                            all += sh.l[k * rows_own + at] * ex2_approx(sh.m[k * rows_own + at] - top);
+                            v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+                        }
+                        if (slot) {
+                            *reinterpret_cast<float4*>(slot + (size_t)at * D + c0 + c) = v;
+                            if (c0 + c == 0) {
+                                slot[kPerTile * D + at] = top;
+                                slot[kPerTile * (D + 1) + at] = all;
+                            }
+                        } else {
+                            const float inv = all > 0.0f ? __fdiv_rn(1.0f, all) : all == 0.0f ? 0.0f : all;
+                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + p->row(a, at) * D + c0 + c) = make_uint2(chunk_out(v.x * inv, v.y * inv, a.bf16), chunk_out(v.z * inv, v.w * inv, a.bf16));
+                        }
+                    }
                     __syncwarp();
                     chunk_sync(1, 256);
                 }
@@ -981,7 +1005,19 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                     }
                 for (int j = 0; j < n; ++j) {
                     const uint32_t now = g + j;
-                    if constexpr (SPLIT) {
+                    if constexpr (SPLIT && S::kApart) {
+                        const int stream = j & 1;
+                        scores_read(stream);
+                        if (j + 2 < n) {
+                            key_ready(now + 2);
+                            scores(stream, now + 2);
+                            commit(sh.k_empty[(now + 2) % NB]);
+                        }
+                        wait(sh.v_full[now % NB], now / NB & 1);
+                        tcgen05_after_sync();
+                        values(stream, now, j < 2);
+                        commit(sh.v_empty[now % NB]);
+                    } else if constexpr (SPLIT) {
                         const int stream = j & 1;
                         wait(sh.v_full[now % NB], now / NB & 1);
                         tcgen05_after_sync();
@@ -1069,7 +1105,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         // ---- the block's stretch, piece by piece
         registers_down<kRegisters.other>();
         int head = sh.start_head, flat = sh.start_flat, skip = sh.start_skip;      // the unit, and how far into it (its fixed cost included) the stretch starts
-        long long left = x1 - x0;
+        long long left = (long long)(x1 - x0);
         uint32_t made = 0;
         bool cut = false;
         auto place = [&]() -> ChunkPiece& {
@@ -1088,7 +1124,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
             if (end > begin || (u.count == 0 && skip == 0)) {
                 ChunkPiece& p = place();
                 if (lane == 0) {
-                    const int token = u.row0 / a.G;
+                    const int token = a.by_group(u.row0);
                     p.n = end - begin;
                     p.head = head;
                     p.b = a.s.b[u.seq];
@@ -1107,9 +1143,8 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                         p.last[i] = p.position(a, SPLIT ? u.rows - 1 : min(i * 128 + 127, u.rows - 1));
                     }
                     if (p.place == 2) {
-                        // the block that has the unit's last tile: the last one whose stretch starts at or before it
-                        const long long x = x1 + u.count - end - 1;
-                        cuts[blockIdx.x] = ChunkCut{head, flat, (int)(((x + 1) * blocks - 1) / total), 1};
+                        const uint64_t x = x1 + u.count - end - 1;     // where the unit's last tile is
+                        cuts[blockIdx.x] = ChunkCut{head, flat, (int)(narrow ? (uint32_t)x / (uint32_t)per : x / per), 1};
                         cut = true;
                     }
                 }
@@ -1134,52 +1169,87 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
     if (warp == kProducts) tmem_free();
 }
 
-// Units that the deal has cut: block x takes the one that starts in block x of the kernel above.
+// Units that the deal has cut: block (x, y) takes ROWS rows of the one that starts in block x of the kernel above.  Its threads are dealt to 4 channels of a row each, and where
+// there are more of them to the parts, of which an order independent of time is kept.
+template <int D, bool SPLIT>
+SA_HD constexpr int chunk_merge_rows() { return (SPLIT ? 256 : 2048) / D; }
 template <int D, bool SPLIT>
 __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ ChunkArgs a) {
-    constexpr int kPerTile = chunk_rows(SPLIT), kQuads = D / 4;
+    constexpr int kPerTile = chunk_rows(SPLIT), kRows = chunk_merge_rows<D, SPLIT>(), kQuads = D / 4, kItems = kRows * kQuads, kGroups = kItems < 256 ? 256 / kItems : 1, kLanes = 256 / kRows;
+    constexpr size_t kSlot = chunk_slot_floats(D, SPLIT);
+    static_assert(kItems % 256 == 0 || 256 % kItems == 0, "items are dealt evenly");
+    __shared__ int lens[kChunkBatch];
+    __shared__ float meet[2][256];
+    __shared__ float4 sums[kGroups > 1 ? 256 : 1];
     pdl_wait();
     pdl_launch_dependents();
     const ChunkCut cut = reinterpret_cast<const ChunkCut*>(a.workspace)[blockIdx.x];
     if (!cut.there) return;
-    __shared__ int lens[kChunkBatch];
-    if (threadIdx.x < a.s.n) lens[threadIdx.x] = max(a.c.seq_lens[a.s.b[threadIdx.x]], 0);
+    const int tid = threadIdx.x, row0 = blockIdx.y * kRows, first = blockIdx.x;
+    if (tid < a.s.n) lens[tid] = max(a.c.seq_lens[a.s.b[tid]], 0);
     __syncthreads();
-    const int per_tile = SPLIT ? kPerTile / a.copies : kPerTile;
-    const ChunkUnit u = chunk_unit(a, lens, cut.tile, per_tile);
+    const ChunkUnit u = chunk_unit(a, lens, cut.tile, SPLIT ? kPerTile / a.copies : kPerTile);
+    if (row0 >= u.rows) return;
     const float* slots = reinterpret_cast<const float*>(a.workspace + kChunkPlanBytes);
-    constexpr size_t kSlot = chunk_slot_floats(D, SPLIT);
-    auto part = [&](int k) { return slots + (size_t)(k == (int)blockIdx.x ? 2 * k + 1 : 2 * k) * kSlot; };
-    for (int i = blockIdx.y * 256 + threadIdx.x; i < u.rows * kQuads; i += gridDim.y * 256) {
-        const int row = i / kQuads, c = i % kQuads * 4;
-        float most = -1e30f;
-        for (int k = blockIdx.x; k <= cut.last; ++k) most = fmaxf(most, part(k)[kPerTile * D + row]);
+    auto part = [&](int k) { return slots + (size_t)(k == first ? 2 * k + 1 : 2 * k) * kSlot; };
+    // references and sums of the rows: kLanes threads a row
+    const int at = tid / kLanes, row = min(row0 + at, u.rows - 1);
+    auto all_lanes = [&](float x, int place, auto join) {
+        meet[place][tid] = x;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kLanes; ++k) x = k ? join(x, meet[place][at * kLanes + k]) : meet[place][at * kLanes];
+        return x;
+    };
+    float most = -1e30f, l = 0.0f;
+    for (int k = first + tid % kLanes; k <= cut.last; k += kLanes) most = fmaxf(most, part(k)[kPerTile * D + row]);
+    most = all_lanes(most, 0, [](float x, float y) { return fmaxf(x, y); });
+    for (int k = first + tid % kLanes; k <= cut.last; k += kLanes) l += part(k)[kPerTile * (D + 1) + row] * ex2_approx(part(k)[kPerTile * D + row] - most);
+    l = all_lanes(l, 1, [](float x, float y) { return x + y; });
+    __syncthreads();
+    meet[0][tid] = most;
+    meet[1][tid] = l;
+    __syncthreads();
+    for (int i = tid; i < kItems * kGroups; i += 256) {
+        const int item = i % kItems, group = i / kItems, r = item / kQuads, c = item % kQuads * 4;
+        const bool there = row0 + r < u.rows;
+        const float top = meet[0][r * kLanes], all = meet[1][r * kLanes];
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        float l = 0.0f;
+        if (there)
 #pragma unroll 4
-        for (int k = blockIdx.x; k <= cut.last; ++k) {
-            const float* s = part(k);
-            const float r = ex2_approx(s[kPerTile * D + row] - most);
-            const float4 x = *reinterpret_cast<const float4*>(s + (size_t)row * D + c);
-            l += s[kPerTile * (D + 1) + row] * r;
-            o.x += x.x * r, o.y += x.y * r, o.z += x.z * r, o.w += x.w * r;
+            for (int k = first + group; k <= cut.last; k += kGroups) {
+                const float* s = part(k);
+                const float f = ex2_approx(s[kPerTile * D + row0 + r] - top);
+                const float4 x = *reinterpret_cast<const float4*>(s + (size_t)(row0 + r) * D + c);
+                o.x += x.x * f, o.y += x.y * f, o.z += x.z * f, o.w += x.w * f;
+            }
+        if constexpr (kGroups > 1) {
+            sums[tid] = o;
+            __syncthreads();
+            if (group == 0)
+#pragma unroll
+                for (int k = 1; k < kGroups; ++k) {
+                    const float4 x = sums[tid + k * kItems];
+                    o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
+                }
         }
-        const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == 0.0f ? 0.0f : l;
-        uint16_t* out = static_cast<uint16_t*>(a.O) + chunk_row(a, u, cut.head, row) * D + c;
-        *reinterpret_cast<uint2*>(out) = make_uint2(chunk_out(o.x * inv, o.y * inv, a.bf16), chunk_out(o.z * inv, o.w * inv, a.bf16));
+        if (there && group == 0) {
+            const float inv = all > 0.0f ? __fdiv_rn(1.0f, all) : all == 0.0f ? 0.0f : all;
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + chunk_row(a, u, cut.head, row0 + r) * D + c) = make_uint2(chunk_out(o.x * inv, o.y * inv, a.bf16), chunk_out(o.z * inv, o.w * inv, a.bf16));
+        }
     }
 }
 
 template <int D, int FMT, bool SPLIT>
-cudaError_t launch_chunk(const ChunkArgs& a, int blocks, cudaStream_t s) {
+cudaError_t launch_chunk(const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s) {
     static OncePerDevice once;
     if (!allow_shared(chunk_kernel<D, FMT, SPLIT>, ChunkShape<D, FMT>::kBytes, once)) return cudaGetLastError();
     const cudaError_t e = launch_pdl(chunk_kernel<D, FMT, SPLIT>, dim3(blocks), dim3(chunk_threads(SPLIT)), (size_t)ChunkShape<D, FMT>::kBytes, s, a);
     if (e != cudaSuccess) return e;
-    return launch_pdl(chunk_merge_kernel<D, SPLIT>, dim3(blocks, SPLIT ? 4 : 16), dim3(256), 0, s, a);
+    return launch_pdl(chunk_merge_kernel<D, SPLIT>, dim3(blocks, (rows_most - 1) / chunk_merge_rows<D, SPLIT>() + 1), dim3(256), 0, s, a);
 }
 
-cudaError_t launch_chunk_pot(int d, int fmt, bool split, const ChunkArgs& a, int blocks, cudaStream_t s);
-cudaError_t launch_chunk_plain(int d, int fmt, bool split, const ChunkArgs& a, int blocks, cudaStream_t s);
+cudaError_t launch_chunk_pot(int d, int fmt, bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s);
+cudaError_t launch_chunk_plain(int d, int fmt, bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s);
 
 }  // namespace sa

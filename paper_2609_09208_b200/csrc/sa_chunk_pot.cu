@@ -4,20 +4,20 @@
 namespace sa {
 
 template <int D, int FMT>
-static cudaError_t launch(bool split, const ChunkArgs& a, int blocks, cudaStream_t s) {
-    return split ? launch_chunk<D, FMT, true>(a, blocks, s) : launch_chunk<D, FMT, false>(a, blocks, s);
+static cudaError_t launch(bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s) {
+    return split ? launch_chunk<D, FMT, true>(a, blocks, rows_most, s) : launch_chunk<D, FMT, false>(a, blocks, rows_most, s);
 }
 template <int D>
-static cudaError_t launch(int fmt, bool split, const ChunkArgs& a, int blocks, cudaStream_t s) {
+static cudaError_t launch(int fmt, bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s) {
     switch (fmt) {
-        case FMT_BYTE: return launch<D, FMT_BYTE>(split, a, blocks, s);
-        case FMT_NIBBLE: return launch<D, FMT_NIBBLE>(split, a, blocks, s);
-        case FMT_PLANAR1: return launch<D, FMT_PLANAR1>(split, a, blocks, s);
-        default: return launch<D, FMT_PLANAR2>(split, a, blocks, s);
+        case FMT_BYTE: return launch<D, FMT_BYTE>(split, a, blocks, rows_most, s);
+        case FMT_NIBBLE: return launch<D, FMT_NIBBLE>(split, a, blocks, rows_most, s);
+        case FMT_PLANAR1: return launch<D, FMT_PLANAR1>(split, a, blocks, rows_most, s);
+        default: return launch<D, FMT_PLANAR2>(split, a, blocks, rows_most, s);
     }
 }
-cudaError_t launch_chunk_pot(int d, int fmt, bool split, const ChunkArgs& a, int blocks, cudaStream_t s) {
-    return d == 64 ? launch<64>(fmt, split, a, blocks, s) : launch<128>(fmt, split, a, blocks, s);
+cudaError_t launch_chunk_pot(int d, int fmt, bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s) {
+    return d == 64 ? launch<64>(fmt, split, a, blocks, rows_most, s) : launch<128>(fmt, split, a, blocks, rows_most, s);
 }
 
 }  // namespace sa
