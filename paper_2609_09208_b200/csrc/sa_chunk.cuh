@@ -34,15 +34,16 @@
 namespace sa {
 
 constexpr int kChunkBatch = 128;          // sequences per launch
-// Warps of a block: softmax of two streams, 8 each (SPLIT: 4), 4 of operands (SPLIT: 4 of keys and 4 of values), then products, loader and two idle ones.
+// Warps of a block: softmax of two streams, 8 each (SPLIT: 4), 4 of operands (SPLIT: 4 of keys and 4 of values, of every other tile, twice), then products, loader, the one that
+// hands out pieces and an idle one.
 SA_HD constexpr int chunk_softmax_warps(bool split) { return split ? 8 : 16; }
-SA_HD constexpr int chunk_operand_warps(bool split) { return split ? 8 : 4; }
+SA_HD constexpr int chunk_operand_warps(bool split) { return split ? 16 : 4; }
 SA_HD constexpr int chunk_threads(bool split) { return 32 * (chunk_softmax_warps(split) + chunk_operand_warps(split) + 4); }
 // Registers of a thread: what the block is launched with, and what the groups of four warps then have of it.
 struct ChunkRegisters {
     int launch, softmax, operand, other;
 };
-SA_HD constexpr ChunkRegisters chunk_registers(bool split) { return split ? ChunkRegisters{96, 136, 80, 48} : ChunkRegisters{80, 96, 56, 40}; }
+SA_HD constexpr ChunkRegisters chunk_registers(bool split) { return split ? ChunkRegisters{72, 120, 56, 40} : ChunkRegisters{80, 96, 56, 40}; }
 SA_HD constexpr bool chunk_registers_fit(bool split) {
     const ChunkRegisters r = chunk_registers(split);
     return 32 * (chunk_softmax_warps(split) * r.softmax + chunk_operand_warps(split) * r.operand + 4 * r.other) <= chunk_threads(split) * r.launch && chunk_threads(split) * r.launch <= 65536;
@@ -180,7 +181,7 @@ struct ChunkShared {                      // behind the rings
     int lens[kChunkBatch];
     uint32_t tmem;
     int start_head, start_flat, start_skip;
-    long long sums[24];
+    long long sums[28];
 };
 static_assert(sizeof(ChunkShared) <= 12288, "room behind the rings");
 
@@ -899,10 +900,12 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         // ---- operands: a key a thread
         registers_down<kRegisters.operand>();
         const int part = warp & 3, row = part * 32 + lane;             // half page of the tile
-        const bool keys = !SPLIT || warp < kOperands + 4, values = !SPLIT || warp >= kOperands + 4;
+        const int group = (warp - kOperands) >> 3;                     // SPLIT: which tiles
+        const bool keys = !SPLIT || !(warp & 4), values = !SPLIT || (warp & 4);
         uint32_t keys_done = 0;
         while (const ChunkPiece* p = reader.next()) {
             for (int j = 0; j < p->n; ++j, ++keys_done) {
+                if (SPLIT && (int)(keys_done & 1) != group) continue;
                 const int stage = keys_done % S::kStages, buffer = keys_done % NB, slot = keys_done & 3;
                 const uint32_t turn = keys_done / NB & 1;
                 const int t0 = p->tile(j) * kChunkTile, key = t0 + row;
