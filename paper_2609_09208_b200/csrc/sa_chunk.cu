@@ -4,7 +4,7 @@
 namespace sa {
 
 static size_t chunk_workspace(const Plan& p, int64_t rows_most, int blocks) {
-    return kChunkPlanBytes + 2 * (size_t)blocks * sizeof(float) * chunk_slot_floats(p.d, rows_most <= chunk_rows(true));
+    return kChunkCutBytes + 2 * (size_t)blocks * sizeof(float) * chunk_slot_floats(p.d, rows_most <= chunk_rows(true));
 }
 static int chunk_blocks_most() { return sm_count() < kChunkBlocksMost ? sm_count() : kChunkBlocksMost; }
 
@@ -31,7 +31,7 @@ static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool spl
     for (int b = 0; b < a.c.batch;) {
         a.s.n = 0;
         a.s.tiles[0] = 0;
-        int64_t work = 0;
+        int64_t work = 0, longest = 0;                                          // key tiles, by what the cache has room for
         for (; b < a.c.batch && a.s.n < kChunkBatch; ++b) {
             const int64_t n = cu[b + 1] - cu[b], rows = n * p.G;
             if (n == 0 || (rows <= chunk_rows(true)) != split) continue;
@@ -43,11 +43,15 @@ static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool spl
             a.s.tiles[i + 1] = a.s.tiles[i] + tiles;
             a.s.n = i + 1;
             const int64_t window = a.window ? ((int64_t)a.window + per_tile / p.G + 1) / kChunkTile + 2 + ((int64_t)a.sinks + kChunkTile - 1) / kChunkTile : tiles_most;
-            work += (int64_t)tiles * (kChunkUnitCost + (window < tiles_most ? window : tiles_most));
+            const int64_t keys = window < tiles_most ? window : tiles_most;
+            work += (int64_t)tiles * (kChunkUnitCost + keys);
+            longest = keys > longest ? keys : longest;
         }
         if (a.s.n == 0) break;
-        int blocks = chunk_blocks_most();
-        if (work * p.Hkv < blocks) blocks = (int)(work * p.Hkv);
+        // A unit a block, none of them cut, where the longest is about as long as an equal share of all: putting parts together costs 5 us, 6 tiles.
+        const int64_t units = (int64_t)a.s.tiles[a.s.n] * p.Hkv, blocks_most = chunk_blocks_most();
+        a.whole = units <= blocks_most && longest * (blocks_most - units) <= 6 * blocks_most;
+        const int blocks = (int)(a.whole ? units : work * p.Hkv < blocks_most ? work * p.Hkv : blocks_most);
         const bool pot = !p.fp16 && !p.fp4 && !p.int8;
         const int rows_most = (int)(most < per_tile ? most : per_tile);
         if ((pot ? launch_chunk_pot(p.d, fmt, split, a, blocks, rows_most, s) : launch_chunk_plain(p.d, fmt, split, a, blocks, rows_most, s)) != cudaSuccess) return false;

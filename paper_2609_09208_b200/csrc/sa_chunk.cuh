@@ -51,8 +51,8 @@ SA_HD constexpr bool chunk_registers_fit(bool split) {
 static_assert(chunk_registers_fit(false) && chunk_registers_fit(true), "the groups' registers are those of the launch");
 constexpr int kChunkTile = 128;           // keys
 constexpr int kChunkUnitCost = 4;         // what a unit costs beside its tiles, in tiles
-constexpr int kChunkPlanBytes = 16384;    // of the workspace, ahead of the partial sums: a ChunkCut a block
-constexpr int kChunkBlocksMost = kChunkPlanBytes / 16;
+constexpr int kChunkBlocksMost = 1024;
+constexpr int kChunkCutBytes = kChunkBlocksMost * 96;      // of the workspace, ahead of the partial sums: the piece of every block that the cut behind it goes through
 SA_HD constexpr int chunk_rows(bool split) { return split ? 128 : 256; }
 SA_HD constexpr size_t chunk_slot_floats(int d, bool split) { return (size_t)chunk_rows(split) * (d + 2); }
 
@@ -82,15 +82,11 @@ struct ChunkArgs {
     uint8_t* workspace;
     int Hq, G, window, sinks;             // G: query heads of a group
     int copies;                           // SPLIT: 1, 2 or 4 copies of the rows in a tile
+    int whole;                            // a unit a block: none is cut
     int bf16;                             // type of O
     float factor;                         // log2(e) / sqrt(d) and the unit of the operands
     ChunkSeqs s;
 };
-// A unit that the cut behind a block goes through and that starts in it: its parts are the block's second place and the first places of the blocks up to `last`.
-struct ChunkCut {
-    int head, tile, last, there;
-};
-
 // Key tiles that the rows of a row tile need, in the order in which they are taken: those of the first tokens, then those of the window.
 struct ChunkUnit {
     int seq, row0, rows;                  // in the launch; rows of the sequence's (token, head of the group) pairs
@@ -134,7 +130,8 @@ struct ChunkPiece {
     int64_t q_token;                      // that token's row in Q and O
     int lo, hi;                           // keys lo .. hi - 1, and below sinks
     int sink_tiles, window_tile, begin;   // of the unit; the piece's first tile
-    int place;                            // 0: the whole unit; 1, 2: its sums go to the block's first, second place
+    int place;                            // 0: the whole unit; 1, 2: its sums go to the block's first, second place,
+    int last_block;                       // 2: the unit's other parts are in the first places of the blocks up to this one
     int first[2], last[2];                // of the streams: positions of the first and last row's token
     SA_D int tile(int i) const { return begin + i < sink_tiles ? begin + i : window_tile + begin + i - sink_tiles; }
     // Row r: its token's position, its row (of heads) in Q and O.
@@ -144,6 +141,8 @@ struct ChunkPiece {
         return (q_token + t) * a.Hq + head * a.G + (at - t * a.G);
     }
 };
+static_assert(sizeof(ChunkPiece) <= 96, "room in the workspace");
+SA_D ChunkPiece* chunk_cut(const ChunkArgs& a, int block) { return reinterpret_cast<ChunkPiece*>(a.workspace + block * 96); }
 constexpr int kChunkPieces = 8;           // of them in the ring, as the loader may be several ahead
 
 // Shared memory of a block.
@@ -158,6 +157,7 @@ struct ChunkShape {
     static constexpr int kFit = (227 * 1024 - 1024 - kFixed) / kRaw;
     static constexpr int kStages = kFit > 4 ? 4 : kFit;
     static constexpr int kBytes = 1024 + kFixed + kStages * kRaw;     // (1024: to align)
+    static constexpr int kRing = kStages % 2 ? 2 * kStages : kStages;  // barriers of the records: an even number, so that warps which take every other tile see all phases of theirs
     static constexpr int kV = (FMT == FMT_FP16) ? 64 * D : FMT == FMT_FP4 ? 18 * D : kHalf - 32 * D;      // offset of the values in a half
     static constexpr int kMeta = FMT == FMT_FP4 ? 16 * D : kV - 128;
     static constexpr bool kScaled = FMT != FMT_FP16 && FMT != FMT_FP4;                                  // keys have a scale of their own
@@ -176,12 +176,10 @@ struct ChunkShared {                      // behind the rings
     int2 info[4];                         // of four tiles: first key; bits 0, 1: pages there are, 2, 3: streams whose rows see all of the tile
     ChunkPiece pieces[kChunkPieces];
     unsigned long long piece_full[kChunkPieces], piece_empty[kChunkPieces];
-    uint32_t raw_info[4];
-    unsigned long long raw_full[4], raw_empty[4], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], s_free[2], p_full[2], o_full[2], done;
+    uint32_t raw_info[4];                 // of a place of records: which of the tile's pages there are
+    unsigned long long raw_full[6], raw_empty[6], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], s_free[2], p_full[2], o_full[2], done;
     int lens[kChunkBatch];
     uint32_t tmem;
-    int start_head, start_flat, start_skip;
-    long long sums[28];
 };
 static_assert(sizeof(ChunkShared) <= 12288, "room behind the rings");
 
@@ -621,12 +619,6 @@ SA_D void chunk_softmax(ChunkRow& row, const float* scale, uint32_t s_col, uint3
     row.l += l0 + l1;
 }
 
-// Row r of a unit: its number in Q and O.
-SA_D int64_t chunk_row(const ChunkArgs& a, const ChunkUnit& u, int head, int r) {
-    const int at = u.row0 + r, token = a.by_group(at);
-    return (a.s.row0[u.seq] + token) * a.Hq + head * a.G + (at - token * a.G);
-}
-
 template <int D, int FMT, bool SPLIT>
 __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __grid_constant__ ChunkArgs a) {
     using S = ChunkShape<D, FMT>;
@@ -643,7 +635,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
     const int per_tile = SPLIT ? kPerTile / a.copies : kPerTile;
 
     if (tid == 0) {
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < S::kRing; ++i) {
             mbar_init(smem_addr(&sh.raw_full[i]), 1);
             mbar_init(smem_addr(&sh.raw_empty[i]), SPLIT ? 8 : 4);
         }
@@ -665,59 +657,12 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         mbar_init(smem_addr(&sh.done), 1);
         fence_mbar_init();
     }
-    pdl_wait();
-    pdl_launch_dependents();
-
-    // ---- the deal
-    const int n_flat = a.s.tiles[a.s.n];
-    if (tid < a.s.n) sh.lens[tid] = max(a.c.seq_lens[a.s.b[tid]], 0);
-    __syncthreads();
-    const int each = (n_flat + kThreads - 1) / kThreads, mine0 = min(tid * each, n_flat), mine1 = min(mine0 + each, n_flat);
-    long long cost = 0;
-    for (int i = mine0; i < mine1; ++i) cost += kChunkUnitCost + chunk_unit(a, sh.lens, i, per_tile).count;
-    long long ahead = cost;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long x = __shfl_up_sync(0xffffffffu, ahead, o);
-        if (lane >= o) ahead += x;
-    }
-    if (lane == 31) sh.sums[warp] = ahead;
-    __syncthreads();
-    long long sum = 0;
-    ahead -= cost;
-    for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) ahead += sh.sums[w];
-        sum += sh.sums[w];
-    }
-    // equal stretches but for the last; 32-bit divisions where the numbers allow (64-bit ones are long routines)
-    const uint64_t total = (uint64_t)sum * a.c.Hkv;
-    const bool narrow = total >> 32 == 0;
-    const uint64_t per = narrow ? ((uint32_t)total - 1) / gridDim.x + 1 : (total - 1) / gridDim.x + 1, x0 = per * blockIdx.x, x1 = min(x0 + per, total);
-    ChunkCut* cuts = reinterpret_cast<ChunkCut*>(a.workspace);
-    if (x0 >= total) {
-        if (tid == 0) cuts[blockIdx.x].there = 0;
-        return;
-    }
-    {
-        const int head = (int)(narrow ? (uint32_t)x0 / (uint32_t)sum : x0 / (uint64_t)sum);
-        long long rest = (long long)x0 - head * sum - ahead;
-        if (rest >= 0 && rest < cost) {                                // the unit at which the stretch starts is one of this thread's
-            int i = mine0;
-            for (;;) {
-                const int c = kChunkUnitCost + chunk_unit(a, sh.lens, i, per_tile).count;
-                if (rest < c) break;
-                rest -= c;
-                ++i;
-            }
-            sh.start_head = head;
-            sh.start_flat = i;
-            sh.start_skip = (int)rest;
-        }
-    }
     if (warp == kProducts) tmem_alloc(smem_addr(&sh.tmem));
     tcgen05_before_sync();
     __syncthreads();
     tcgen05_after_sync();
+    pdl_wait();
+    pdl_launch_dependents();
     ChunkWait wait;
     ChunkReader reader{sh};
 
@@ -806,7 +751,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
             }
             // ---- the piece's sums
             float* slot = nullptr;
-            if (p->place) slot = reinterpret_cast<float*>(a.workspace + kChunkPlanBytes) + (size_t)(2 * blockIdx.x + p->place - 1) * chunk_slot_floats(D, SPLIT);
+            if (p->place) slot = reinterpret_cast<float*>(a.workspace + kChunkCutBytes) + (size_t)(2 * blockIdx.x + p->place - 1) * chunk_slot_floats(D, SPLIT);
             const bool there = row < p->rows;
             if constexpr (!SPLIT) {
                 const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == 0.0f ? 0.0f : l;
@@ -839,7 +784,6 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
             } else {
                 // The 2 x copies parts of every row meet in the queries' place: all channels at a time where the rows are few, else 16 of them.
                 sh.m[tid] = m;
-                sh.l[tid] = wait.lost ? __int_as_float(0x7fc00000) : l;
                 __syncwarp();
                 chunk_sync(1, 256);
                 const int rows = p->rows, parts = 2 * copies;
@@ -847,48 +791,50 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 float most = -1e30f;
                 for (int k = 0; k < parts; ++k) most = fmaxf(most, sh.m[k * rows_own + row]);
                 const float r = ex2_approx(m - most);
+                sh.l[tid] = wait.lost ? __int_as_float(0x7fc00000) : l * r;
                 const bool wide = parts * rows * (D + 4) * 4 <= 2 * S::kOperand;
-                const int width = wide ? D : 16, pitch = width + 4, quads = width / 4, own_part = tid / rows_own;
+                const int width = wide ? D : 16, pitch = width + 4, quads = width / 4;
 #pragma unroll 1
                 for (int c0 = 0; c0 < D; c0 += width) {
-#pragma unroll 1
-                    for (int c = 0; c < width; c += 16) {
-                        uint32_t x[16] = {};
+                    auto put = [&](auto columns, int c) {
+                        constexpr int C = decltype(columns)::value;
+                        uint32_t x[C] = {};
                         if (mine > 0) {
                             tmem_load(o_col + c0 + c, x);
                             tmem_loaded();
                         }
                         if (there) {
-                            float4* to = reinterpret_cast<float4*>(exchange + (own_part * rows + row) * pitch + c);
+                            float4* to = reinterpret_cast<float4*>(exchange + (tid / rows_own * rows + row) * pitch + c);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
+                            for (int e = 0; e < C / 4; ++e)
                                 to[e] = make_float4(__uint_as_float(x[4 * e]) * r, __uint_as_float(x[4 * e + 1]) * r, __uint_as_float(x[4 * e + 2]) * r, __uint_as_float(x[4 * e + 3]) * r);
                         }
                         __syncwarp();
-                    }
+                    };
+                    if (wide) {
+#pragma unroll 1
+                        for (int c = 0; c < D; c += 32) put(std::integral_constant<int, 32>(), c);
+                    } else put(std::integral_constant<int, 16>(), 0);
                     chunk_sync(1, 256);
                     for (int i = tid; i < rows * quads; i += 256) {
                         const int at = i / quads, c = i % quads * 4;
-                        float top = -1e30f, all = 0.0f;
+                        float all = 0.0f;
                         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        for (int k = 0; k < parts; ++k) top = fmaxf(top, sh.m[k * rows_own + at]);
-#pragma unroll 2
+#pragma unroll 4
                         for (int k = 0; k < parts; ++k) {
                             const float4 w = *reinterpret_cast<const float4*>(exchange + (k * rows + at) * pitch + c);
-                            all += sh.l[k * rows_own + at] * ex2_approx(sh.m[k * rows_own + at] - top);
+                            all += sh.l[k * rows_own + at];
                             v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
                         }
                         if (slot) {
                             *reinterpret_cast<float4*>(slot + (size_t)at * D + c0 + c) = v;
-                            if (c0 + c == 0) {
-                                slot[kPerTile * D + at] = top;
-                                slot[kPerTile * (D + 1) + at] = all;
-                            }
+                            if (c0 + c == 0) slot[kPerTile * (D + 1) + at] = all;
                         } else {
                             const float inv = all > 0.0f ? __fdiv_rn(1.0f, all) : all == 0.0f ? 0.0f : all;
                             *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + p->row(a, at) * D + c0 + c) = make_uint2(chunk_out(v.x * inv, v.y * inv, a.bf16), chunk_out(v.z * inv, v.w * inv, a.bf16));
                         }
                     }
+                    if (slot && c0 == 0 && tid < rows) slot[kPerTile * D + tid] = most;      // (threads 0 .. rows - 1 are the first copies of their rows)
                     __syncwarp();
                     chunk_sync(1, 256);
                 }
@@ -906,10 +852,11 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         while (const ChunkPiece* p = reader.next()) {
             for (int j = 0; j < p->n; ++j, ++keys_done) {
                 if (SPLIT && (int)(keys_done & 1) != group) continue;
-                const int stage = keys_done % S::kStages, buffer = keys_done % NB, slot = keys_done & 3;
-                const uint32_t turn = keys_done / NB & 1;
+                const int stage = keys_done % S::kStages, record = keys_done % S::kRing, buffer = keys_done % NB, slot = keys_done & 3;
+                // the operands' places are free once the products of the tile NB ahead are done: announced by turns at two barriers, so that warps which take every other tile have one
+                const uint32_t free_at = keys_done & 1, turn = ((keys_done + 2 - NB) >> 1) - 1 & 1;
                 const int t0 = p->tile(j) * kChunkTile, key = t0 + row;
-                wait(sh.raw_full[stage], keys_done / S::kStages & 1);
+                wait(sh.raw_full[record], keys_done / S::kRing & 1);
                 const uint8_t* half = raw + stage * S::kRaw + part * S::kHalf;
                 const int pages = (int)sh.raw_info[stage];
                 // what no row sees is zero: it may hold anything, and a weight of zero times that is not zero
@@ -917,7 +864,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 if (keys) {
                     const uint32_t operand = k_at + buffer * S::kOperand;
                     ChunkCodes<D, FMT, true> codes(half, lane);
-                    wait(sh.k_empty[buffer], turn ^ 1);
+                    wait(sh.k_empty[free_at], turn);
                     codes.put(half, lane, operand, row, seen);
                     if constexpr (S::kScaled) {
                         // (of a key of zeros, whose scores are zeros, and of one that nobody sees: any number but zero, which -inf is multiplied by)
@@ -935,13 +882,13 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 if (values) {
                     const uint32_t operand = v_at + buffer * S::kOperand;
                     ChunkCodes<D, FMT, false> codes(half, lane);
-                    wait(sh.v_empty[buffer], turn ^ 1);
+                    wait(sh.v_empty[free_at], turn);
                     codes.put(half, lane, operand, row, seen);
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_addr(&sh.v_full[buffer]));
                 }
-                if (lane == 0) mbar_arrive(smem_addr(&sh.raw_empty[stage]));
+                if (lane == 0) mbar_arrive(smem_addr(&sh.raw_empty[record]));
             }
             reader.leave();
         }
@@ -999,12 +946,12 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 key_ready(g);
                 scores(0, g);
                 if constexpr (!SPLIT) scores(1, g);
-                commit(sh.k_empty[g % NB]);
+                commit(sh.k_empty[(g + NB) & 1]);
                 if constexpr (SPLIT)
                     if (n > 1) {
                         key_ready(g + 1);
                         scores(1, g + 1);
-                        commit(sh.k_empty[(g + 1) % NB]);
+                        commit(sh.k_empty[(g + 1 + NB) & 1]);
                     }
                 for (int j = 0; j < n; ++j) {
                     const uint32_t now = g + j;
@@ -1014,23 +961,23 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                         if (j + 2 < n) {
                             key_ready(now + 2);
                             scores(stream, now + 2);
-                            commit(sh.k_empty[(now + 2) % NB]);
+                            commit(sh.k_empty[(now + 2 + NB) & 1]);
                         }
                         wait(sh.v_full[now % NB], now / NB & 1);
                         tcgen05_after_sync();
                         values(stream, now, j < 2);
-                        commit(sh.v_empty[now % NB]);
+                        commit(sh.v_empty[(now + NB) & 1]);
                     } else if constexpr (SPLIT) {
                         const int stream = j & 1;
                         wait(sh.v_full[now % NB], now / NB & 1);
                         tcgen05_after_sync();
                         values(stream, now, j < 2);
-                        commit(sh.v_empty[now % NB]);
+                        commit(sh.v_empty[(now + NB) & 1]);
                         scores_read(stream);
                         if (j + 2 < n) {
                             key_ready(now + 2);
                             scores(stream, now + 2);
-                            commit(sh.k_empty[(now + 2) % NB]);
+                            commit(sh.k_empty[(now + 2 + NB) & 1]);
                         }
                     } else if constexpr (S::kApart) {
                         scores_read(0);
@@ -1041,13 +988,13 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                         scores_read(1);
                         if (j + 1 < n) {
                             scores(1, now + 1);
-                            commit(sh.k_empty[(now + 1) % NB]);
+                            commit(sh.k_empty[(now + 1 + NB) & 1]);
                         }
                         wait(sh.v_full[now % NB], now / NB & 1);
                         tcgen05_after_sync();
                         values(0, now, j == 0);
                         values(1, now, j == 0);
-                        commit(sh.v_empty[now % NB]);
+                        commit(sh.v_empty[(now + NB) & 1]);
                     } else {
                         wait(sh.v_full[now % NB], now / NB & 1);
                         tcgen05_after_sync();
@@ -1057,10 +1004,10 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                             scores(0, now + 1);
                         }
                         values(1, now, j == 0);
-                        commit(sh.v_empty[now % NB]);
+                        commit(sh.v_empty[(now + NB) & 1]);
                         if (j + 1 < n) {
                             scores(1, now + 1);
-                            commit(sh.k_empty[(now + 1) % NB]);
+                            commit(sh.k_empty[(now + 1 + NB) & 1]);
                         }
                     }
                 }
@@ -1084,10 +1031,10 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 if (at >= a.c.n_pages) at = -1;
                 for (int i = 0; i < 16 && j0 + i < n; ++i, ++keys_done) {
                     const int at0 = __shfl_sync(0xffffffffu, at, 2 * i), at1 = __shfl_sync(0xffffffffu, at, 2 * i + 1);
-                    const int stage = keys_done % S::kStages;
-                    wait(sh.raw_empty[stage], keys_done / S::kStages & 1 ^ 1);
+                    const uint32_t stage = keys_done % S::kStages, before = keys_done - S::kStages;      // (before: the tile whose place this one takes)
+                    if (keys_done >= (uint32_t)S::kStages) wait(sh.raw_empty[before % S::kRing], before / S::kRing & 1);
                     if (lane == 0 && !wait.lost) {
-                        const uint32_t bar = smem_addr(&sh.raw_full[stage]), to = smem_addr(raw + stage * S::kRaw);
+                        const uint32_t bar = smem_addr(&sh.raw_full[keys_done % S::kRing]), to = smem_addr(raw + stage * S::kRaw);
                         sh.raw_info[stage] = (at0 >= 0 ? 1u : 0u) | (at1 >= 0 ? 2u : 0u);
                         mbar_arrive_expect_tx(bar, ((at0 >= 0) + (at1 >= 0)) * 2u * S::kHalf);
                         if (at0 >= 0) bulk_g2s(to, a.c.pages + ((size_t)at0 * a.c.Hkv + head) * (2 * S::kHalf), 2 * S::kHalf, bar);
@@ -1102,13 +1049,49 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         const uint32_t last = keys_done < (uint32_t)S::kStages ? keys_done : (uint32_t)S::kStages;
         for (uint32_t i = 0; i < last; ++i) {
             const uint32_t k = keys_done - 1 - i;
-            wait(sh.raw_full[k % S::kStages], k / S::kStages & 1);
+            wait(sh.raw_full[k % S::kRing], k / S::kRing & 1);
         }
     } else if (warp == kProducts + 2) {
-        // ---- the block's stretch, piece by piece
+        // ---- the deal: the block's stretch of all units' tiles, piece by piece
         registers_down<kRegisters.other>();
-        int head = sh.start_head, flat = sh.start_flat, skip = sh.start_skip;      // the unit, and how far into it (its fixed cost included) the stretch starts
-        long long left = (long long)(x1 - x0);
+        for (int i = lane; i < a.s.n; i += 32) sh.lens[i] = max(a.c.seq_lens[a.s.b[i]], 0);
+        __syncwarp();
+        const int n_flat = a.s.tiles[a.s.n];
+        int head, flat, skip = 0;                                      // the unit, and how far into it (its fixed cost included) the stretch starts
+        uint64_t at = 0, end_at = 1, per = 1;                          // the stretch; the length of one
+        if (a.whole) {
+            head = blockIdx.x / n_flat;
+            flat = blockIdx.x % n_flat;
+        } else {
+            const int each = (n_flat + 31) / 32, mine0 = min(lane * each, n_flat), mine1 = min(mine0 + each, n_flat);
+            uint64_t cost = 0;
+            for (int i = mine0; i < mine1; ++i) cost += kChunkUnitCost + chunk_unit(a, sh.lens, i, per_tile).count;
+            uint64_t ahead = cost;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint64_t x = __shfl_up_sync(0xffffffffu, ahead, o);
+                if (lane >= o) ahead += x;
+            }
+            const uint64_t sum = __shfl_sync(0xffffffffu, ahead, 31), total = sum * a.c.Hkv;
+            ahead -= cost;
+            // equal stretches but for the last; 32-bit divisions where the numbers allow (64-bit ones are long routines)
+            per = total >> 32 == 0 ? ((uint32_t)total - 1) / gridDim.x + 1 : (total - 1) / gridDim.x + 1;
+            at = min(per * blockIdx.x, total);
+            end_at = min(at + per, total);
+            head = (int)(total >> 32 == 0 ? (uint32_t)at / (uint32_t)sum : at / sum);
+            uint64_t rest = at - head * sum;
+            const uint32_t owner = __ballot_sync(0xffffffffu, rest >= ahead && rest - ahead < cost);      // the lane that has the unit at which the stretch starts (none: no stretch)
+            int i = mine0;
+            if (owner >> lane & 1u)
+                for (rest -= ahead;; ++i) {
+                    const uint32_t c = kChunkUnitCost + chunk_unit(a, sh.lens, i, per_tile).count;
+                    if (rest < c) break;
+                    rest -= c;
+                }
+            const int from = owner ? __ffs(owner) - 1 : 0;
+            flat = __shfl_sync(0xffffffffu, i, from);
+            skip = (int)__shfl_sync(0xffffffffu, (uint32_t)rest, from);
+        }
         uint32_t made = 0;
         bool cut = false;
         auto place = [&]() -> ChunkPiece& {
@@ -1120,9 +1103,9 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
             if (lane == 0 && !wait.lost) mbar_arrive(smem_addr(&sh.piece_full[made % kChunkPieces]));
             ++made;
         };
-        while (left > 0) {
+        while (at < end_at) {
             const ChunkUnit u = chunk_unit(a, sh.lens, flat, per_tile);
-            const int cost = kChunkUnitCost + u.count, to = left < cost - skip ? skip + (int)left : cost;
+            const int cost = kChunkUnitCost + u.count, to = a.whole || end_at - at >= (uint64_t)(cost - skip) ? cost : skip + (int)(end_at - at);
             const int begin = max(skip - kChunkUnitCost, 0), end = max(to - kChunkUnitCost, 0);
             if (end > begin || (u.count == 0 && skip == 0)) {
                 ChunkPiece& p = place();
@@ -1141,26 +1124,29 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                     p.window_tile = u.window_tile;
                     p.begin = begin;
                     p.place = begin == 0 && end == u.count ? 0 : begin == 0 ? 2 : 1;
+                    if (p.place == 2) {
+                        const uint64_t last = at - skip + cost - 1;    // where the unit's last tile is
+                        p.last_block = (int)(last >> 32 == 0 ? (uint32_t)last / (uint32_t)per : last / per);
+                    }
                     for (int i = 0; i < 2; ++i) {
                         p.first[i] = p.position(a, SPLIT ? 0 : min(i * 128, u.rows - 1));
                         p.last[i] = p.position(a, SPLIT ? u.rows - 1 : min(i * 128 + 127, u.rows - 1));
                     }
                     if (p.place == 2) {
-                        const uint64_t x = x1 + u.count - end - 1;     // where the unit's last tile is
-                        cuts[blockIdx.x] = ChunkCut{head, flat, (int)(narrow ? (uint32_t)x / (uint32_t)per : x / per), 1};
+                        *chunk_cut(a, blockIdx.x) = p;
                         cut = true;
                     }
                 }
                 ready();
             }
-            left -= to - skip;
+            at += a.whole ? 1 : to - skip;
             skip = 0;
             if (++flat == n_flat) flat = 0, ++head;
         }
         ChunkPiece& p = place();
         if (lane == 0) {
             p.n = -1;
-            if (!cut) cuts[blockIdx.x].there = 0;
+            if (!cut) chunk_cut(a, blockIdx.x)->place = 0;
         }
         ready();
     } else {
@@ -1181,22 +1167,18 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
     constexpr int kPerTile = chunk_rows(SPLIT), kRows = chunk_merge_rows<D, SPLIT>(), kQuads = D / 4, kItems = kRows * kQuads, kGroups = kItems < 256 ? 256 / kItems : 1, kLanes = 256 / kRows;
     constexpr size_t kSlot = chunk_slot_floats(D, SPLIT);
     static_assert(kItems % 256 == 0 || 256 % kItems == 0, "items are dealt evenly");
-    __shared__ int lens[kChunkBatch];
     __shared__ float meet[2][256];
     __shared__ float4 sums[kGroups > 1 ? 256 : 1];
     pdl_wait();
     pdl_launch_dependents();
-    const ChunkCut cut = reinterpret_cast<const ChunkCut*>(a.workspace)[blockIdx.x];
-    if (!cut.there) return;
+    const ChunkPiece& p = *chunk_cut(a, blockIdx.x);
     const int tid = threadIdx.x, row0 = blockIdx.y * kRows, first = blockIdx.x;
-    if (tid < a.s.n) lens[tid] = max(a.c.seq_lens[a.s.b[tid]], 0);
-    __syncthreads();
-    const ChunkUnit u = chunk_unit(a, lens, cut.tile, SPLIT ? kPerTile / a.copies : kPerTile);
-    if (row0 >= u.rows) return;
-    const float* slots = reinterpret_cast<const float*>(a.workspace + kChunkPlanBytes);
+    if (p.place != 2 || row0 >= p.rows) return;
+    const int rows = p.rows, last = p.last_block;
+    const float* slots = reinterpret_cast<const float*>(a.workspace + kChunkCutBytes);
     auto part = [&](int k) { return slots + (size_t)(k == first ? 2 * k + 1 : 2 * k) * kSlot; };
     // references and sums of the rows: kLanes threads a row
-    const int at = tid / kLanes, row = min(row0 + at, u.rows - 1);
+    const int at = tid / kLanes, row = min(row0 + at, rows - 1);
     auto all_lanes = [&](float x, int place, auto join) {
         meet[place][tid] = x;
         __syncthreads();
@@ -1205,9 +1187,9 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
         return x;
     };
     float most = -1e30f, l = 0.0f;
-    for (int k = first + tid % kLanes; k <= cut.last; k += kLanes) most = fmaxf(most, part(k)[kPerTile * D + row]);
+    for (int k = first + tid % kLanes; k <= last; k += kLanes) most = fmaxf(most, part(k)[kPerTile * D + row]);
     most = all_lanes(most, 0, [](float x, float y) { return fmaxf(x, y); });
-    for (int k = first + tid % kLanes; k <= cut.last; k += kLanes) l += part(k)[kPerTile * (D + 1) + row] * ex2_approx(part(k)[kPerTile * D + row] - most);
+    for (int k = first + tid % kLanes; k <= last; k += kLanes) l += part(k)[kPerTile * (D + 1) + row] * ex2_approx(part(k)[kPerTile * D + row] - most);
     l = all_lanes(l, 1, [](float x, float y) { return x + y; });
     __syncthreads();
     meet[0][tid] = most;
@@ -1215,12 +1197,12 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
     __syncthreads();
     for (int i = tid; i < kItems * kGroups; i += 256) {
         const int item = i % kItems, group = i / kItems, r = item / kQuads, c = item % kQuads * 4;
-        const bool there = row0 + r < u.rows;
+        const bool there = row0 + r < rows;
         const float top = meet[0][r * kLanes], all = meet[1][r * kLanes];
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (there)
 #pragma unroll 4
-            for (int k = first + group; k <= cut.last; k += kGroups) {
+            for (int k = first + group; k <= last; k += kGroups) {
                 const float* s = part(k);
                 const float f = ex2_approx(s[kPerTile * D + row0 + r] - top);
                 const float4 x = *reinterpret_cast<const float4*>(s + (size_t)(row0 + r) * D + c);
@@ -1238,7 +1220,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
         }
         if (there && group == 0) {
             const float inv = all > 0.0f ? __fdiv_rn(1.0f, all) : all == 0.0f ? 0.0f : all;
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + chunk_row(a, u, cut.head, row0 + r) * D + c) = make_uint2(chunk_out(o.x * inv, o.y * inv, a.bf16), chunk_out(o.z * inv, o.w * inv, a.bf16));
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + p.row(a, row0 + r) * D + c) = make_uint2(chunk_out(o.x * inv, o.y * inv, a.bf16), chunk_out(o.z * inv, o.w * inv, a.bf16));
         }
     }
 }
@@ -1248,7 +1230,7 @@ cudaError_t launch_chunk(const ChunkArgs& a, int blocks, int rows_most, cudaStre
     static OncePerDevice once;
     if (!allow_shared(chunk_kernel<D, FMT, SPLIT>, ChunkShape<D, FMT>::kBytes, once)) return cudaGetLastError();
     const cudaError_t e = launch_pdl(chunk_kernel<D, FMT, SPLIT>, dim3(blocks), dim3(chunk_threads(SPLIT)), (size_t)ChunkShape<D, FMT>::kBytes, s, a);
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || a.whole || blocks == 1) return e;
     return launch_pdl(chunk_merge_kernel<D, SPLIT>, dim3(blocks, (rows_most - 1) / chunk_merge_rows<D, SPLIT>() + 1), dim3(256), 0, s, a);
 }
 
