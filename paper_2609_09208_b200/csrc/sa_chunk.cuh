@@ -34,21 +34,6 @@
 namespace sa {
 
 constexpr int kChunkBatch = 128;          // sequences per launch
-// Warps of a block: softmax of two streams, 8 each (SPLIT: 4), 4 of operands (SPLIT: 4 of keys and 4 of values, of every other tile, twice), then products, loader, the one that
-// hands out pieces and an idle one.
-SA_HD constexpr int chunk_softmax_warps(bool split) { return split ? 8 : 16; }
-SA_HD constexpr int chunk_operand_warps(bool split) { return split ? 16 : 4; }
-SA_HD constexpr int chunk_threads(bool split) { return 32 * (chunk_softmax_warps(split) + chunk_operand_warps(split) + 4); }
-// Registers of a thread: what the block is launched with, and what the groups of four warps then have of it.
-struct ChunkRegisters {
-    int launch, softmax, operand, other;
-};
-SA_HD constexpr ChunkRegisters chunk_registers(bool split) { return split ? ChunkRegisters{72, 120, 56, 40} : ChunkRegisters{80, 96, 56, 40}; }
-SA_HD constexpr bool chunk_registers_fit(bool split) {
-    const ChunkRegisters r = chunk_registers(split);
-    return 32 * (chunk_softmax_warps(split) * r.softmax + chunk_operand_warps(split) * r.operand + 4 * r.other) <= chunk_threads(split) * r.launch && chunk_threads(split) * r.launch <= 65536;
-}
-static_assert(chunk_registers_fit(false) && chunk_registers_fit(true), "the groups' registers are those of the launch");
 constexpr int kChunkTile = 128;           // keys
 constexpr int kChunkUnitCost = 4;         // what a unit costs beside its tiles, in tiles
 constexpr int kChunkBlocksMost = 1024;
@@ -144,6 +129,21 @@ struct ChunkPiece {
 static_assert(sizeof(ChunkPiece) <= 96, "room in the workspace");
 SA_D ChunkPiece* chunk_cut(const ChunkArgs& a, int block) { return reinterpret_cast<ChunkPiece*>(a.workspace + block * 96); }
 constexpr int kChunkPieces = 8;           // of them in the ring, as the loader may be several ahead
+
+// Warps of a block, and registers of their threads: what the block is launched with and what the groups of four warps then have of it.
+//   softmax   two streams of 4 warps, a row a thread; at head_dim 64 of 8, half a row's columns a thread: there the powers bound the kernel, and twice the warps hide more of what
+//             is around them (2048 tokens over 32 768 PoT-M4 keys 834 -> 777 us); at 128 the two threads' meeting costs more than that (a prompt of 8192 tokens, 4 bits, 549 -> 583);
+//   operands  4 warps, a key a thread (SPLIT, where little else is done with a tile: 4 for keys and 4 for values, of every other tile, twice: 209 -> 184 us of 32 single
+//             tokens over 32 768 keys);
+//   others    products, loader, the one that deals, an idle one.
+template <int D, bool SPLIT>
+struct ChunkForm {
+    static constexpr int kHalves = SPLIT || D == 128 ? 1 : 2;         // threads of a row
+    static constexpr int kSoftmax = 8 * kHalves, kOperand = SPLIT ? 16 : 4, kThreads = 32 * (kSoftmax + kOperand + 4);
+    static constexpr int kLaunch = SPLIT ? 72 : kHalves == 2 ? 80 : 128;
+    static constexpr int kSoftmaxRegs = SPLIT ? 120 : kHalves == 2 ? 96 : 192, kOperandRegs = SPLIT || kHalves == 2 ? 56 : 72, kOtherRegs = SPLIT || kHalves == 2 ? 40 : 56;
+    static_assert(32 * (kSoftmax * kSoftmaxRegs + kOperand * kOperandRegs + 4 * kOtherRegs) <= kThreads * kLaunch && kThreads * kLaunch <= 65536, "the groups' registers are those of the launch");
+};
 
 // Shared memory of a block.
 template <int D, int FMT>
@@ -533,16 +533,25 @@ SA_D float chunk_reference(ChunkRow& row, float top, bool& grown) {
     return shrink;
 }
 // Weights of 32 columns, and their sum to l (of the numbers ahead of their rounding: with the sum of the rounded ones outputs are no nearer, and a fifth more instructions).
-SA_D void chunk_weights(const ChunkRow& row, const f32x2 (&y)[16], uint32_t (&w)[16], f32x2 (&l)[2]) {
+SA_D void chunk_weights(const ChunkRow& row, f32x2 (&y)[16], uint32_t (&w)[16], f32x2 (&l)[2]) {
     const f32x2 f2 = pack_f32x2(row.factor, row.factor), m2 = pack_f32x2(7.0f - row.m, 7.0f - row.m);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        float u0, u1;
-        unpack_f32x2(ffma2(y[e], f2, m2), &u0, &u1);
-        u0 = ex2_approx(u0);
-        u1 = ex2_approx(u1);
-        w[e] = half2_of(u0, u1);
-        l[e & 1] = add2(l[e & 1], pack_f32x2(u0, u1));
+    for (int e = 0; e < 16; ++e) y[e] = ffma2(y[e], f2, m2);
+#pragma unroll
+    for (int b = 0; b < 16; b += 4) {
+#pragma unroll
+        for (int e = b; e < b + 4; ++e) {
+            float u0, u1;
+            unpack_f32x2(y[e], &u0, &u1);
+            y[e] = pack_f32x2(ex2_approx(u0), ex2_approx(u1));
+        }
+#pragma unroll
+        for (int e = b; e < b + 4; ++e) {
+            float u0, u1;
+            unpack_f32x2(y[e], &u0, &u1);
+            w[e] = half2_of(u0, u1);
+            l[e & 1] = add2(l[e & 1], y[e]);
+        }
     }
 }
 template <int D>
@@ -620,11 +629,10 @@ SA_D void chunk_softmax(ChunkRow& row, const float* scale, uint32_t s_col, uint3
 }
 
 template <int D, int FMT, bool SPLIT>
-__global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __grid_constant__ ChunkArgs a) {
+__global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel(const __grid_constant__ ChunkArgs a) {
     using S = ChunkShape<D, FMT>;
-    constexpr int kPerTile = chunk_rows(SPLIT), NB = S::kBuffers, kThreads = chunk_threads(SPLIT);
-    constexpr int kOperands = chunk_softmax_warps(SPLIT), kProducts = kOperands + chunk_operand_warps(SPLIT), kHalves = SPLIT ? 1 : 2;      // first warps; parts of a row's columns
-    constexpr ChunkRegisters kRegisters = chunk_registers(SPLIT);
+    using Form = ChunkForm<D, SPLIT>;
+    constexpr int kPerTile = chunk_rows(SPLIT), NB = S::kBuffers, kHalves = Form::kHalves, kOperands = Form::kSoftmax, kProducts = kOperands + Form::kOperand;      // (first warps)
     extern __shared__ uint8_t dynamic[];
     const uint32_t base = (smem_addr(dynamic) + 1023u) & ~1023u;
     uint8_t* const rings = dynamic + (base - smem_addr(dynamic));
@@ -652,7 +660,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         }
         for (int i = 0; i < kChunkPieces; ++i) {
             mbar_init(smem_addr(&sh.piece_full[i]), 1);
-            mbar_init(smem_addr(&sh.piece_empty[i]), chunk_softmax_warps(SPLIT) + chunk_operand_warps(SPLIT) + 2);
+            mbar_init(smem_addr(&sh.piece_empty[i]), Form::kSoftmax + Form::kOperand + 2);
         }
         mbar_init(smem_addr(&sh.done), 1);
         fence_mbar_init();
@@ -673,8 +681,8 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         const uint32_t q_operand = q_at + stream * S::kOperand;
         const int copies = SPLIT ? a.copies : 1, rows_own = 128 / copies;
         const int row = SPLIT ? own & (rows_own - 1) : stream * 128 + own;       // of the piece
-        const int chunks = 4 / (copies * kHalves), chunk0 = SPLIT ? own / rows_own * chunks : 2 * part;      // columns of 32 that this thread has
-        registers_up<kRegisters.softmax>();
+        const int chunks = 4 / (copies * kHalves), chunk0 = SPLIT ? own / rows_own * chunks : chunks * part;      // columns of 32 that this thread has
+        registers_up<Form::kSoftmaxRegs>();
         uint32_t tiles_done = 0, keys_done = 0;
         // The halves of a row meet at a barrier of their two warps, with a number of each (one barrier a meeting will do, as the next one has another place).
         auto meet = [&](float x, uint32_t place) {
@@ -694,7 +702,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 };
                 // (a half has the factors of its 16 rows in the lanes that the other half's 16 leave)
                 r.factor = chunk_queries<D, FMT, kHalves>(a, q_operand, lane, quarter * 32, part, query);
-                if constexpr (!SPLIT) {
+                if constexpr (kHalves == 2) {
                     const float others = meet(r.factor, 2);
                     if (lane / 16 != part) r.factor = others;
                 }
@@ -719,7 +727,9 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 };
                 auto same = [](float x) { return x; };
                 const uint32_t read = smem_addr(&sh.s_free[stream]);
-                if constexpr (!SPLIT) {
+                if constexpr (!SPLIT && kHalves == 1) {
+                    chunk_softmax<D, FMT, 4, false, D>(r, sh.scale[slot], s_col, p_col, 0, read, ahead, same, i > 0, o_col);
+                } else if constexpr (!SPLIT) {
                     chunk_softmax<D, FMT, 2, false, D / 2>(r, sh.scale[slot], s_col, p_col, chunk0, read, ahead, [&](float x) { return fmaxf(x, meet(x, tiles_done & 1)); }, i > 0, o_col + part * (D / 2));
                 } else {
                     if (copies == 1) chunk_softmax<D, FMT, 4, true, D>(r, sh.scale[slot], s_col, p_col, chunk0, read, ahead, same, i > 0, o_col);
@@ -747,7 +757,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
             float l = r.l;
             if constexpr (!SPLIT) {
                 if (wait.lost) l = __int_as_float(0x7fc00000);
-                l += meet(l, 2);
+                if constexpr (kHalves == 2) l += meet(l, 2);
             }
             // ---- the piece's sums
             float* slot = nullptr;
@@ -761,7 +771,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
                 }
                 uint16_t* out = there ? static_cast<uint16_t*>(a.O) + p->row(a, row) * D : nullptr;
 #pragma unroll 1
-                for (int c = part * (D / 2); c < (part + 1) * (D / 2); c += 32) {
+                for (int c = part * (D / kHalves); c < (part + 1) * (D / kHalves); c += 32) {
                     uint32_t x[32] = {};
                     if (mine > 0) {
                         tmem_load(o_col + c, x);
@@ -844,7 +854,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         }
     } else if (warp < kProducts) {
         // ---- operands: a key a thread
-        registers_down<kRegisters.operand>();
+        registers_down<Form::kOperandRegs>();
         const int part = warp & 3, row = part * 32 + lane;             // half page of the tile
         const int group = (warp - kOperands) >> 3;                     // SPLIT: which tiles
         const bool keys = !SPLIT || !(warp & 4), values = !SPLIT || (warp & 4);
@@ -894,7 +904,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         }
     } else if (warp == kProducts) {
         // ---- products
-        registers_down<kRegisters.other>();
+        registers_down<Form::kOtherRegs>();
         {
             const bool elected = elect_lane();
             const uint32_t q_first = smem_operand(q_at), k_first = smem_operand(k_at), v_first = smem_operand(v_at, 16384);
@@ -1018,7 +1028,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         }
     } else if (warp == kProducts + 1) {
         // ---- loader
-        registers_down<kRegisters.other>();
+        registers_down<Form::kOtherRegs>();
         fence_proxy_async_global();                                    // (the records were written by ordinary stores)
         uint32_t keys_done = 0;
         while (const ChunkPiece* p = reader.next()) {
@@ -1053,7 +1063,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         }
     } else if (warp == kProducts + 2) {
         // ---- the deal: the block's stretch of all units' tiles, piece by piece
-        registers_down<kRegisters.other>();
+        registers_down<Form::kOtherRegs>();
         for (int i = lane; i < a.s.n; i += 32) sh.lens[i] = max(a.c.seq_lens[a.s.b[i]], 0);
         __syncwarp();
         const int n_flat = a.s.tiles[a.s.n];
@@ -1150,7 +1160,7 @@ __global__ void __launch_bounds__(chunk_threads(SPLIT), 1) chunk_kernel(const __
         }
         ready();
     } else {
-        registers_down<kRegisters.other>();
+        registers_down<Form::kOtherRegs>();
     }
     tcgen05_before_sync();
     __syncthreads();
@@ -1229,7 +1239,7 @@ template <int D, int FMT, bool SPLIT>
 cudaError_t launch_chunk(const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s) {
     static OncePerDevice once;
     if (!allow_shared(chunk_kernel<D, FMT, SPLIT>, ChunkShape<D, FMT>::kBytes, once)) return cudaGetLastError();
-    const cudaError_t e = launch_pdl(chunk_kernel<D, FMT, SPLIT>, dim3(blocks), dim3(chunk_threads(SPLIT)), (size_t)ChunkShape<D, FMT>::kBytes, s, a);
+    const cudaError_t e = launch_pdl(chunk_kernel<D, FMT, SPLIT>, dim3(blocks), dim3(ChunkForm<D, SPLIT>::kThreads), (size_t)ChunkShape<D, FMT>::kBytes, s, a);
     if (e != cudaSuccess || a.whole || blocks == 1) return e;
     return launch_pdl(chunk_merge_kernel<D, SPLIT>, dim3(blocks, (rows_most - 1) / chunk_merge_rows<D, SPLIT>() + 1), dim3(256), 0, s, a);
 }
