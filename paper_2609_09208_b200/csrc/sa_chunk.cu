@@ -52,6 +52,7 @@ static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool spl
         const int64_t units = (int64_t)a.s.tiles[a.s.n] * p.Hkv, blocks_most = chunk_blocks_most();
         a.whole = units <= blocks_most && longest * (blocks_most - units) <= 6 * blocks_most;
         const int blocks = (int)(a.whole ? units : work * p.Hkv < blocks_most ? work * p.Hkv : blocks_most);
+        a.merged = !a.whole && blocks > 1;
         const bool pot = !p.fp16 && !p.fp4 && !p.int8;
         const int rows_most = (int)(most < per_tile ? most : per_tile);
         if ((pot ? launch_chunk_pot(p.d, fmt, split, a, blocks, rows_most, s) : launch_chunk_plain(p.d, fmt, split, a, blocks, rows_most, s)) != cudaSuccess) return false;

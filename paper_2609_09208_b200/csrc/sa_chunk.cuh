@@ -67,7 +67,7 @@ struct ChunkArgs {
     uint8_t* workspace;
     int Hq, G, window, sinks;             // G: query heads of a group
     int copies;                           // SPLIT: 1, 2 or 4 copies of the rows in a tile
-    int whole;                            // a unit a block: none is cut
+    int whole, merged;                    // a unit a block: none is cut; chunk_merge_kernel follows
     int bf16;                             // type of O
     float factor;                         // log2(e) / sqrt(d) and the unit of the operands
     ChunkSeqs s;
@@ -153,7 +153,7 @@ struct ChunkShape {
     static constexpr int kRaw = 4 * kHalf;                            // records of a tile
     static constexpr int kOperand = D / 64 * 16384;                   // 128 rows
     static constexpr int kBuffers = D == 64 ? 2 : 1;                  // of operands
-    static constexpr int kFixed = (2 + 2 * kBuffers) * kOperand + 12288;
+    static constexpr int kFixed = (2 + 2 * kBuffers) * kOperand + 14336;
     static constexpr int kFit = (227 * 1024 - 1024 - kFixed) / kRaw;
     static constexpr int kStages = kFit > 4 ? 4 : kFit;
     static constexpr int kBytes = 1024 + kFixed + kStages * kRaw;     // (1024: to align)
@@ -170,18 +170,20 @@ struct ChunkShape {
     SA_HD static constexpr uint32_t sums(int stream) { return 256 + D * stream; }
 };
 struct ChunkShared {                      // behind the rings
-    float scale[4][kChunkTile];           // of the keys of four tiles
+    // Of eight tiles.  Tile j's place is written once the products of the scores of tile j - 2 (head_dim 128: j - 1) are done, which are issued when the softmax has read the scores of the
+    // tile before in their stream: it may be at tile j - 5 then, no further back (SPLIT; else at j - 3).
+    float scale[8][kChunkTile];           // of the keys
     float m[256], l[256];                 // SPLIT: of all threads' rows
-    float meet[3][512];                   // else: what the two halves of a row tell each other: largest scores of a tile and of the next, and what a piece begins and ends with
-    int2 info[4];                         // of four tiles: first key; bits 0, 1: pages there are, 2, 3: streams whose rows see all of the tile
+    float meet[3][512];                   // else: what the two halves of a row tell each other
+    int2 info[8];                         // first key, and raw_info
     ChunkPiece pieces[kChunkPieces];
     unsigned long long piece_full[kChunkPieces], piece_empty[kChunkPieces];
-    uint32_t raw_info[4];                 // of a place of records: which of the tile's pages there are
+    uint32_t raw_info[4];                 // of a place of records: bits 0, 1: which of the tile's pages there are, 2, 3: streams whose rows see all of the tile
     unsigned long long raw_full[6], raw_empty[6], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], s_free[2], p_full[2], o_full[2], done;
     int lens[kChunkBatch];
     uint32_t tmem;
 };
-static_assert(sizeof(ChunkShared) <= 12288, "room behind the rings");
+static_assert(sizeof(ChunkShared) <= 14336, "room behind the rings");
 
 // A wait that ends: where the limit is reached, nothing is waited for any more and the outputs become NaN.  A poll may sleep up to 2 us, so that waiting warps leave
 // their issue slots to the others (without it a tenth of all instructions were polls), and the limit is a third of a second.
@@ -670,7 +672,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
     __syncthreads();
     tcgen05_after_sync();
     pdl_wait();
-    pdl_launch_dependents();
+    if (a.merged) pdl_launch_dependents();                             // (else a call behind this one that reads its output early would be too early)
     ChunkWait wait;
     ChunkReader reader{sh};
 
@@ -684,7 +686,8 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         const int chunks = 4 / (copies * kHalves), chunk0 = SPLIT ? own / rows_own * chunks : chunks * part;      // columns of 32 that this thread has
         registers_up<Form::kSoftmaxRegs>();
         uint32_t tiles_done = 0, keys_done = 0;
-        // The halves of a row meet at a barrier of their two warps, with a number of each (one barrier a meeting will do, as the next one has another place).
+        // The halves of a row meet at a barrier of their two warps, with a number of each.  One barrier a meeting will do where between two meetings at the same place there is one at
+        // another: factors at place 2, tiles at 0 and 1 in turn, sums at that of the next tile.
         auto meet = [&](float x, uint32_t place) {
             float* at = sh.meet[place];
             at[tid] = x;
@@ -712,7 +715,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                 if (lane == 0) mbar_arrive(smem_addr(&sh.q_full[stream]));
             }
             for (int i = 0; i < mine; ++i) {
-                const int slot = (SPLIT ? keys_done + 2 * i + stream : tiles_done) & 3;
+                const int slot = (SPLIT ? keys_done + 2 * i + stream : tiles_done) & 7;
                 wait(sh.s_full[stream], tiles_done & 1);
                 tcgen05_after_sync();
                 const int2 info = sh.info[slot];
@@ -757,7 +760,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
             float l = r.l;
             if constexpr (!SPLIT) {
                 if (wait.lost) l = __int_as_float(0x7fc00000);
-                if constexpr (kHalves == 2) l += meet(l, 2);
+                if (kHalves == 2 && n > 0) l += meet(l, tiles_done & 1);
             }
             // ---- the piece's sums
             float* slot = nullptr;
@@ -852,6 +855,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
             tcgen05_before_sync();
             reader.leave();
         }
+        if (!a.merged) __threadfence();                                // as sa_rotate_qkv's kernel: a decode call behind this one reads its queries before it waits
     } else if (warp < kProducts) {
         // ---- operands: a key a thread
         registers_down<Form::kOperandRegs>();
@@ -862,7 +866,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         while (const ChunkPiece* p = reader.next()) {
             for (int j = 0; j < p->n; ++j, ++keys_done) {
                 if (SPLIT && (int)(keys_done & 1) != group) continue;
-                const int stage = keys_done % S::kStages, record = keys_done % S::kRing, buffer = keys_done % NB, slot = keys_done & 3;
+                const int stage = keys_done % S::kStages, record = keys_done % S::kRing, buffer = keys_done % NB, slot = keys_done & 7;
                 // the operands' places are free once the products of the tile NB ahead are done: announced by turns at two barriers, so that warps which take every other tile have one
                 const uint32_t free_at = keys_done & 1, turn = ((keys_done + 2 - NB) >> 1) - 1 & 1;
                 const int t0 = p->tile(j) * kChunkTile, key = t0 + row;
@@ -874,17 +878,13 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                 if (keys) {
                     const uint32_t operand = k_at + buffer * S::kOperand;
                     ChunkCodes<D, FMT, true> codes(half, lane);
+                    uint32_t scale = 0;
+                    if constexpr (S::kScaled) scale = seen ? *reinterpret_cast<const uint16_t*>(half + S::kMeta + lane * 4) : 0u;
                     wait(sh.k_empty[free_at], turn);
+                    // (of a key of zeros, whose scores are zeros, and of one that nobody sees: any number but zero, which -inf is multiplied by)
+                    if constexpr (S::kScaled) sh.scale[slot][row] = scale ? half_bits_to_float(scale) : 1.0f;
+                    if (row == 0) sh.info[slot] = make_int2(t0, pages);
                     codes.put(half, lane, operand, row, seen);
-                    if constexpr (S::kScaled) {
-                        // (of a key of zeros, whose scores are zeros, and of one that nobody sees: any number but zero, which -inf is multiplied by)
-                        const uint32_t bits = seen ? *reinterpret_cast<const uint16_t*>(half + S::kMeta + lane * 4) : 0u;
-                        sh.scale[slot][row] = bits ? half_bits_to_float(bits) : 1.0f;
-                    }
-                    if (row == 0) {
-                        auto whole = [&](int stream) { return pages == 3 && p->first[stream] - t0 >= kChunkTile - 1 && (a.window == 0 || p->last[stream] - t0 < a.window || t0 + kChunkTile <= a.sinks); };
-                        sh.info[slot] = make_int2(t0, pages | (whole(0) ? 4 : 0) | (whole(1) ? 8 : 0));
-                    }
                     fence_proxy_async();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_addr(&sh.k_full[buffer]));
@@ -1045,7 +1045,10 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                     if (keys_done >= (uint32_t)S::kStages) wait(sh.raw_empty[before % S::kRing], before / S::kRing & 1);
                     if (lane == 0 && !wait.lost) {
                         const uint32_t bar = smem_addr(&sh.raw_full[keys_done % S::kRing]), to = smem_addr(raw + stage * S::kRaw);
-                        sh.raw_info[stage] = (at0 >= 0 ? 1u : 0u) | (at1 >= 0 ? 2u : 0u);
+                        // (the streams whose rows see all of the tile)
+                        const int t0 = p->tile(j0 + i) * kChunkTile;
+                        auto whole = [&](int stream) { return at0 >= 0 && at1 >= 0 && p->first[stream] - t0 >= kChunkTile - 1 && (a.window == 0 || p->last[stream] - t0 < a.window || t0 + kChunkTile <= a.sinks); };
+                        sh.raw_info[stage] = (at0 >= 0 ? 1u : 0u) | (at1 >= 0 ? 2u : 0u) | (whole(0) ? 4u : 0u) | (whole(1) ? 8u : 0u);
                         mbar_arrive_expect_tx(bar, ((at0 >= 0) + (at1 >= 0)) * 2u * S::kHalf);
                         if (at0 >= 0) bulk_g2s(to, a.c.pages + ((size_t)at0 * a.c.Hkv + head) * (2 * S::kHalf), 2 * S::kHalf, bar);
                         if (at1 >= 0) bulk_g2s(to + 2 * S::kHalf, a.c.pages + ((size_t)at1 * a.c.Hkv + head) * (2 * S::kHalf), 2 * S::kHalf, bar);
@@ -1180,7 +1183,6 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
     __shared__ float meet[2][256];
     __shared__ float4 sums[kGroups > 1 ? 256 : 1];
     pdl_wait();
-    pdl_launch_dependents();
     const ChunkPiece& p = *chunk_cut(a, blockIdx.x);
     const int tid = threadIdx.x, row0 = blockIdx.y * kRows, first = blockIdx.x;
     if (p.place != 2 || row0 >= p.rows) return;
@@ -1233,6 +1235,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
             *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + p.row(a, row0 + r) * D + c) = make_uint2(chunk_out(o.x * inv, o.y * inv, a.bf16), chunk_out(o.z * inv, o.w * inv, a.bf16));
         }
     }
+    __threadfence();
 }
 
 template <int D, int FMT, bool SPLIT>
@@ -1240,7 +1243,7 @@ cudaError_t launch_chunk(const ChunkArgs& a, int blocks, int rows_most, cudaStre
     static OncePerDevice once;
     if (!allow_shared(chunk_kernel<D, FMT, SPLIT>, ChunkShape<D, FMT>::kBytes, once)) return cudaGetLastError();
     const cudaError_t e = launch_pdl(chunk_kernel<D, FMT, SPLIT>, dim3(blocks), dim3(ChunkForm<D, SPLIT>::kThreads), (size_t)ChunkShape<D, FMT>::kBytes, s, a);
-    if (e != cudaSuccess || a.whole || blocks == 1) return e;
+    if (e != cudaSuccess || !a.merged) return e;
     return launch_pdl(chunk_merge_kernel<D, SPLIT>, dim3(blocks, (rows_most - 1) / chunk_merge_rows<D, SPLIT>() + 1), dim3(256), 0, s, a);
 }
 

@@ -249,3 +249,53 @@ def test_one_token_is_a_decode_step():
             sa.decode_attention(call.cfg, call.cache.handle, call.Qd, O, call.cache.workspace)
         off = call.want()[1] + 1e-5
         assert (np.abs((got - O.double()).cpu().numpy()) <= off).all()
+
+
+def test_a_pool_and_rows_beyond_32_bits():
+    """Pages behind the first 2^32 bytes of a pool, and rows of queries and outputs behind the first 2^32 bytes of theirs."""
+    import torch
+    d, H, n = 128, 8, 90
+    small = Call(sa.SA_KV_FP16, False, d, H, H, [300, 130], [n, 1], seed=20)
+    want = small(window=200, sinks=10)
+    c, page = small.cache, small.cache.layout.page_bytes * H
+    far = (1 << 32) // page + 11
+    pool = torch.zeros((far + c.n_pages) * page, dtype=torch.uint8, device="cuda")
+    pool[far * page:] = c.pages
+    table = (c.page_table + far * (c.page_table >= 0)).int()
+    handle = sa.make_cache(pool, table, c.seq_lens, far + c.n_pages)
+    row0 = (1 << 32) // (2 * d * H) + 3
+    Q, O = (torch.zeros(row0 + n + 1, H, d, dtype=torch.float16, device="cuda") for _ in "qo")
+    Q[row0:] = small.Qd.view(torch.float16)
+    sa.chunk_attention(small.cfg, handle, Q, O, small.workspace, small.cu + row0, 200, 10)
+    torch.cuda.synchronize()
+    assert torch.equal(O[row0:], want) and not O[:row0].any()
+
+
+def test_on_another_stream_behind_the_writes():
+    """A chain on a side stream: cache written, attended to and written again, over and over; every output is that of its own cache."""
+    import torch
+    calls = [Call(sa.SA_POTM2, False, 64, 4, 2, [700, 65], [40, 2], seed=21 + i) for i in range(2)]
+    want = [c() for c in calls]
+    torch.cuda.synchronize()
+    one, stream, got = calls[0], torch.cuda.Stream(), []
+    rows = [(up(c.case.K), up(c.case.V)) for c in calls]
+    with torch.cuda.stream(stream):
+        for i in range(30):
+            sa.fill_kv(one.cfg, one.cache.handle, *rows[i % 2], one.case.cu_lens)
+            got.append(torch.zeros_like(want[0]))
+            sa.chunk_attention(one.cfg, one.cache.handle, calls[i % 2].Qd, got[-1], one.workspace, one.cu)
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i % 2]) for i, g in enumerate(got))
+
+
+@pytest.mark.parametrize("code,dense", [(sa.SA_POTM4, False), (sa.SA_POT4, True), (sa.SA_KV_FP16, False), (sa.SA_KV_FP4, False)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_same_outputs_over_and_over(code, dense, d):
+    """Calls of every kind of row tile, fifty times: bit for bit (a wait that is missing shows here)."""
+    import torch
+    for lens, new in (([5000, 3000, 900], [1, 4, 3]), ([5000, 3000, 900], [8, 5, 8]), ([5000, 3000], [13, 16]), ([3000, 1500], [200, 700])):
+        call = Call(code, dense, d, 8, 2, lens, new, seed=23)
+        first = call()
+        others = [call() for _ in range(50)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(first, o) for o in others)
