@@ -185,8 +185,9 @@ struct ChunkShared {                      // behind the rings
 };
 static_assert(sizeof(ChunkShared) <= 14336, "room behind the rings");
 
-// A wait that ends: where the limit is reached, nothing is waited for any more and the outputs become NaN.  A poll may sleep up to 2 us, so that waiting warps leave
-// their issue slots to the others (without it a tenth of all instructions were polls), and the limit is a third of a second.
+// A wait that ends: where the limit is reached (kWaitLimit polls, each of which may sleep up to 2 us: half a second; LONGER of them where a whole piece is waited for) nothing is
+// waited for any more and the outputs become NaN.  The sleep leaves the waiting warps' issue slots to the others.
+template <uint32_t LONGER = 1>
 struct ChunkWait {
     bool lost = false;
     SA_D static bool poll(uint32_t bar, uint32_t parity) {
@@ -204,22 +205,22 @@ struct ChunkWait {
         if (!over(at, parity) && !lost) {
             lost = true;
 #pragma unroll 1
-            for (uint32_t i = 0; i < kWaitLimit && lost; ++i) lost = !poll(at, parity);
+            for (uint32_t i = 0; i < LONGER * kWaitLimit && lost; ++i) lost = !poll(at, parity);
         }
         __syncwarp();
     }
 };
 
 // The pieces, one after another: next() gives the one at hand (null: no more), leave() hands its place back.  By a whole warp.  (Its waits are its own: warps that have given
-// up on a tile go on from piece to piece, so that all rows of the block come out as NaN.)
+// up on a tile go on from piece to piece, so that all rows of the block that follow come out as NaN.)
 struct ChunkReader {
     ChunkShared& sh;
-    ChunkWait wait{};
+    ChunkWait<32> wait{};
     uint32_t i = 0;
     SA_D const ChunkPiece* next() {
         wait(sh.piece_full[i % kChunkPieces], i / kChunkPieces & 1);
         const ChunkPiece* p = &sh.pieces[i % kChunkPieces];
-        return wait.lost || p->n < 0 ? nullptr : p;
+        return __any_sync(0xffffffffu, wait.lost) || p->n < 0 ? nullptr : p;
     }
     SA_D void leave() {
         __syncwarp();
@@ -673,7 +674,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
     tcgen05_after_sync();
     pdl_wait();
     if (a.merged) pdl_launch_dependents();                             // (else a call behind this one that reads its output early would be too early)
-    ChunkWait wait;
+    ChunkWait<> wait;
     ChunkReader reader{sh};
 
     if (warp < kOperands) {
@@ -887,7 +888,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                     codes.put(half, lane, operand, row, seen);
                     fence_proxy_async();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_addr(&sh.k_full[buffer]));
+                    if (lane == 0 && !wait.lost) mbar_arrive(smem_addr(&sh.k_full[buffer]));
                 }
                 if (values) {
                     const uint32_t operand = v_at + buffer * S::kOperand;
@@ -896,7 +897,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                     codes.put(half, lane, operand, row, seen);
                     fence_proxy_async();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_addr(&sh.v_full[buffer]));
+                    if (lane == 0 && !wait.lost) mbar_arrive(smem_addr(&sh.v_full[buffer]));
                 }
                 if (lane == 0) mbar_arrive(smem_addr(&sh.raw_empty[record]));
             }
@@ -1023,14 +1024,15 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                 }
                 keys_done += n;
             }
-            commit(sh.done);
-            wait(sh.done, 0);
+            ChunkWait<> end;                                           // (products in flight, also where a wait was lost)
+            tcgen05_commit(smem_addr(&sh.done), elected);
+            end(sh.done, 0);
         }
     } else if (warp == kProducts + 1) {
         // ---- loader
         registers_down<Form::kOtherRegs>();
         fence_proxy_async_global();                                    // (the records were written by ordinary stores)
-        uint32_t keys_done = 0;
+        uint32_t keys_done = 0, copied = 0;
         while (const ChunkPiece* p = reader.next()) {
             const int n = p->n, hi = p->hi, head = p->head;
             const int32_t* table = a.c.page_table + (size_t)p->b * a.c.max_pages;
@@ -1054,15 +1056,18 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                         if (at1 >= 0) bulk_g2s(to + 2 * S::kHalf, a.c.pages + ((size_t)at1 * a.c.Hkv + head) * (2 * S::kHalf), 2 * S::kHalf, bar);
                     }
                     __syncwarp();
+                    copied += !wait.lost;
                 }
             }
             reader.leave();
         }
         // copies in flight land before the block ends, also where the operands' warps have given up
-        const uint32_t last = keys_done < (uint32_t)S::kStages ? keys_done : (uint32_t)S::kStages;
+        copied = __shfl_sync(0xffffffffu, copied, 0);
+        const uint32_t last = copied < (uint32_t)S::kStages ? copied : (uint32_t)S::kStages;
         for (uint32_t i = 0; i < last; ++i) {
-            const uint32_t k = keys_done - 1 - i;
-            wait(sh.raw_full[k % S::kRing], k / S::kRing & 1);
+            const uint32_t k = copied - 1 - i;
+            ChunkWait<> landed;
+            landed(sh.raw_full[k % S::kRing], k / S::kRing & 1);
         }
     } else if (warp == kProducts + 2) {
         // ---- the deal: the block's stretch of all units' tiles, piece by piece
@@ -1107,13 +1112,16 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         }
         uint32_t made = 0;
         bool cut = false;
+        ChunkWait<16> free;
+        bool lost = false;                                             // (no place came free: nothing more is dealt)
         auto place = [&]() -> ChunkPiece& {
-            wait(sh.piece_empty[made % kChunkPieces], made / kChunkPieces & 1 ^ 1);
+            free(sh.piece_empty[made % kChunkPieces], made / kChunkPieces & 1 ^ 1);
+            lost = __any_sync(0xffffffffu, free.lost);
             return sh.pieces[made % kChunkPieces];
         };
         auto ready = [&] {
             __syncwarp();
-            if (lane == 0 && !wait.lost) mbar_arrive(smem_addr(&sh.piece_full[made % kChunkPieces]));
+            if (lane == 0) mbar_arrive(smem_addr(&sh.piece_full[made % kChunkPieces]));
             ++made;
         };
         while (at < end_at) {
@@ -1122,6 +1130,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
             const int begin = max(skip - kChunkUnitCost, 0), end = max(to - kChunkUnitCost, 0);
             if (end > begin || (u.count == 0 && skip == 0)) {
                 ChunkPiece& p = place();
+                if (lost) break;
                 if (lane == 0) {
                     const int token = a.by_group(u.row0);
                     p.n = end - begin;
@@ -1156,12 +1165,14 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
             skip = 0;
             if (++flat == n_flat) flat = 0, ++head;
         }
-        ChunkPiece& p = place();
-        if (lane == 0) {
-            p.n = -1;
-            if (!cut) chunk_cut(a, blockIdx.x)->place = 0;
+        if (lane == 0 && !cut) chunk_cut(a, blockIdx.x)->place = 0;
+        if (!lost) {
+            ChunkPiece& p = place();
+            if (!lost) {
+                if (lane == 0) p.n = -1;
+                ready();
+            }
         }
-        ready();
     } else {
         registers_down<Form::kOtherRegs>();
     }
