@@ -125,6 +125,13 @@ struct Args {
         if (o && x == -1 && PyErr_Occurred()) bad = true;
         return (int)x;
     }
+    int integer_32(const char* what) {
+        PyObject* o = bad ? nullptr : next();
+        const long x = o ? PyLong_AsLong(o) : 0;
+        if (o && x == -1 && PyErr_Occurred()) bad = true;
+        if (!bad && x != (int)x) fail(what);
+        return (int)x;
+    }
     // torch's current stream on the current device
     sa_stream stream() {
         if (bad) return nullptr;
@@ -390,7 +397,8 @@ PyObject* chunk_attention(PyObject*, PyObject* const* v, Py_ssize_t n) {
     size_t bytes;
     void* ws = a.tensor_and_bytes(&bytes);
     HostArray cu(a, a.bad || cache->batch < 0 ? 1 : (Py_ssize_t)cache->batch + 1, false, "cu_lens holds at least batch + 1 64-bit integers");
-    const int window = a.integer(), sinks = a.integer();
+    const char* const range = "window and sinks are below 2^31";
+    const int window = a.integer_32(range), sinks = a.integer_32(range);
     const long long dev = a.current_device(), rows = a.bad || cache->batch < 0 ? 0 : cu.p[cache->batch];
     int dtype = SA_F16;
     for (int i = 0; i < 2 && !a.bad; ++i) {

@@ -95,3 +95,11 @@ def test_what_the_binding_takes():
     assert got["good"] == [3] * 6
     assert got["bad"] == ["refused"] * 8
     assert got["append"] == [3] + ["refused"] * 6
+
+
+def test_windows_that_are_no_32_bit_numbers():
+    """2^32 + 5 is not a window of 5, nor 2^32 none at all."""
+    got = outcomes("""(lambda cu: [outcome(lambda: sa.chunk_attention(cfg, cache, Stand(torch.float16, 9, 4, 64), Stand(torch.float16, 9, 4, 64), ws, cu, w, s)) for w, s in (
+        (5, 2), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 0), (2 ** 32, 0), (2 ** 32 + 5, 0), (5, 2 ** 32), (5, -2 ** 32))])(np.array([0, 5, 9]))
+        if [globals().update(ws=type('W', (), dict(nbytes=1 << 30, data_ptr=lambda self: 256))())] else None""")
+    assert got == [3, 3] + ["refused"] * 5
