@@ -155,7 +155,7 @@ struct ChunkShape {
     static constexpr int kBuffers = D == 64 ? 2 : 1;                  // of operands
     static constexpr int kFixed = (2 + 2 * kBuffers) * kOperand + 14336;
     static constexpr int kFit = (227 * 1024 - 1024 - kFixed) / kRaw;
-    static constexpr int kStages = kFit > 4 ? 4 : kFit;
+    static constexpr int kStages = kFit >= 8 ? 8 : kFit >= 6 ? 6 : kFit > 4 ? 4 : kFit;      // (4 to 8: 32 single tokens over 32 768 keys 178 -> 172 us)
     static constexpr int kBytes = 1024 + kFixed + kStages * kRaw;     // (1024: to align)
     static constexpr int kRing = kStages % 2 ? 2 * kStages : kStages;  // barriers of the records: an even number, so that warps which take every other tile see all phases of theirs
     static constexpr int kV = (FMT == FMT_FP16) ? 64 * D : FMT == FMT_FP4 ? 18 * D : kHalf - 32 * D;      // offset of the values in a half
@@ -175,24 +175,24 @@ struct ChunkShared {                      // behind the rings
     float scale[8][kChunkTile];           // of the keys
     float m[256], l[256];                 // SPLIT: of all threads' rows
     float meet[3][512];                   // else: what the two halves of a row tell each other
-    int2 info[8];                         // first key, and raw_info
+    int2 info[8];                         // raw_info
     ChunkPiece pieces[kChunkPieces];
     unsigned long long piece_full[kChunkPieces], piece_empty[kChunkPieces];
-    uint32_t raw_info[4];                 // of a place of records: bits 0, 1: which of the tile's pages there are, 2, 3: streams whose rows see all of the tile
-    unsigned long long raw_full[6], raw_empty[6], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], s_free[2], p_full[2], o_full[2], done;
+    int2 raw_info[8];                     // of a place of records: first key; bits 0, 1: which of the tile's pages there are, 2, 3: streams whose rows see all of the tile, 4: some row sees each key
+    unsigned long long raw_full[8], raw_empty[8], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], s_free[2], p_full[2], o_full[2], done;
     int lens[kChunkBatch];
     uint32_t tmem;
 };
 static_assert(sizeof(ChunkShared) <= 14336, "room behind the rings");
 
-// A wait that ends: where the limit is reached (kWaitLimit polls, each of which may sleep up to 2 us: half a second; LONGER of them where a whole piece is waited for) nothing is
-// waited for any more and the outputs become NaN.  The sleep leaves the waiting warps' issue slots to the others.
+// A wait that ends: where the limit is reached (kWaitLimit polls, which sleep for up to 4 us each: a second; LONGER of them where a whole piece is waited for) nothing is
+// waited for any more and the outputs become NaN.  (With a shorter sleep asked for, each poll is a loop of several instructions: a prompt of 8192 tokens, 4 bits, 547 us, not 531.)
 template <uint32_t LONGER = 1>
 struct ChunkWait {
     bool lost = false;
     SA_D static bool poll(uint32_t bar, uint32_t parity) {
         uint32_t ok;
-        asm volatile("{.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;}" : "=r"(ok) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
+        asm volatile("{.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
         return ok != 0;
     }
     SA_D static bool over(uint32_t bar, uint32_t parity) {                      // (the phase is over already: a look that cannot sleep is the faster one)
@@ -865,17 +865,21 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         const bool keys = !SPLIT || !(warp & 4), values = !SPLIT || (warp & 4);
         uint32_t keys_done = 0;
         while (const ChunkPiece* p = reader.next()) {
-            for (int j = 0; j < p->n; ++j, ++keys_done) {
-                if (SPLIT && (int)(keys_done & 1) != group) continue;
-                const int stage = keys_done % S::kStages, record = keys_done % S::kRing, buffer = keys_done % NB, slot = keys_done & 7;
+            const int n = p->n;
+            for (int j = SPLIT ? (group ^ keys_done) & 1 : 0; j < n; j += SPLIT ? 2 : 1) {
+                const uint32_t now = keys_done + j;
+                const int stage = now % S::kStages, record = now % S::kRing, buffer = now % NB, slot = now & 7;
                 // the operands' places are free once the products of the tile NB ahead are done: announced by turns at two barriers, so that warps which take every other tile have one
-                const uint32_t free_at = keys_done & 1, turn = ((keys_done + 2 - NB) >> 1) - 1 & 1;
-                const int t0 = p->tile(j) * kChunkTile, key = t0 + row;
-                wait(sh.raw_full[record], keys_done / S::kRing & 1);
+                const uint32_t free_at = now & 1, turn = ((now + 2 - NB) >> 1) - 1 & 1;
+                wait(sh.raw_full[record], now / S::kRing & 1);
+                const int2 info = sh.raw_info[stage];
                 const uint8_t* half = raw + stage * S::kRaw + part * S::kHalf;
-                const int pages = (int)sh.raw_info[stage];
                 // what no row sees is zero: it may hold anything, and a weight of zero times that is not zero
-                const bool seen = (pages >> (part >> 1) & 1) && key < p->hi && (key >= p->lo || key < a.sinks);
+                bool seen = info.y >> 4 & 1;
+                if (!seen) {
+                    const int key = info.x + row;
+                    seen = (info.y >> (part >> 1) & 1) && key < p->hi && (key >= p->lo || key < a.sinks);
+                }
                 if (keys) {
                     const uint32_t operand = k_at + buffer * S::kOperand;
                     ChunkCodes<D, FMT, true> codes(half, lane);
@@ -884,7 +888,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                     wait(sh.k_empty[free_at], turn);
                     // (of a key of zeros, whose scores are zeros, and of one that nobody sees: any number but zero, which -inf is multiplied by)
                     if constexpr (S::kScaled) sh.scale[slot][row] = scale ? half_bits_to_float(scale) : 1.0f;
-                    if (row == 0) sh.info[slot] = make_int2(t0, pages);
+                    if (row == 0) sh.info[slot] = info;
                     codes.put(half, lane, operand, row, seen);
                     fence_proxy_async();
                     __syncwarp();
@@ -901,6 +905,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                 }
                 if (lane == 0) mbar_arrive(smem_addr(&sh.raw_empty[record]));
             }
+            keys_done += n;
             reader.leave();
         }
     } else if (warp == kProducts) {
@@ -1036,21 +1041,22 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         while (const ChunkPiece* p = reader.next()) {
             const int n = p->n, hi = p->hi, head = p->head;
             const int32_t* table = a.c.page_table + (size_t)p->b * a.c.max_pages;
-            for (int j0 = 0; j0 < n; j0 += 16) {                       // the pages of 16 tiles, one a lane
-                const int j = j0 + lane / 2, page = p->tile(min(j, n - 1)) * 2 + lane % 2;
+            for (int j0 = 0; j0 < n; j0 += 16) {                       // 16 tiles, two lanes a tile: a page and a stream each
+                const int t0 = p->tile(min(j0 + lane / 2, n - 1)) * kChunkTile, page = t0 / kPageTokens + lane % 2;
                 int at = -1;                                           // (none)
-                if (j < n && page < a.c.max_pages && page * kPageTokens < hi) at = table[page];
+                if (j0 + lane / 2 < n && page < a.c.max_pages && page * kPageTokens < hi) at = table[page];
                 if (at >= a.c.n_pages) at = -1;
+                const uint32_t there = __ballot_sync(0xffffffffu, at >= 0);
+                const bool both = (there >> (lane & 30) & 3) == 3;
+                const uint32_t whole = __ballot_sync(0xffffffffu, both && p->first[lane % 2] - t0 >= kChunkTile - 1 && (a.window == 0 || p->last[lane % 2] - t0 < a.window || t0 + kChunkTile <= a.sinks));
+                const uint32_t seen = __ballot_sync(0xffffffffu, both && hi - t0 >= kChunkTile && (t0 >= p->lo || t0 + kChunkTile <= a.sinks));
                 for (int i = 0; i < 16 && j0 + i < n; ++i, ++keys_done) {
-                    const int at0 = __shfl_sync(0xffffffffu, at, 2 * i), at1 = __shfl_sync(0xffffffffu, at, 2 * i + 1);
+                    const int at0 = __shfl_sync(0xffffffffu, at, 2 * i), at1 = __shfl_sync(0xffffffffu, at, 2 * i + 1), first = __shfl_sync(0xffffffffu, t0, 2 * i);
                     const uint32_t stage = keys_done % S::kStages, before = keys_done - S::kStages;      // (before: the tile whose place this one takes)
                     if (keys_done >= (uint32_t)S::kStages) wait(sh.raw_empty[before % S::kRing], before / S::kRing & 1);
                     if (lane == 0 && !wait.lost) {
                         const uint32_t bar = smem_addr(&sh.raw_full[keys_done % S::kRing]), to = smem_addr(raw + stage * S::kRaw);
-                        // (the streams whose rows see all of the tile)
-                        const int t0 = p->tile(j0 + i) * kChunkTile;
-                        auto whole = [&](int stream) { return at0 >= 0 && at1 >= 0 && p->first[stream] - t0 >= kChunkTile - 1 && (a.window == 0 || p->last[stream] - t0 < a.window || t0 + kChunkTile <= a.sinks); };
-                        sh.raw_info[stage] = (at0 >= 0 ? 1u : 0u) | (at1 >= 0 ? 2u : 0u) | (whole(0) ? 4u : 0u) | (whole(1) ? 8u : 0u);
+                        sh.raw_info[stage] = make_int2(first, (there >> 2 * i & 3) | (whole >> 2 * i & 3) << 2 | (seen >> 2 * i & 1) << 4);
                         mbar_arrive_expect_tx(bar, ((at0 >= 0) + (at1 >= 0)) * 2u * S::kHalf);
                         if (at0 >= 0) bulk_g2s(to, a.c.pages + ((size_t)at0 * a.c.Hkv + head) * (2 * S::kHalf), 2 * S::kHalf, bar);
                         if (at1 >= 0) bulk_g2s(to + 2 * S::kHalf, a.c.pages + ((size_t)at1 * a.c.Hkv + head) * (2 * S::kHalf), 2 * S::kHalf, bar);
@@ -1061,8 +1067,8 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
             }
             reader.leave();
         }
-        // copies in flight land before the block ends, also where the operands' warps have given up
         copied = __shfl_sync(0xffffffffu, copied, 0);
+        // copies in flight land before the block ends, also where the operands' warps have given up
         const uint32_t last = copied < (uint32_t)S::kStages ? copied : (uint32_t)S::kStages;
         for (uint32_t i = 0; i < last; ++i) {
             const uint32_t k = copied - 1 - i;
