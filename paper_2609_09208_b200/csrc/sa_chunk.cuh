@@ -4,13 +4,14 @@
 // window and the first few tokens.  The rows of a product are (token, query head of the KV head's group) pairs, so that a group's heads share a tile of keys.
 //
 // A block (one per SM) walks through pieces: 128 or 256 rows of one (sequence, KV head) and a stretch of tiles of 128 keys.  Its warps:
-//   loader     copies the pages' records as they are into a ring in shared memory (bulk copies);
-//   4 warps    turn the records of a tile into operands, 16 bits a number: a key's code (PoT: bfloat16, INT8, 4 bits, binary16: binary16) without its
-//              scale, which the softmax applies in FP32 to the sums, and values as the binary16 numbers that the codes stand for: both exact, as the
+//   softmax    two streams of products, of 4 warps each (8 at head_dim 64): a row a thread, or half a row's columns;
+//   operands   turn the records of a tile into operands, 16 bits a number: a key's code (PoT: bfloat16, INT8, 4 bits, binary16: binary16) without its
+//              scale, which the softmax applies in FP32 to the scores, and values as the binary16 numbers that the codes stand for: both exact, as the
 //              decode kernels' operands are;
-//   1 thread   issues the products (tcgen05): S = Q K^T into tensor memory, O += P V with the weights P read from there;
-//   2 x 4 warps, a row a thread: the online softmax.  The weights take the place of the scores that they come from.
-// Two streams of products take turns, so that the tensor core works on one while the softmax works on the other: two tiles of 128 rows
+//   products   one warp issues them (tcgen05): S = Q K^T into tensor memory, O += P V with the weights P read from there;
+//   loader     copies the pages' records as they are into a ring in shared memory (bulk copies);
+//   the deal   works out the block's pieces and hands them to the others through a ring, several ahead.
+// The two streams take turns, so that the tensor core works on one while the softmax works on the other: two tiles of 128 rows
 // against the same keys; or, where a sequence has no more than 128 rows (SPLIT), the same rows against every other tile of keys.  Of few rows a tile of
 // 128 is filled up with copies, each for a part of the tile's keys (a thread then has 32 or 64 scores of a tile, not 128); the parts' sums meet at the end.
 //
@@ -19,7 +20,17 @@
 // average and independent from key to key, costs an output no more than its own rounding to binary16 does.
 //
 // Work is dealt on the device, as only that knows the lengths: units (KV head, sequence, row tile) in order, each with its tiles and a fixed cost, are cut into
-// equal stretches, one a block.  A unit that a cut goes through leaves partial sums in the workspace, two places a block, for chunk_merge_kernel.
+// equal stretches, one a block.  A unit that a cut goes through leaves partial sums in the workspace, two places a block, for chunk_merge_kernel.  Where there are no more units
+// than blocks and an equal deal would not be much shorter, a block has a unit and nothing is merged.
+//
+// What bounds it (in a CUDA graph; TFLOP/s of products that are needed):
+//   head_dim 64, many rows: the powers.  256 rows x 128 keys take 2048 cycles of the unit for 2^x and about 3600 in all: it is busy for 63 %, issue slots for 62 %, the tensor core for 30 %.
+//     2048 tokens over 32 768 PoT-M4 keys, 32 / 4 heads: 800 us, 663 TFLOP/s (585 with the powers left out, 528 with the codes' conversion left out as well).
+//   head_dim 128, many rows: products (2050 cycles a tile at the rate of a library's) and powers (2048) beside one another.  8192 tokens, 32 / 8 heads, 4 bits: 518 us,
+//     1060 TFLOP/s, 65 % of that rate; 4096 tokens over binary16 keys 169 us.
+//   few rows (SPLIT): the way of a tile through the warps, each of which waits for the one before: 1400 cycles a tile, where 730 are what memory needs, and all but 200 of them
+//     stay when powers and conversion are left out.  32 single tokens over 32 768 PoT-M4 keys: 169 us, 3.3 TB/s.
+//   one short call: what it takes to get going, 7 us: lengths, deal, page table, records, operands, one product after another, outputs.
 #pragma once
 #include <cuda_bf16.h>
 #include <type_traits>
@@ -48,7 +59,7 @@ struct ChunkSeqs {
     int64_t row0[kChunkBatch];
     int tiles[kChunkBatch + 1];           // row tiles ahead of it
 };
-// x / d for 0 <= x < 2^31 by a product (Granlund and Montgomery): mul = floor(2^(31 + s) / d) + 1 with 2^s >= d is off by at most d / d 2^-s, too little to matter.
+// x / d for 0 <= x < 2^31 by a product (Granlund and Montgomery): with 2^s >= d, mul = floor(2^(31 + s) / d) + 1 is above the quotient by at most 1, the product by less than 1 / d.
 struct ChunkDivisor {
     uint32_t mul;
     int shift;
@@ -678,7 +689,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
     ChunkReader reader{sh};
 
     if (warp < kOperands) {
-        // ---- softmax: a row a thread (SPLIT), or half a row
+        // ---- softmax: a row a thread, or half a row's columns
         const int stream = warp / (4 * kHalves), part = warp / 4 % kHalves, quarter = warp & 3, own = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_col = lanes + stream * 128, p_col = lanes + S::weights(stream), o_col = lanes + S::sums(stream);
         const uint32_t q_operand = q_at + stream * S::kOperand;
@@ -858,7 +869,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         }
         if (!a.merged) __threadfence();                                // as sa_rotate_qkv's kernel: a decode call behind this one reads its queries before it waits
     } else if (warp < kProducts) {
-        // ---- operands: a key a thread
+        // ---- operands: a key a thread (SPLIT: its key or its value, of every other tile)
         registers_down<Form::kOperandRegs>();
         const int part = warp & 3, row = part * 32 + lane;             // half page of the tile
         const int group = (warp - kOperands) >> 3;                     // SPLIT: which tiles
