@@ -37,9 +37,8 @@ extern "C" sa_status sa_append_qkv(const sa_config* cfg, const sa_cache* cache, 
         longest = T > longest ? T : longest;
     }
     if (cu_lens_host[a.c.batch] > n) return SA_ERR_INVALID_ARG;                // (rows that are not there)
-    constexpr int kRowsMost = 200 * 1024;                                      // bytes of keys and values that wait in shared memory
     const int tokens_most = p.d == 64 ? 4 : 2;
-    if ((int64_t)tokens_most * 4 * p.Hkv * p.d > kRowsMost) return SA_ERR_UNSUPPORTED;
+    if ((int64_t)tokens_most * 4 * p.Hkv * p.d > kAppendRowsMost) return SA_ERR_UNSUPPORTED;
     if (total == 0) return SA_OK;
     a.form = p.fp16 ? APPEND_FP16 : p.fp4 ? APPEND_FP4 : p.int8 ? APPEND_INT8 : p.nibble ? APPEND_DENSE : APPEND_BYTE;
     // As sa_rotate_qkv, a token a block while a wave of blocks holds them; but two tokens whose 4-bit values share bytes have to be in one.
@@ -59,8 +58,10 @@ extern "C" sa_status sa_append_qkv(const sa_config* cfg, const sa_cache* cache, 
         }
         if (a.s.blocks[a.s.n] == 0) continue;
         const cudaError_t e = rot->dtype == SA_F16 ? launch_append_typed<__half>(a, p.d, tokens, s) : rot->dtype == SA_BF16 ? launch_append_bf16(a, p.d, tokens, s) : launch_append_f32(a, p.d, tokens, s);
-        if (e != cudaSuccess) return SA_ERR_CUDA;
-        if (bump_lens && several && launch_pdl(append_lengths_kernel, dim3((unsigned)a.s.n), dim3(32), 0, s, a.c, a.s) != cudaSuccess) return SA_ERR_CUDA;
+        if (e != cudaSuccess || (bump_lens && several && launch_pdl(append_lengths_kernel, dim3((unsigned)a.s.n), dim3(32), 0, s, a.c, a.s) != cudaSuccess)) {
+            cudaGetLastError();                                                // (not the next call's)
+            return SA_ERR_CUDA;
+        }
     }
     return cudaGetLastError() == cudaSuccess ? SA_OK : SA_ERR_CUDA;
 }

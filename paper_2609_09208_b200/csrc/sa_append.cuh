@@ -17,6 +17,7 @@
 namespace sa {
 
 constexpr int kAppendBatch = 64;          // sequences per launch
+constexpr int kAppendRowsMost = 200 * 1024;      // bytes of keys and values that wait in shared memory
 struct AppendSeqs {
     int64_t row0[kAppendBatch];           // first row of the sequence's new tokens
     int tokens[kAppendBatch];
@@ -249,13 +250,14 @@ cudaError_t launch_append(const AppendArgs& a, int tokens, cudaStream_t s) {
     constexpr int kTokens = D == 64 ? 4 : 2;
     const int rows = (int)sizeof(uint16_t) * 2 * a.c.Hkv * D;
     const unsigned grid = (unsigned)a.s.blocks[a.s.n];
+    // The most that any call needs, not this one's rows: it is asked for once, and the kernel's sines and cosines count against the 48 KB that need no asking.
     if (tokens == 1) {
         static OncePerDevice once;
-        if (!allow_shared(append_qkv_kernel<D, T, P, 1, NEIGHBOURS>, rows, once)) return cudaGetLastError();
+        if (!allow_shared(append_qkv_kernel<D, T, P, 1, NEIGHBOURS>, kAppendRowsMost, once)) return cudaGetLastError();
         return launch_pdl(append_qkv_kernel<D, T, P, 1, NEIGHBOURS>, dim3(grid), dim3(rotate_threads(1)), (size_t)rows, s, a);
     }
     static OncePerDevice once;
-    if (!allow_shared(append_qkv_kernel<D, T, P, kTokens, NEIGHBOURS>, kTokens * rows, once)) return cudaGetLastError();
+    if (!allow_shared(append_qkv_kernel<D, T, P, kTokens, NEIGHBOURS>, kAppendRowsMost, once)) return cudaGetLastError();
     return launch_pdl(append_qkv_kernel<D, T, P, kTokens, NEIGHBOURS>, dim3(grid), dim3(rotate_threads(kTokens)), (size_t)kTokens * rows, s, a);
 }
 template <int D, typename T>

@@ -120,6 +120,18 @@ def test_many_heads():
             c.check()
 
 
+@pytest.mark.parametrize("d,new,heads", [(64, [6, 3], (40, 47, 48, 60, 100, 200)), (64, [1, 1], (100, 191, 192, 193, 200)), (128, [6, 3], (47, 48, 64, 96, 200)), (128, [1, 1], (95, 96, 97, 130, 200))])
+def test_more_heads_from_call_to_call(d, new, heads):
+    """Keys and values around the 48 KB of shared memory that a block has without asking, up to the most, each count above the last: FP32 and neighbouring pairs, a kernel that no other
+    test gives as many heads."""
+    import torch
+    for H in heads:
+        cfg = sa.make_config(d, H, H, sa.SA_KV_FP4)
+        c = Calls(cfg, rotary(cfg, torch.float32, pairs="neighbours"), torch.float32, [5, 66], new, seed=H)
+        c.append()
+        c.check()
+
+
 @pytest.mark.parametrize("code", [sa.SA_KV_FP4, sa.SA_POTM2])
 def test_pages_that_are_not_mapped(code):
     """A sequence of which one page is missing is left as it is, its queries are not; the others get their tokens."""
