@@ -436,6 +436,8 @@ SA_D float chunk_queries(const ChunkArgs& a, uint32_t operand, int lane, int fir
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {
         if (a.c.hadamard && any[i]) f.rotate(x[i]);
+        // A query with an infinity or a NaN is a NaN in the operand, and scores are NaN where a key is seen and nowhere else: in the factor it would be in hidden keys' weights too, and
+        // an infinity can make all scores minus infinity, which reads as nothing seen.
         if (S::kScaled && any[i]) {                                                     // as quantise_query_vec: 127 steps of the largest magnitude
             uint32_t top = x[i][0] & 0x7fff7fffu;
 #pragma unroll
@@ -456,8 +458,13 @@ SA_D float chunk_queries(const ChunkArgs& a, uint32_t operand, int lane, int fir
                     x[i][e] = *reinterpret_cast<const uint32_t*>(&h);
                 }
             }
-            const float d = __shfl_sync(0xffffffffu, top ? delta : 1.0f, (lane % RPW) * LPV);      // (a query of zeros: any factor but zero)
+            const bool number = top < 0x7c00u;
+            if (!number) x[i][0] = 0x7fff7fffu;
+            const float d = __shfl_sync(0xffffffffu, top && number ? delta : 1.0f, (lane % RPW) * LPV);      // (a query of zeros: any factor but zero)
             if (lane / RPW == half * STEPS + i) mine = d * a.factor;
+        } else if (any[i]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[i][0] = fma_half2(x[i][e], 0u, x[i][0]);      // (times zero)
         }
         const int row = first_row + row0 + i * RPW + lane / LPV;
         put_operand(operand, row, 2 * f.blk, x[i][0], x[i][1], x[i][2], x[i][3]);

@@ -299,3 +299,30 @@ def test_the_same_outputs_over_and_over(code, dense, d):
         others = [call() for _ in range(50)]
         torch.cuda.synchronize()
         assert all(torch.equal(first, o) for o in others)
+
+
+@pytest.mark.parametrize("d,Hq,Hkv", [(64, 8, 2), (128, 6, 2)])
+@pytest.mark.parametrize("code", [sa.SA_POTM4, sa.SA_POT4, sa.SA_INT8, sa.SA_KV_FP4, sa.SA_KV_FP16])
+@pytest.mark.parametrize("new", [(5, 5), (90, 90), (9, 300)])
+def test_queries_that_are_no_numbers(code, d, Hq, Hkv, new):
+    """A query with an infinity or a NaN yields NaN, also where all its scores are minus infinity; zeros where it sees no token; and no other row changes."""
+    import torch
+    call = Call(code, False, d, Hq, Hkv, [310, 305], new, seed=24)
+    K = call.case.K
+    K[..., 3] = np.abs(K[..., 3]) + np.float16(0.5)            # a channel that no key has negative or zero
+    call.cache.fill(up(K), up(call.case.V), call.case.cu_lens)
+    call.cache.seq_lens[0] = new[0] - 3                        # its first three queries see nothing, the fourth one token
+    clean = call()
+    rng = np.random.default_rng(3)
+    bad = np.zeros(call.Q.shape[:2], bool)
+    for row in (0, 1, 2, 3, 4, new[0] - 1, new[0], new[0] + 1, new[0] + 3, len(call.Q) - 1):
+        for h, x in zip(rng.permutation(Hq)[:3], (np.nan, np.inf, -np.inf)):
+            call.Q[row, h, 3] = x
+            bad[row, h] = True
+    got = call()
+    torch.cuda.synchronize()
+    bad = torch.from_numpy(bad).cuda()
+    nothing = torch.zeros_like(bad)
+    nothing[:3] = True
+    assert torch.equal(got[~bad], clean[~bad]) and not got[nothing].any() and not clean[nothing].any()
+    assert got[bad & ~nothing].isnan().all()
