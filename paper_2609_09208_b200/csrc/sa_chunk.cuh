@@ -483,6 +483,22 @@ SA_D uint32_t chunk_out(float a, float b, int bf16) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// Outputs are means of numbers that binary16 has, but the weights are rounded and the sum that they are divided by is not: a mean of values of the largest magnitude, 65504, may come out
+// as up to 2^-11 more, which rounds to infinity.  So sums whose output would be 65520 or more, and are no infinities, are cut down to 65504 times the row's sum of weights.
+constexpr float kChunkRoundsUp = 65520.0f;
+SA_D float chunk_cut_down(float x, float l) { return fabsf(x) < INFINITY ? fminf(fmaxf(x, -65504.0f * l), 65504.0f * l) : x; }
+SA_D float max3_abs(float a, float b, float c) {
+    float d;
+    asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Four outputs: sums of a row whose weights' sum is l.
+SA_D uint2 chunk_out4(float4 v, float l, int bf16) {
+    const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == 0.0f ? 0.0f : l;
+    if (!bf16 && max3_abs(max3_abs(v.x, v.y, v.z), v.w, 0.0f) * inv >= kChunkRoundsUp)
+        v = make_float4(chunk_cut_down(v.x, l), chunk_cut_down(v.y, l), chunk_cut_down(v.z, l), chunk_cut_down(v.w, l));
+    return make_uint2(chunk_out(v.x * inv, v.y * inv, bf16), chunk_out(v.z * inv, v.w * inv, bf16));
+}
 SA_D uint32_t bits_below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 SA_D void chunk_sync(int barrier, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory"); }
 
@@ -803,6 +819,14 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) *reinterpret_cast<uint4*>(slot + (size_t)row * D + c + e) = make_uint4(x[e], x[e + 1], x[e + 2], x[e + 3]);
                     } else if (there) {
+                        if (FMT != FMT_FP4 && !a.bf16) {               // (4 bits: 61440 at most)
+                            float top = 0.0f;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2) top = max3_abs(top, __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                            if (top * inv >= kChunkRoundsUp)
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(chunk_cut_down(__uint_as_float(x[e]), l));
+                        }
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) {
                             uint32_t w[4];
@@ -862,8 +886,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                             *reinterpret_cast<float4*>(slot + (size_t)at * D + c0 + c) = v;
                             if (c0 + c == 0) slot[kPerTile * (D + 1) + at] = all;
                         } else {
-                            const float inv = all > 0.0f ? __fdiv_rn(1.0f, all) : all == 0.0f ? 0.0f : all;
-                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + p->row(a, at) * D + c0 + c) = make_uint2(chunk_out(v.x * inv, v.y * inv, a.bf16), chunk_out(v.z * inv, v.w * inv, a.bf16));
+                            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + p->row(a, at) * D + c0 + c) = chunk_out4(v, all, a.bf16);
                         }
                     }
                     if (slot && c0 == 0 && tid < rows) slot[kPerTile * D + tid] = most;      // (threads 0 .. rows - 1 are the first copies of their rows)
@@ -1266,10 +1289,7 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
                     o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
                 }
         }
-        if (there && group == 0) {
-            const float inv = all > 0.0f ? __fdiv_rn(1.0f, all) : all == 0.0f ? 0.0f : all;
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + p.row(a, row0 + r) * D + c) = make_uint2(chunk_out(o.x * inv, o.y * inv, a.bf16), chunk_out(o.z * inv, o.w * inv, a.bf16));
-        }
+        if (there && group == 0) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.O) + p.row(a, row0 + r) * D + c) = chunk_out4(o, all, a.bf16);
     }
     __threadfence();
 }

@@ -326,3 +326,31 @@ def test_queries_that_are_no_numbers(code, d, Hq, Hkv, new):
     nothing[:3] = True
     assert torch.equal(got[~bad], clean[~bad]) and not got[nothing].any() and not clean[nothing].any()
     assert got[bad & ~nothing].isnan().all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,n", [(257, 1), (257, 100), (3000, 200), (20000, 2)])
+def test_values_of_the_largest_magnitude(d, T, n):
+    """Equal values of the largest magnitude: their mean is that number, however the weights have been rounded, and no infinity.  (All keys but the first weigh a bit more than half a
+    step of binary16 above a power of two, which the rounding takes up by 2^-11.)"""
+    import torch
+    call = Call(sa.SA_KV_FP16, False, d, 4, 2, [T], [n], seed=25)
+    # q k / sqrt(d) log2(e) = -1 + log2(1 + 2^-11 + a little)
+    want = (np.log2(1 + 2.0 ** -11 * 1.03) - 1) * d ** 0.5 / np.log2(np.e)
+    q = np.linspace(1, 2, 1024, endpoint=False).astype(np.float16)
+    k = (want / q.astype(np.float64)).astype(np.float16)
+    best = np.abs(q.astype(np.float64) * k.astype(np.float64) - want).argmin()
+    call.Q[:] = 0
+    call.Q[..., 0] = q[best]
+    c = call.case
+    c.K[:] = 0
+    c.K[1:, :, 0] = k[best]
+    c.V[:] = 65504
+    c.V[..., ::2] = -65504
+    call.cache.fill(up(c.K), up(c.V), c.cu_lens)
+    for dtype in (torch.float16, torch.bfloat16):
+        got = call(dtype=dtype).double()
+        torch.cuda.synchronize()
+        # (weights off by 2^-11 at most, then the output's rounding)
+        assert ((got.abs() - 65504).abs() <= 65504 * (2.0 ** -11 + (0 if dtype == torch.float16 else 2.0 ** -8 * 1.01))).all(), (got.abs().max(), got.abs().min())
+        assert (got[..., ::2] < 0).all() and (got[..., 1::2] > 0).all()
