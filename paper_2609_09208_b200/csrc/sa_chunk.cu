@@ -27,11 +27,12 @@ static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool spl
     if (most == 0) return true;
     a.copies = !split || most > 64 ? 1 : most > 32 ? 2 : 4;
     const int per_tile = chunk_rows(split) / a.copies;
-    const int64_t tiles_most = ((int64_t)a.c.max_pages + 1) / 2;
+    const int64_t tiles_most = ((int64_t)a.c.max_pages + 1) / 2, blocks_most = chunk_blocks_most();
     for (int b = 0; b < a.c.batch;) {
         a.s.n = 0;
         a.s.tiles[0] = 0;
         int64_t work = 0, longest = 0;                                          // key tiles, by what the cache has room for
+        int64_t least = 0, reach = 0;                                           // ... where it holds the new tokens only; the most that a unit has beyond what its sequence then adds to a block's share
         for (; b < a.c.batch && a.s.n < kChunkBatch; ++b) {
             const int64_t n = cu[b + 1] - cu[b], rows = n * p.G;
             if (n == 0 || (rows <= chunk_rows(true)) != split) continue;
@@ -46,11 +47,18 @@ static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool spl
             const int64_t keys = window < tiles_most ? window : tiles_most;
             work += (int64_t)tiles * (kChunkUnitCost + keys);
             longest = keys > longest ? keys : longest;
+            const int64_t own = (n - 1) / kChunkTile + 1, last = own < keys ? own : keys, beyond = keys * blocks_most - tiles * (keys - last) * p.Hkv;
+            least += tiles * kChunkUnitCost + tiles * (1 + last) / 2;           // (causal: from one tile to `last`)
+            reach = beyond > reach ? beyond : reach;
         }
         if (a.s.n == 0) break;
-        // A unit a block, none of them cut, where the longest is about as long as an equal share of all: putting parts together costs 5 us, 6 tiles.
-        const int64_t units = (int64_t)a.s.tiles[a.s.n] * p.Hkv, blocks_most = chunk_blocks_most();
-        a.whole = units <= blocks_most && longest * (blocks_most - units) <= 6 * blocks_most;
+        // A unit a block, none of them cut, where that is as good.  Only the device knows the lengths and can decide on that, for which it needs the second launch, that of the merge, which
+        // costs 2.5 us even where nothing is cut.  So not where the longest unit cannot be much longer than an equal share whatever the lengths are (worst: one sequence fills
+        // the cache, the others hold their new tokens only; 2.5 tiles more than what cutting costs: a prompt of 2048 tokens, 16 / 2 heads of 128, binary16, 44.3 us whole, 46.4 cut); nor for few rows where that holds for equal lengths and units are short, as windows make them: 32 single tokens with a
+        // window of 4096 32.9 us, 35.4 with the second launch, for which one sequence at its window beside 36 of 300 tokens takes 32.2, which 22.1 would do.
+        const int64_t units = (int64_t)a.s.tiles[a.s.n] * p.Hkv, bound = (2 * (chunk_cut_cost(p.d, split) - kChunkUnitCost) + 5) * blocks_most / 2;
+        const bool worst = reach - least * p.Hkv <= bound, equal = longest * blocks_most - work * p.Hkv <= bound;
+        a.whole = units <= blocks_most && (worst || (split && equal && longest <= (p.d == 64 ? 40 : 20)));
         const int blocks = (int)(a.whole ? units : work * p.Hkv < blocks_most ? work * p.Hkv : blocks_most);
         a.merged = !a.whole && blocks > 1;
         const bool pot = !p.fp16 && !p.fp4 && !p.int8;

@@ -21,7 +21,7 @@
 //
 // Work is dealt on the device, as only that knows the lengths: units (KV head, sequence, row tile) in order, each with its tiles and a fixed cost, are cut into
 // equal stretches, one a block.  A unit that a cut goes through leaves partial sums in the workspace, two places a block, for chunk_merge_kernel.  Where there are no more units
-// than blocks and an equal deal would not be much shorter, a block has a unit and nothing is merged.
+// than blocks and the longest is not much more than an equal stretch, a block has a unit and none is cut.
 //
 // What bounds it (in a CUDA graph; TFLOP/s of products that are needed):
 //   head_dim 64, many rows: the powers.  256 rows x 128 keys take 2048 cycles of the unit for 2^x and about 3600 in all: it is busy for 63 %, issue slots for 62 %, the tensor core for 30 %.
@@ -47,6 +47,10 @@ namespace sa {
 constexpr int kChunkBatch = 128;          // sequences per launch
 constexpr int kChunkTile = 128;           // keys
 constexpr int kChunkUnitCost = 4;         // what a unit costs beside its tiles, in tiles
+// What cutting units costs, in tiles, beside a kernel of a unit a block: a second start in most blocks, partial sums, putting them together.  (As many tiles as the longest unit has more than
+// an equal stretch where both take equally long, 4 to 136 equal units and causal ones: few rows at head_dim 64 8 to 10 tiles, 8 sequences of 1024 tokens 15.9 us cut, 15.6 whole, of 2048 17.6
+// and 21.3; the others 7 to 8, 1024 new tokens of 16 / 2 heads of 128 34.6 and 36.9, 512 27.9 and 26.4.)
+SA_HD constexpr int chunk_cut_cost(int d, bool split) { return split && d == 64 ? 9 : 7; }
 constexpr int kChunkBlocksMost = 1024;
 constexpr int kChunkCutBytes = kChunkBlocksMost * 96;      // of the workspace, ahead of the partial sums: the piece of every block that the cut behind it goes through
 SA_HD constexpr int chunk_rows(bool split) { return split ? 128 : 256; }
@@ -78,7 +82,7 @@ struct ChunkArgs {
     uint8_t* workspace;
     int Hq, G, window, sinks;             // G: query heads of a group
     int copies;                           // SPLIT: 1, 2 or 4 copies of the rows in a tile
-    int whole, merged;                    // a unit a block: none is cut; chunk_merge_kernel follows
+    int whole, merged;                    // a unit a block, whatever the lengths: none is cut; else the deal decides: chunk_merge_kernel follows
     int bf16;                             // type of O
     float factor;                         // log2(e) / sqrt(d) and the unit of the operands
     ChunkSeqs s;
@@ -1125,13 +1129,17 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         const int n_flat = a.s.tiles[a.s.n];
         int head, flat, skip = 0;                                      // the unit, and how far into it (its fixed cost included) the stretch starts
         uint64_t at = 0, end_at = 1, per = 1;                          // the stretch; the length of one
-        if (a.whole) {
-            head = blockIdx.x / n_flat;
-            flat = blockIdx.x % n_flat;
-        } else {
+        bool whole = a.whole;
+        if (!whole) {
             const int each = (n_flat + 31) / 32, mine0 = min(lane * each, n_flat), mine1 = min(mine0 + each, n_flat);
             uint64_t cost = 0;
-            for (int i = mine0; i < mine1; ++i) cost += kChunkUnitCost + chunk_unit(a, sh.lens, i, per_tile).count;
+            uint32_t longest = 0;
+            for (int i = mine0; i < mine1; ++i) {
+                const uint32_t c = kChunkUnitCost + chunk_unit(a, sh.lens, i, per_tile).count;
+                cost += c;
+                longest = max(longest, c);
+            }
+            longest = __reduce_max_sync(0xffffffffu, longest);
             uint64_t ahead = cost;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -1142,6 +1150,8 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
             ahead -= cost;
             // equal stretches but for the last; 32-bit divisions where the numbers allow (64-bit ones are long routines)
             per = total >> 32 == 0 ? ((uint32_t)total - 1) / gridDim.x + 1 : (total - 1) / gridDim.x + 1;
+            // A unit a block where the longest costs no more than an equal stretch and what cutting costs.
+            whole = (uint64_t)n_flat * a.c.Hkv <= gridDim.x && longest <= per + chunk_cut_cost(D, SPLIT);
             at = min(per * blockIdx.x, total);
             end_at = min(at + per, total);
             head = (int)(total >> 32 == 0 ? (uint32_t)at / (uint32_t)sum : at / sum);
@@ -1157,6 +1167,12 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
             const int from = owner ? __ffs(owner) - 1 : 0;
             flat = __shfl_sync(0xffffffffu, i, from);
             skip = (int)__shfl_sync(0xffffffffu, (uint32_t)rest, from);
+        }
+        if (whole) {
+            head = blockIdx.x / n_flat;
+            flat = blockIdx.x % n_flat;
+            at = skip = 0;
+            end_at = head < a.c.Hkv;
         }
         uint32_t made = 0;
         bool cut = false;
@@ -1174,7 +1190,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         };
         while (at < end_at) {
             const ChunkUnit u = chunk_unit(a, sh.lens, flat, per_tile);
-            const int cost = kChunkUnitCost + u.count, to = a.whole || end_at - at >= (uint64_t)(cost - skip) ? cost : skip + (int)(end_at - at);
+            const int cost = kChunkUnitCost + u.count, to = whole || end_at - at >= (uint64_t)(cost - skip) ? cost : skip + (int)(end_at - at);
             const int begin = max(skip - kChunkUnitCost, 0), end = max(to - kChunkUnitCost, 0);
             if (end > begin || (u.count == 0 && skip == 0)) {
                 ChunkPiece& p = place();
@@ -1209,7 +1225,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                 }
                 ready();
             }
-            at += a.whole ? 1 : to - skip;
+            at += whole ? 1 : to - skip;
             skip = 0;
             if (++flat == n_flat) flat = 0, ++head;
         }

@@ -354,3 +354,56 @@ def test_values_of_the_largest_magnitude(d, T, n):
         # (weights off by 2^-11 at most, then the output's rounding)
         assert ((got.abs() - 65504).abs() <= 65504 * (2.0 ** -11 + (0 if dtype == torch.float16 else 2.0 ** -8 * 1.01))).all(), (got.abs().max(), got.abs().min())
         assert (got[..., ::2] < 0).all() and (got[..., 1::2] > 0).all()
+
+
+@pytest.mark.parametrize("d,code,new", [(64, sa.SA_POTM4, 1), (128, sa.SA_KV_FP4, 3), (64, sa.SA_INT8, 60), (128, sa.SA_KV_FP16, 40)])
+@pytest.mark.parametrize("batch", [36, 37])
+def test_about_as_many_units_as_blocks(d, code, new, batch):
+    """144 and 148 units, equal and ragged: a unit a block, or cut ones; a captured call decides by the lengths that it finds."""
+    import torch
+    rng = np.random.default_rng(batch)
+    lens = rng.integers(new, 300, batch)
+    lens[5] = 6000
+    call = Call(code, False, d, 16, 4, lens, [new] * batch, seed=26)
+    check(call)
+    check(call, window=100, sinks=7)
+    ragged, equal = call(), torch.full((batch,), int(min(lens)), dtype=torch.int32, device="cuda")
+    lengths = call.cache.seq_lens.clone()
+    call.cache.seq_lens.copy_(equal)
+    short, O, Q = call(), torch.zeros_like(ragged), call.Qd
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sa.chunk_attention(call.cfg, call.cache.handle, Q, O, call.workspace, call.cu)
+    for now, want in ((equal, short), (lengths, ragged), (equal, short)):
+        call.cache.seq_lens.copy_(now)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(O, want)
+    del graph
+
+
+def test_one_long_sequence_beside_short_ones():
+    """148 units of which 4 have 256 tiles of keys and the others one: about as long as the long sequence by itself and the others by themselves, not a block's walk through 256 tiles."""
+    import torch
+
+    def time(lens):
+        call = Call(sa.SA_POTM4, False, 64, 32, 4, lens, [1] * len(lens), seed=27)
+        O = call()
+        go = lambda: sa.chunk_attention(call.cfg, call.cache.handle, call.Qd, O, call.workspace, call.cu)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for _ in range(20):
+                go()
+        start, end = (torch.cuda.Event(enable_timing=True) for _ in "se")
+        best = np.inf
+        for _ in range(10):
+            start.record()
+            graph.replay()
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end))
+        del graph
+        return best
+
+    both, long, short = time([32768] + [100] * 36), time([32768]), time([100] * 36)
+    assert both <= 2 * (long + short), (both, long, short)      # (5 times as long where nothing is cut)
