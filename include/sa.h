@@ -418,6 +418,13 @@ sa_status sa_debug_decode_lost_copy(const sa_config* cfg, const sa_cache* cache,
                                     void* workspace, size_t workspace_bytes, int b, int kv_head, int tile,
                                     sa_stream stream);
 
+/* The same of sa_chunk_attention (no window, binary16 outputs): the copy of the 128-token tile `tile` of sequence `b`, KV head `kv_head`, is never issued, and waits give up after
+ * a few milliseconds instead of a second.  The rows that need the tile come out as NaN, and with them the rows that the blocks which gave up would have worked on
+ * after them; every other row is the ordinary result.  tile < 0: the blocks stop handing out work after the first -1 - tile pieces each, whose rows are the ordinary result or, where
+ * other parts of theirs are missing, NaN; all other rows are NaN.  The call returns like any other.  Only head_dim 64, SA_POTM4 in the byte container: else SA_ERR_UNSUPPORTED. */
+sa_status sa_debug_chunk_lost_copy(const sa_config* cfg, const sa_cache* cache, const uint16_t* Q, const int64_t* cu_lens_host, void* O, void* workspace,
+                                   size_t workspace_bytes, int b, int kv_head, int tile, sa_stream stream);
+
 /* Instruction-throughput micro-benchmark (measurement aid; the paper has no counterpart — it stands
  * in for the paper's disassembly-based operation counts, section III and Table V).  Launches `blocks`
  * blocks of 256 threads in which every thread runs iters * 64 instructions of one kind on 8

@@ -33,7 +33,7 @@ EXPORTS = [
     "sa_decode_attention_fp16", "sa_decode_attention_stages", "sa_decode_attention_fp16_stages", "sa_debug_unpack", "sa_staging_bytes", "sa_decode_step_host",
     "sa_decode_attention_static", "sa_pipe_microbench", "sa_shiftav_workspace_bytes", "sa_decode_attention_shiftav",
     "sa_decode_step", "sa_debug_decode_lost_copy", "sa_read_kv", "sa_rotate_qkv",
-    "sa_append_qkv", "sa_chunk_workspace_bytes", "sa_chunk_attention",
+    "sa_append_qkv", "sa_chunk_workspace_bytes", "sa_chunk_attention", "sa_debug_chunk_lost_copy",
 ]
 
 
@@ -328,6 +328,13 @@ def debug_decode_lost_copy(cfg, cache: SaCache, Q, O, workspace, b: int, kv_head
     _check(lib().sa_debug_decode_lost_copy(C.byref(cfg), C.byref(cache), _ptr(Q), _ptr(O), _ptr(workspace),
                                            C.c_size_t(workspace.numel() * workspace.element_size()), C.c_int(b),
                                            C.c_int(kv_head), C.c_int(tile), _stream()), "sa_debug_decode_lost_copy")
+
+
+def debug_chunk_lost_copy(cfg, cache: SaCache, Q, O, workspace, cu_lens_host, b: int, kv_head: int, tile: int):
+    """Test hook: chunk_attention in which the copy of one 128-token tile is never issued, or (tile < 0) the blocks stop handing out work after -1 - tile pieces."""
+    _check(lib().sa_debug_chunk_lost_copy(C.byref(cfg), C.byref(cache), _ptr(Q), cu_lens_host.ctypes.data_as(C.POINTER(C.c_int64)), _ptr(O), _ptr(workspace),
+                                          C.c_size_t(workspace.numel() * workspace.element_size()), C.c_int(b), C.c_int(kv_head), C.c_int(tile), _stream()),
+           "sa_debug_chunk_lost_copy")
 
 
 def debug_unpack(cfg, cache: SaCache, b: int, n_tokens: int, codes=None, scales=None, v_hat=None, g=None):

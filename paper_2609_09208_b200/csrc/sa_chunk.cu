@@ -17,7 +17,7 @@ static int chunk_format(const Plan& p) {
 }
 
 // The sequences of one kind (SPLIT: of at most 128 rows; or the others), kChunkBatch a launch.
-static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool split, cudaStream_t s) {
+static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool split, bool lost, cudaStream_t s) {
     const int fmt = chunk_format(p);
     int64_t most = 0;
     for (int b = 0; b < a.c.batch; ++b) {
@@ -63,36 +63,28 @@ static bool launch_kind(const Plan& p, ChunkArgs& a, const int64_t* cu, bool spl
         a.merged = !a.whole && blocks > 1;
         const bool pot = !p.fp16 && !p.fp4 && !p.int8;
         const int rows_most = (int)(most < per_tile ? most : per_tile);
-        if ((pot ? launch_chunk_pot(p.d, fmt, split, a, blocks, rows_most, s) : launch_chunk_plain(p.d, fmt, split, a, blocks, rows_most, s)) != cudaSuccess) return false;
+        const cudaError_t e = lost ? launch_chunk_lost(split, a, blocks, rows_most, s)
+                              : pot ? launch_chunk_pot(p.d, fmt, split, a, blocks, rows_most, s) : launch_chunk_plain(p.d, fmt, split, a, blocks, rows_most, s);
+        if (e != cudaSuccess) return false;
     }
     return true;
 }
 
-}  // namespace sa
-
-using namespace sa;
-
-extern "C" {
-
-sa_status sa_chunk_workspace_bytes(const sa_config* cfg, int batch, int64_t n_tokens, size_t* out) {
-    if (!out || batch <= 0 || n_tokens < 0) return SA_ERR_INVALID_ARG;
-    Plan p;
-    const sa_status st = make_plan(cfg, &p);
-    if (st != SA_OK) return st;
-    // (the longest chunk may have all tokens)
-    *out = chunk_workspace(p, n_tokens > 0x7fffffff ? 0x7fffffff : n_tokens * p.G, chunk_blocks_most());
-    return SA_OK;
-}
-
-sa_status sa_chunk_attention(const sa_config* cfg, const sa_cache* cache, const uint16_t* Q, const int64_t* cu_lens_host, int window, int sinks, void* O, int o_dtype,
-                             void* workspace, size_t workspace_bytes, sa_stream stream) {
+// lost: null, or {b, kv_head, tile} of sa_debug_chunk_lost_copy.
+static sa_status chunk_attention(const sa_config* cfg, const sa_cache* cache, const uint16_t* Q, const int64_t* cu_lens_host, int window, int sinks, void* O, int o_dtype, void* workspace,
+                                 size_t workspace_bytes, const int* lost, sa_stream stream) {
     Plan p;
     sa_status st = make_plan(cfg, &p);
     if (st != SA_OK) return st;
     if (p.mulshift || p.addalu || p.shiftadd) return SA_ERR_UNSUPPORTED;      // (decode kernels only)
+    if (lost && (p.d != 64 || p.k != 4 || p.fp16 || p.fp4 || p.int8 || p.nibble)) return SA_ERR_UNSUPPORTED;
     ChunkArgs a{};
     st = check_cache(p, cache, &a.c);
     if (st != SA_OK) return st;
+    if (lost) {
+        if (lost[0] < 0 || lost[0] >= a.c.batch || lost[1] < 0 || lost[1] >= p.Hkv) return SA_ERR_INVALID_ARG;
+        a.lost_b = lost[0], a.lost_head = lost[1], a.lost_tile = lost[2];
+    }
     if (!cu_lens_host || window < 0 || sinks < 0) return SA_ERR_INVALID_ARG;
     if (o_dtype != SA_F16 && o_dtype != SA_BF16) return SA_ERR_UNSUPPORTED;
     int64_t longest = 0;
@@ -123,8 +115,35 @@ sa_status sa_chunk_attention(const sa_config* cfg, const sa_cache* cache, const 
     const float log2e_over_root = 1.4426950408889634f / (p.d == 64 ? 8.0f : 11.313708498984761f);
     a.factor = log2e_over_root * (p.fp16 || p.fp4 ? 1.0f : p.int8 ? 1.0f / 127.0f : 256.0f);       // (power-of-two codes: operands of 2^-120 and 2^112)
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (!launch_kind(p, a, cu_lens_host, false, s) || !launch_kind(p, a, cu_lens_host, true, s)) return SA_ERR_CUDA;
+    if (!launch_kind(p, a, cu_lens_host, false, lost != nullptr, s) || !launch_kind(p, a, cu_lens_host, true, lost != nullptr, s)) return SA_ERR_CUDA;
     return cudaGetLastError() == cudaSuccess ? SA_OK : SA_ERR_CUDA;
+}
+
+}  // namespace sa
+
+using namespace sa;
+
+extern "C" {
+
+sa_status sa_chunk_workspace_bytes(const sa_config* cfg, int batch, int64_t n_tokens, size_t* out) {
+    if (!out || batch <= 0 || n_tokens < 0) return SA_ERR_INVALID_ARG;
+    Plan p;
+    const sa_status st = make_plan(cfg, &p);
+    if (st != SA_OK) return st;
+    // (the longest chunk may have all tokens)
+    *out = chunk_workspace(p, n_tokens > 0x7fffffff ? 0x7fffffff : n_tokens * p.G, chunk_blocks_most());
+    return SA_OK;
+}
+
+sa_status sa_chunk_attention(const sa_config* cfg, const sa_cache* cache, const uint16_t* Q, const int64_t* cu_lens_host, int window, int sinks, void* O, int o_dtype,
+                             void* workspace, size_t workspace_bytes, sa_stream stream) {
+    return chunk_attention(cfg, cache, Q, cu_lens_host, window, sinks, O, o_dtype, workspace, workspace_bytes, nullptr, stream);
+}
+
+sa_status sa_debug_chunk_lost_copy(const sa_config* cfg, const sa_cache* cache, const uint16_t* Q, const int64_t* cu_lens_host, void* O, void* workspace, size_t workspace_bytes,
+                                   int b, int kv_head, int tile, sa_stream stream) {
+    const int lost[3] = {b, kv_head, tile};
+    return chunk_attention(cfg, cache, Q, cu_lens_host, 0, 0, O, SA_F16, workspace, workspace_bytes, lost, stream);
 }
 
 }  // extern "C"

@@ -84,6 +84,7 @@ struct ChunkArgs {
     int copies;                           // SPLIT: 1, 2 or 4 copies of the rows in a tile
     int whole, merged;                    // a unit a block, whatever the lengths: none is cut; else the deal decides: chunk_merge_kernel follows
     int bf16;                             // type of O
+    int lost_b, lost_head, lost_tile;     // LOST (sa_debug_chunk_lost_copy)
     float factor;                         // log2(e) / sqrt(d) and the unit of the operands
     ChunkSeqs s;
 };
@@ -143,6 +144,11 @@ struct ChunkPiece {
 };
 static_assert(sizeof(ChunkPiece) <= 96, "room in the workspace");
 SA_D ChunkPiece* chunk_cut(const ChunkArgs& a, int block) { return reinterpret_cast<ChunkPiece*>(a.workspace + block * 96); }
+// The sums that a piece leaves at place 1 or 2 of its block: [rows][D] outputs, references, sums of weights.
+template <int D, bool SPLIT>
+SA_D float* chunk_slot(const ChunkArgs& a, int block, int place) {
+    return reinterpret_cast<float*>(a.workspace + kChunkCutBytes) + (size_t)(2 * block + place - 1) * chunk_slot_floats(D, SPLIT);
+}
 constexpr int kChunkPieces = 8;           // of them in the ring, as the loader may be several ahead
 
 // Warps of a block, and registers of their threads: what the block is launched with and what the groups of four warps then have of it.
@@ -191,7 +197,7 @@ struct ChunkShared {                      // behind the rings
     float m[256], l[256];                 // SPLIT: of all threads' rows
     float meet[3][512];                   // else: what the two halves of a row tell each other
     int2 info[8];                         // raw_info
-    ChunkPiece pieces[kChunkPieces];
+    ChunkPiece pieces[kChunkPieces], undealt;
     unsigned long long piece_full[kChunkPieces], piece_empty[kChunkPieces];
     int2 raw_info[8];                     // of a place of records: first key; bits 0, 1: which of the tile's pages there are, 2, 3: streams whose rows see all of the tile, 4: some row sees each key
     unsigned long long raw_full[8], raw_empty[8], k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], s_free[2], p_full[2], o_full[2], done;
@@ -200,10 +206,12 @@ struct ChunkShared {                      // behind the rings
 };
 static_assert(sizeof(ChunkShared) <= 14336, "room behind the rings");
 
-// A wait that ends: where the limit is reached (kWaitLimit polls, which sleep for up to 4 us each: a second; LONGER of them where a whole piece is waited for) nothing is
-// waited for any more and the outputs become NaN.  (With a shorter sleep asked for, each poll is a loop of several instructions: a prompt of 8192 tokens, 4 bits, 547 us, not 531.)
-template <uint32_t LONGER = 1>
+// A wait that ends: where the limit is reached (kWaitLimit polls, which sleep for up to 4 us each: a second; LONGER of them where a whole piece is waited for) the warp waits for nothing
+// any more: what it makes from there on goes into no product, and the rows of its block's pieces, this one and those that follow, become NaN (the deal: those that it hands out no more).
+// LOST: the kernel of sa_debug_chunk_lost_copy, where some waits do run out, with a limit of a few ms.  (With a shorter sleep asked for, each poll is a loop of several instructions: a prompt of 8192 tokens, 4 bits, 547 us, not 531.)
+template <uint32_t LONGER, bool LOST>
 struct ChunkWait {
+    static constexpr uint32_t kPolls = LONGER * (LOST ? 1u << 10 : kWaitLimit);
     bool lost = false;
     SA_D static bool poll(uint32_t bar, uint32_t parity) {
         uint32_t ok;
@@ -220,17 +228,19 @@ struct ChunkWait {
         if (!over(at, parity) && !lost) {
             lost = true;
 #pragma unroll 1
-            for (uint32_t i = 0; i < LONGER * kWaitLimit && lost; ++i) lost = !poll(at, parity);
+            for (uint32_t i = 0; i < kPolls && lost; ++i) lost = !poll(at, parity);
         }
         __syncwarp();
     }
 };
 
 // The pieces, one after another: next() gives the one at hand (null: no more), leave() hands its place back.  By a whole warp.  (Its waits are its own: warps that have given
-// up on a tile go on from piece to piece, so that all rows of the block that follow come out as NaN.)
+// up on a tile go on from piece to piece, and write the NaN.  They run out where the deal has given up, all warps' together; it waits for 16 limits, more than the other warps take to give up
+// on whatever they wait for, so that takes a warp that makes no way at all.)
+template <bool LOST>
 struct ChunkReader {
     ChunkShared& sh;
-    ChunkWait<32> wait{};
+    ChunkWait<32, LOST> wait{};
     uint32_t i = 0;
     SA_D const ChunkPiece* next() {
         wait(sh.piece_full[i % kChunkPieces], i / kChunkPieces & 1);
@@ -669,7 +679,24 @@ SA_D void chunk_softmax(ChunkRow& row, const float* scale, uint32_t s_col, uint3
     row.l += l0 + l1;
 }
 
-template <int D, int FMT, bool SPLIT>
+// The rows of a piece that is not handed out: NaN, or its place's sums of weights, so that no merge takes what an earlier call has left there.  By a whole warp.
+template <int D, bool SPLIT>
+SA_D void chunk_undealt(const ChunkArgs& a, const ChunkPiece& p, int lane) {
+    const float nan = __int_as_float(0x7fc00000);
+    if (p.place) {
+        float* slot = chunk_slot<D, SPLIT>(a, blockIdx.x, p.place);
+        for (int r = lane; r < p.rows; r += 32) {
+            slot[chunk_rows(SPLIT) * D + r] = 0.0f;
+            slot[chunk_rows(SPLIT) * (D + 1) + r] = nan;
+        }
+    } else {
+        for (int i = lane; i < p.rows * (D / 8); i += 32)
+            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.O) + p.row(a, i / (D / 8)) * D + i % (D / 8) * 8) = make_uint4(0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu);
+    }
+    __threadfence();
+}
+
+template <int D, int FMT, bool SPLIT, bool LOST>
 __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel(const __grid_constant__ ChunkArgs a) {
     using S = ChunkShape<D, FMT>;
     using Form = ChunkForm<D, SPLIT>;
@@ -712,8 +739,8 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
     tcgen05_after_sync();
     pdl_wait();
     if (a.merged) pdl_launch_dependents();                             // (else a call behind this one that reads its output early would be too early)
-    ChunkWait<> wait;
-    ChunkReader reader{sh};
+    ChunkWait<1, LOST> wait;
+    ChunkReader<LOST> reader{sh};
 
     if (warp < kOperands) {
         // ---- softmax: a row a thread, or half a row's columns
@@ -803,7 +830,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
             }
             // ---- the piece's sums
             float* slot = nullptr;
-            if (p->place) slot = reinterpret_cast<float*>(a.workspace + kChunkCutBytes) + (size_t)(2 * blockIdx.x + p->place - 1) * chunk_slot_floats(D, SPLIT);
+            if (p->place) slot = chunk_slot<D, SPLIT>(a, blockIdx.x, p->place);
             const bool there = row < p->rows;
             if constexpr (!SPLIT) {
                 const float inv = l > 0.0f ? __fdiv_rn(1.0f, l) : l == 0.0f ? 0.0f : l;
@@ -1075,7 +1102,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                 }
                 keys_done += n;
             }
-            ChunkWait<> end;                                           // (products in flight, also where a wait was lost)
+            ChunkWait<1, LOST> end;                                           // (products in flight, also where a wait was lost)
             tcgen05_commit(smem_addr(&sh.done), elected);
             end(sh.done, 0);
         }
@@ -1100,7 +1127,8 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                     const int at0 = __shfl_sync(0xffffffffu, at, 2 * i), at1 = __shfl_sync(0xffffffffu, at, 2 * i + 1), first = __shfl_sync(0xffffffffu, t0, 2 * i);
                     const uint32_t stage = keys_done % S::kStages, before = keys_done - S::kStages;      // (before: the tile whose place this one takes)
                     if (keys_done >= (uint32_t)S::kStages) wait(sh.raw_empty[before % S::kRing], before / S::kRing & 1);
-                    if (lane == 0 && !wait.lost) {
+                    const bool never = LOST && first == a.lost_tile * kChunkTile && p->b == a.lost_b && head == a.lost_head;
+                    if (lane == 0 && !wait.lost && !never) {
                         const uint32_t bar = smem_addr(&sh.raw_full[keys_done % S::kRing]), to = smem_addr(raw + stage * S::kRaw);
                         sh.raw_info[stage] = make_int2(first, (there >> 2 * i & 3) | (whole >> 2 * i & 3) << 2 | (seen >> 2 * i & 1) << 4);
                         mbar_arrive_expect_tx(bar, ((at0 >= 0) + (at1 >= 0)) * 2u * S::kHalf);
@@ -1118,7 +1146,7 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         const uint32_t last = copied < (uint32_t)S::kStages ? copied : (uint32_t)S::kStages;
         for (uint32_t i = 0; i < last; ++i) {
             const uint32_t k = copied - 1 - i;
-            ChunkWait<> landed;
+            ChunkWait<1, LOST> landed;
             landed(sh.raw_full[k % S::kRing], k / S::kRing & 1);
         }
     } else if (warp == kProducts + 2) {
@@ -1176,12 +1204,12 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         }
         uint32_t made = 0;
         bool cut = false;
-        ChunkWait<16> free;
-        bool lost = false;                                             // (no place came free: nothing more is dealt)
+        ChunkWait<16, LOST> free;
+        bool lost = false;                                             // no place came free: nothing more is handed out
         auto place = [&]() -> ChunkPiece& {
-            free(sh.piece_empty[made % kChunkPieces], made / kChunkPieces & 1 ^ 1);
-            lost = __any_sync(0xffffffffu, free.lost);
-            return sh.pieces[made % kChunkPieces];
+            if (!lost) free(sh.piece_empty[made % kChunkPieces], made / kChunkPieces & 1 ^ 1);
+            lost = __any_sync(0xffffffffu, free.lost) || (LOST && a.lost_tile < 0 && (int)made >= -1 - a.lost_tile);
+            return lost ? sh.undealt : sh.pieces[made % kChunkPieces];
         };
         auto ready = [&] {
             __syncwarp();
@@ -1194,7 +1222,6 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
             const int begin = max(skip - kChunkUnitCost, 0), end = max(to - kChunkUnitCost, 0);
             if (end > begin || (u.count == 0 && skip == 0)) {
                 ChunkPiece& p = place();
-                if (lost) break;
                 if (lane == 0) {
                     const int token = a.by_group(u.row0);
                     p.n = end - begin;
@@ -1223,7 +1250,13 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
                         cut = true;
                     }
                 }
-                ready();
+                if (!lost) {
+                    ready();
+                } else {
+                    __syncwarp();
+                    chunk_undealt<D, SPLIT>(a, p, lane);
+                    __syncwarp();
+                }
             }
             at += whole ? 1 : to - skip;
             skip = 0;
@@ -1310,16 +1343,17 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
     __threadfence();
 }
 
-template <int D, int FMT, bool SPLIT>
+template <int D, int FMT, bool SPLIT, bool LOST = false>
 cudaError_t launch_chunk(const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s) {
     static OncePerDevice once;
-    if (!allow_shared(chunk_kernel<D, FMT, SPLIT>, ChunkShape<D, FMT>::kBytes, once)) return cudaGetLastError();
-    const cudaError_t e = launch_pdl(chunk_kernel<D, FMT, SPLIT>, dim3(blocks), dim3(ChunkForm<D, SPLIT>::kThreads), (size_t)ChunkShape<D, FMT>::kBytes, s, a);
+    if (!allow_shared(chunk_kernel<D, FMT, SPLIT, LOST>, ChunkShape<D, FMT>::kBytes, once)) return cudaGetLastError();
+    const cudaError_t e = launch_pdl(chunk_kernel<D, FMT, SPLIT, LOST>, dim3(blocks), dim3(ChunkForm<D, SPLIT>::kThreads), (size_t)ChunkShape<D, FMT>::kBytes, s, a);
     if (e != cudaSuccess || !a.merged) return e;
     return launch_pdl(chunk_merge_kernel<D, SPLIT>, dim3(blocks, (rows_most - 1) / chunk_merge_rows<D, SPLIT>() + 1), dim3(256), 0, s, a);
 }
 
 cudaError_t launch_chunk_pot(int d, int fmt, bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s);
 cudaError_t launch_chunk_plain(int d, int fmt, bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s);
+cudaError_t launch_chunk_lost(bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s);      // (sa_chunk_pot.cu; head_dim 64, PoT-M4 in bytes)
 
 }  // namespace sa

@@ -19,5 +19,8 @@ static cudaError_t launch(int fmt, bool split, const ChunkArgs& a, int blocks, i
 cudaError_t launch_chunk_pot(int d, int fmt, bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s) {
     return d == 64 ? launch<64>(fmt, split, a, blocks, rows_most, s) : launch<128>(fmt, split, a, blocks, rows_most, s);
 }
+cudaError_t launch_chunk_lost(bool split, const ChunkArgs& a, int blocks, int rows_most, cudaStream_t s) {
+    return split ? launch_chunk<64, FMT_BYTE, true, true>(a, blocks, rows_most, s) : launch_chunk<64, FMT_BYTE, false, true>(a, blocks, rows_most, s);
+}
 
 }  // namespace sa

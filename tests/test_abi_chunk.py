@@ -103,3 +103,16 @@ def test_windows_that_are_no_32_bit_numbers():
         (5, 2), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 0), (2 ** 32, 0), (2 ** 32 + 5, 0), (5, 2 ** 32), (5, -2 ** 32))])(np.array([0, 5, 9]))
         if [globals().update(ws=type('W', (), dict(nbytes=1 << 30, data_ptr=lambda self: 256))())] else None""")
     assert got == [3, 3] + ["refused"] * 5
+
+
+def test_lost_copy_hook_refuses():
+    lib, good, cache = sa.lib(), sa.make_config(64, 32, 4, sa.SA_POTM4), sa.SaCache(256, 256, 256, 2, 4, 8)
+
+    def call(cfg=good, b=0, kv_head=0, tile=0, cu=i64(0, 1, 3), ws_bytes=1 << 40):
+        return lib.sa_debug_chunk_lost_copy(C.byref(cfg), C.byref(cache), ONE, cu, FAR, ONE, C.c_size_t(ws_bytes), C.c_int(b), C.c_int(kv_head), C.c_int(tile), NULL)
+
+    for cfg in (sa.make_config(128, 32, 4, sa.SA_POTM4), sa.make_config(64, 32, 4, sa.SA_POTM2), sa.make_config(64, 32, 4, sa.SA_KV_FP4), sa.make_config(64, 32, 4, sa.SA_POTM1, nibble=True)):
+        assert call(cfg=cfg) == 2
+    for bad in (dict(b=2), dict(b=-1), dict(kv_head=4), dict(kv_head=-1), dict(cu=i64(0, 2, 1))):
+        assert call(**bad) == 1, bad
+    assert call(ws_bytes=8) == 4 and call(cu=i64(0, 0, 0), tile=-3) == 0

@@ -407,3 +407,50 @@ def test_one_long_sequence_beside_short_ones():
 
     both, long, short = time([32768] + [100] * 36), time([32768]), time([100] * 36)
     assert both <= 2 * (long + short), (both, long, short)      # (5 times as long where nothing is cut)
+
+
+def lost(call, b, kv_head, tile):
+    """The rows that the hook's call leaves, where they are NaN, and what they hold else: all of a row is NaN or none."""
+    import torch
+    O = torch.full(call.Q.shape, 777.0, dtype=torch.float16, device="cuda")
+    sa.debug_chunk_lost_copy(call.cfg, call.cache.handle, call.Qd, O, call.workspace, call.cu, b, kv_head, tile)
+    torch.cuda.synchronize()
+    nan = O.isnan()
+    assert torch.equal(nan.any(-1), nan.all(-1))
+    return O, nan.all(-1)
+
+
+@pytest.mark.parametrize("lens,new,at,alone", [
+    ([300, 500, 100], [1, 5, 2], (1, 1, 2), True), ([128, 90], [1, 20], (0, 0, 0), True), ([20000, 700], [3, 1], (0, 0, 100), False), ([3000, 500], [700, 400], (0, 1, 10), False),
+    ([3000, 500], [700, 400], (1, 0, 0), False), ([900, 200, 640], [30, 1, 400], (2, 1, 4), False)])
+def test_a_copy_that_never_comes(lens, new, at, alone):
+    """The rows that need the tile are NaN; the others are what they are otherwise, or NaN too where their block had given up (`alone`: blocks have one unit each); the next call is as any."""
+    import torch
+    call = Call(sa.SA_POTM4, False, 64, 8, 2, lens, new, seed=28)
+    want = call()
+    O, nan = lost(call, *at)
+    b, kv_head, tile = at
+    first = max(128 * tile - (lens[b] - new[b]), 0)
+    hit = torch.zeros_like(nan)
+    hit[call.cu[b] + first:call.cu[b + 1], 4 * kv_head:4 * kv_head + 4] = True
+    assert hit.any() and nan[hit].all() and torch.equal(O[~nan], want[~nan])
+    if alone:
+        assert torch.equal(nan, hit)
+    assert torch.equal(call(), want)
+
+
+@pytest.mark.parametrize("pieces", [0, 1, 2])
+@pytest.mark.parametrize("lens,new", [([20000, 3000], [3, 1]), ([3000, 500], [700, 400]), (range(100, 250), [1] * 150), ([2000] * 20, [60] * 20)])
+def test_blocks_that_give_up(lens, new, pieces):
+    """Rows that blocks had not handed out yet are NaN, also where an earlier call has left finite sums of theirs in the workspace."""
+    import torch
+    call = Call(sa.SA_POTM4, False, 64, 8, 2, list(lens), new, seed=29)
+    call()
+    call.Q[:] = call.Q[::-1].copy()
+    workspace, call.workspace = call.workspace, call.workspace.clone()
+    want = call()
+    call.workspace = workspace
+    O, nan = lost(call, 0, 0, -1 - pieces)
+    # (a second piece: with 300 units on fewer than 150 blocks some have one, where an equal stretch is shorter than a unit's fixed cost of 4 tiles and two more none has)
+    assert torch.equal(O[~nan], want[~nan]) and (nan.all() if pieces == 0 else nan.any() or pieces == 2 or len(lens) < 150)
+    assert torch.equal(call(), want)
