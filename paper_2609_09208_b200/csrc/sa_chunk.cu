@@ -115,7 +115,10 @@ static sa_status chunk_attention(const sa_config* cfg, const sa_cache* cache, co
     const float log2e_over_root = 1.4426950408889634f / (p.d == 64 ? 8.0f : 11.313708498984761f);
     a.factor = log2e_over_root * (p.fp16 || p.fp4 ? 1.0f : p.int8 ? 1.0f / 127.0f : 256.0f);       // (power-of-two codes: operands of 2^-120 and 2^112)
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-    if (!launch_kind(p, a, cu_lens_host, false, lost != nullptr, s) || !launch_kind(p, a, cu_lens_host, true, lost != nullptr, s)) return SA_ERR_CUDA;
+    if (!launch_kind(p, a, cu_lens_host, false, lost != nullptr, s) || !launch_kind(p, a, cu_lens_host, true, lost != nullptr, s)) {
+        cudaGetLastError();                                                    // (not the next call's)
+        return SA_ERR_CUDA;
+    }
     return cudaGetLastError() == cudaSuccess ? SA_OK : SA_ERR_CUDA;
 }
 
