@@ -132,6 +132,28 @@ def test_more_heads_from_call_to_call(d, new, heads):
         c.check()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("code,dense,hadamard", [(*c, h) for c in CODES for h in (False, True) if c[0] != sa.SA_KV_FP16 or not h])
+def test_projections_that_are_no_numbers(code, dense, d, hadamard):
+    """Infinities, NaN, numbers beyond binary16 and zeros, with and without norms: the codes and queries of rotate_qkv and fill_kv."""
+    import torch
+    for norm in (False, True):
+        for new in ([1, 1, 1], [9, 70, 33]):
+            cfg = sa.make_config(d, 4, 2, code, nibble=dense, hadamard=hadamard)
+            rot = rotary(cfg, torch.float32, norm=norm)
+            c = Calls(cfg, rot, torch.float32, [5, 61, 0], new, seed=11)
+            gen = torch.Generator(device="cuda").manual_seed(12)
+            at = torch.rand(c.x_new.shape, device="cuda", generator=gen)
+            for i, x in enumerate((torch.inf, -torch.inf, torch.nan, 70000.0, -65520.0, 0.0)):
+                c.x_new[(at >= 0.002 * i) & (at < 0.002 * (i + 1))] = x
+            c.x_new[-1, -d:], c.x_new[-1, 4 * d:5 * d] = 0, 0
+            c.x[c.at] = c.x_new
+            sa.rotate_qkv(rot, *c.parts(c.x), c.pos, *c.rows)
+            c.caches[1].fill(c.rows[1], c.rows[2], c.cu_all)
+            c.append()
+            c.check()
+
+
 @pytest.mark.parametrize("code", [sa.SA_KV_FP4, sa.SA_POTM2])
 def test_pages_that_are_not_mapped(code):
     """A sequence of which one page is missing is left as it is, its queries are not; the others get their tokens."""

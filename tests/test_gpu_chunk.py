@@ -328,6 +328,31 @@ def test_queries_that_are_no_numbers(code, d, Hq, Hkv, new):
     assert got[bad & ~nothing].isnan().all()
 
 
+@pytest.mark.parametrize("d,Hq,Hkv", [(64, 8, 2), (128, 6, 2)])
+@pytest.mark.parametrize("code", [sa.SA_POTM4, sa.SA_POT4, sa.SA_INT8, sa.SA_KV_FP4, sa.SA_KV_FP16])
+@pytest.mark.parametrize("new", [1, 40, 200])
+def test_tokens_that_are_no_numbers(code, d, Hq, Hkv, new):
+    """A key with a NaN shows in every query that sees it, and in no other sequence or KV head; a value with one too, where the cache can hold it."""
+    import torch
+    call = Call(code, False, d, Hq, Hkv, [300, 305, 260], [new] * 3, seed=30)
+    clean = call()
+    cu, c, G = call.case.cu_lens, call.case, Hq // Hkv
+    place = 300 - 1 - new // 2                                  # the token of query new - 1 - new // 2
+    which = [c.K] + [c.V] * (code in (sa.SA_KV_FP16, sa.SA_KV_FP4))
+    for x in which:
+        keep = x[cu[0] + place, 1].copy()
+        x[cu[0] + place, 1, 7] = np.nan
+        call.cache.fill(up(c.K), up(c.V), cu)
+        got = call()
+        torch.cuda.synchronize()
+        x[cu[0] + place, 1] = keep
+        sees = torch.zeros(call.Q.shape[:2], dtype=torch.bool, device="cuda")
+        sees[new - 1 - new // 2:new, G:2 * G] = True
+        shows = got.isnan().any(-1)
+        assert shows[sees].all() and not shows[new:].any() and not shows[:, :G].any()
+        assert torch.equal(got[new:], clean[new:]) and torch.equal(got[:, :G], clean[:, :G])
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("T,n", [(257, 1), (257, 100), (3000, 200), (20000, 2)])
 def test_values_of_the_largest_magnitude(d, T, n):
