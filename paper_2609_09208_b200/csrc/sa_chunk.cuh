@@ -477,8 +477,10 @@ SA_D float chunk_queries(const ChunkArgs& a, uint32_t operand, int lane, int fir
             const float d = __shfl_sync(0xffffffffu, top && number ? delta : 1.0f, (lane % RPW) * LPV);      // (a query of zeros: any factor but zero)
             if (lane / RPW == half * STEPS + i) mine = d * a.factor;
         } else if (any[i]) {
+            uint32_t zero[2] = {mul_half2(x[i][0], 0u), mul_half2(x[i][1], 0u)};        // (or NaN)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][0] = fma_half2(x[i][e], 0u, x[i][0]);      // (times zero)
+            for (int e = 2; e < 8; ++e) zero[e & 1] = fma_half2(x[i][e], 0u, zero[e & 1]);
+            x[i][0] = fma_half2(zero[0], 0u, fma_half2(zero[1], 0u, x[i][0]));
         }
         const int row = first_row + row0 + i * RPW + lane / LPV;
         put_operand(operand, row, 2 * f.blk, x[i][0], x[i][1], x[i][2], x[i][3]);
@@ -1207,61 +1209,67 @@ __global__ void __launch_bounds__(ChunkForm<D, SPLIT>::kThreads, 1) chunk_kernel
         ChunkWait<16, LOST> free;
         bool lost = false;                                             // no place came free: nothing more is handed out
         auto place = [&]() -> ChunkPiece& {
-            if (!lost) free(sh.piece_empty[made % kChunkPieces], made / kChunkPieces & 1 ^ 1);
+            free(sh.piece_empty[made % kChunkPieces], made / kChunkPieces & 1 ^ 1);
             lost = __any_sync(0xffffffffu, free.lost) || (LOST && a.lost_tile < 0 && (int)made >= -1 - a.lost_tile);
-            return lost ? sh.undealt : sh.pieces[made % kChunkPieces];
+            return sh.pieces[made % kChunkPieces];
         };
         auto ready = [&] {
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_addr(&sh.piece_full[made % kChunkPieces]));
             ++made;
         };
-        while (at < end_at) {
-            const ChunkUnit u = chunk_unit(a, sh.lens, flat, per_tile);
-            const int cost = kChunkUnitCost + u.count, to = whole || end_at - at >= (uint64_t)(cost - skip) ? cost : skip + (int)(end_at - at);
-            const int begin = max(skip - kChunkUnitCost, 0), end = max(to - kChunkUnitCost, 0);
-            if (end > begin || (u.count == 0 && skip == 0)) {
-                ChunkPiece& p = place();
-                if (lane == 0) {
-                    const int token = a.by_group(u.row0);
-                    p.n = end - begin;
-                    p.head = head;
-                    p.b = a.s.b[u.seq];
-                    p.rows = u.rows;
-                    p.token_row = u.row0 - token * a.G;
-                    p.token = u.first;
-                    p.q_token = a.s.row0[u.seq] + token;
-                    p.lo = u.lo;
-                    p.hi = u.hi;
-                    p.sink_tiles = u.sink_tiles;
-                    p.window_tile = u.window_tile;
-                    p.begin = begin;
-                    p.place = begin == 0 && end == u.count ? 0 : begin == 0 ? 2 : 1;
-                    if (p.place == 2) {
-                        const uint64_t last = at - skip + cost - 1;    // where the unit's last tile is
-                        p.last_block = (int)(last >> 32 == 0 ? (uint32_t)last / (uint32_t)per : last / per);
+        auto deal = [&](auto whether) {
+            constexpr bool handed_out = decltype(whether)::value;
+            while (at < end_at) {
+                const ChunkUnit u = chunk_unit(a, sh.lens, flat, per_tile);
+                const int cost = kChunkUnitCost + u.count, to = whole || end_at - at >= (uint64_t)(cost - skip) ? cost : skip + (int)(end_at - at);
+                const int begin = max(skip - kChunkUnitCost, 0), end = max(to - kChunkUnitCost, 0);
+                if (end > begin || (u.count == 0 && skip == 0)) {
+                    ChunkPiece& p = handed_out ? place() : sh.undealt;
+                    if (handed_out && lost) return;
+                    if (lane == 0) {
+                        const int token = a.by_group(u.row0);
+                        p.n = end - begin;
+                        p.head = head;
+                        p.b = a.s.b[u.seq];
+                        p.rows = u.rows;
+                        p.token_row = u.row0 - token * a.G;
+                        p.token = u.first;
+                        p.q_token = a.s.row0[u.seq] + token;
+                        p.lo = u.lo;
+                        p.hi = u.hi;
+                        p.sink_tiles = u.sink_tiles;
+                        p.window_tile = u.window_tile;
+                        p.begin = begin;
+                        p.place = begin == 0 && end == u.count ? 0 : begin == 0 ? 2 : 1;
+                        if (p.place == 2) {
+                            const uint64_t last = at - skip + cost - 1;    // where the unit's last tile is
+                            p.last_block = (int)(last >> 32 == 0 ? (uint32_t)last / (uint32_t)per : last / per);
+                        }
+                        for (int i = 0; i < 2; ++i) {
+                            p.first[i] = p.position(a, SPLIT ? 0 : min(i * 128, u.rows - 1));
+                            p.last[i] = p.position(a, SPLIT ? u.rows - 1 : min(i * 128 + 127, u.rows - 1));
+                        }
+                        if (p.place == 2) {
+                            *chunk_cut(a, blockIdx.x) = p;
+                            cut = true;
+                        }
                     }
-                    for (int i = 0; i < 2; ++i) {
-                        p.first[i] = p.position(a, SPLIT ? 0 : min(i * 128, u.rows - 1));
-                        p.last[i] = p.position(a, SPLIT ? u.rows - 1 : min(i * 128 + 127, u.rows - 1));
-                    }
-                    if (p.place == 2) {
-                        *chunk_cut(a, blockIdx.x) = p;
-                        cut = true;
+                    if (handed_out) {
+                        ready();
+                    } else {
+                        __syncwarp();
+                        chunk_undealt<D, SPLIT>(a, p, lane);
+                        __syncwarp();
                     }
                 }
-                if (!lost) {
-                    ready();
-                } else {
-                    __syncwarp();
-                    chunk_undealt<D, SPLIT>(a, p, lane);
-                    __syncwarp();
-                }
+                at += whole ? 1 : to - skip;
+                skip = 0;
+                if (++flat == n_flat) flat = 0, ++head;
             }
-            at += whole ? 1 : to - skip;
-            skip = 0;
-            if (++flat == n_flat) flat = 0, ++head;
-        }
+        };
+        deal(std::true_type());
+        if (lost) deal(std::false_type());
         if (lane == 0 && !cut) chunk_cut(a, blockIdx.x)->place = 0;
         if (!lost) {
             ChunkPiece& p = place();
