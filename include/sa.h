@@ -269,7 +269,7 @@ sa_status sa_append_qkv(const sa_config* cfg, const sa_cache* cache, const sa_ro
  * rounded to 8 bits first, as in sa_decode_attention.  All codes and containers; of the flags SA_FLAG_HADAMARD only.  FP32 statistics and sums; a weight enters as
  * one binary16 number (which costs no more than the rounding of O).  A query that sees no token (p < 0, or none of its pages is mapped) yields zeros, whatever it
  * holds; else one with an infinity or a NaN yields NaN.  Rows of O outside cu_lens_host[0] .. cu_lens_host[batch] are not touched.  Q and O must not overlap.  What tokens hold that no query of a call sees does not matter; a token with an
- * infinity or a NaN that some of a sequence's queries see may show in the others.  cu_lens_host: HOST array of batch + 1 entries, read during the call; seq_lens is
+ * infinity or a NaN that some of a sequence's queries see may show in the others (a key whose score is minus infinity weighs nothing).  cu_lens_host: HOST array of batch + 1 entries, read during the call; seq_lens is
  * read on the device (a captured call follows it).  workspace: sa_chunk_workspace_bytes, 256-byte aligned, any contents, not shared by calls that overlap on the GPU;
  * ask for it on the device that the call will run on, with the most tokens that a call has.  Deterministic run to run. */
 sa_status sa_chunk_workspace_bytes(const sa_config* cfg, int batch, int64_t n_tokens, size_t* out);

@@ -5,8 +5,8 @@
 // vector, a lane a block of 16 channels: no trip of theirs through memory, and no second launch.  The places a block takes start at a multiple of their
 // number, wherever the sequence ends, so that a byte which two tokens share (4-bit values) belongs to one lane.
 //
-// What bounds it (in a CUDA graph): long chunks memory, projections in, queries and codes out,: 4 chunks of up to 5001 tokens, 32 / 8 heads of 128, FP32
-// to rotated INT8 codes 77 us, 81 % of the copy rate (sa_rotate_qkv and sa_fill_kv would move the keys and values twice more).  Few tokens: a launch of 2.3 us and one latency after another, length, page,
+// What bounds it (in a CUDA graph): long chunks memory and the way there (projections in, queries and codes out; a block loads, waits and codes without overlap): 4 chunks of up to 5001
+// tokens, 32 / 8 heads of 128, FP32 to rotated INT8 codes 77 us for 349 MB, 69 % of the copy rate (sa_rotate_qkv and sa_fill_kv would move the keys and values twice more).  Few tokens: a launch of 2.3 us and one latency after another, length, page,
 // projections, rotation, codes: one token 4.3 us, 32 single tokens 8.2, a chunk of 2048 (with the launch that moves the lengths) 9.2.
 #pragma once
 #include "sa_cache_write.cuh"
