@@ -25,7 +25,7 @@
 //
 // What bounds it (in a CUDA graph; TFLOP/s of products that are needed):
 //   head_dim 64, many rows: the powers.  256 rows x 128 keys take 2048 cycles of the unit for 2^x and about 3600 in all: it is busy for 63 %, issue slots for 62 %, the tensor core for 30 %.
-//     2048 tokens over 32 768 PoT-M4 keys, 32 / 4 heads: 800 us, 663 TFLOP/s (585 with the powers left out, 528 with the codes' conversion left out as well).
+//     2048 tokens over 32 768 PoT-M4 keys, 32 / 4 heads: 806 us, 660 TFLOP/s (585 with the powers left out, 528 with the codes' conversion left out as well).
 //   head_dim 128, many rows: products (2050 cycles a tile at the rate of a library's) and powers (2048) beside one another.  8192 tokens, 32 / 8 heads, 4 bits: 517 us,
 //     1060 TFLOP/s, 65 % of that rate; 4096 tokens over binary16 keys 168 us.
 //   few rows (SPLIT): the way of a tile through the warps, each of which waits for the one before: 1400 cycles a tile, where 730 are what memory needs, and all but 200 of them
